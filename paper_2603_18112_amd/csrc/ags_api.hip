@@ -1385,3 +1385,7 @@ extern "C" ags_status ags_stats_noalloc(const ags_config* cfg, const float* d_w,
     }
     return AGS_OK;
 }
+
+// ------------------------------------------------------- further operators --
+
+#include "ags_clip_api.inc"

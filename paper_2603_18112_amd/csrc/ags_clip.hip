@@ -1,0 +1,274 @@
+// gfx950 kernels of gradient clipping (include/ags_clip.h).
+//
+// clip_norm_kernel   one block per piece: the piece's sum (or maximum) in
+//                    fp64; the block that finishes last adds the partials of
+//                    each group in index order and writes N_g and c_g.
+// clip_scale_kernel  one block per piece: out = x c_g.  In place, blocks of a
+//                    group with c_g = 1 exit at once.
+//
+// Both stream from HBM (about one flop per byte) and use no matrix cores.
+#include <math.h>
+
+#include "ags_clip_internal.h"
+
+namespace ags {
+namespace {
+
+constexpr int kWaves = kClipBlock / 64;
+
+__device__ __forceinline__ float bf16_value(unsigned short b) {
+    return __uint_as_float((unsigned)b << 16);
+}
+
+// Round to nearest even; a NaN keeps its sign and stays a NaN.
+__device__ __forceinline__ unsigned short bf16_round(float x) {
+    const unsigned u = __float_as_uint(x);
+    if ((u & 0x7fffffffu) > 0x7f800000u) return (unsigned short)((u >> 16) | 0x40u);
+    return (unsigned short)((u + 0x7fffu + ((u >> 16) & 1u)) >> 16);
+}
+
+template <int KIND>
+__device__ __forceinline__ double accumulate(double acc, float x) {
+    if (KIND == AGS_CLIP_L2) return fma((double)x, (double)x, acc);
+    if (KIND == AGS_CLIP_L1) return acc + fabs((double)x);
+    const double a = fabs((double)x);
+    return a > acc || a != a ? a : acc;  // a NaN replaces and is never replaced
+}
+
+template <int KIND>
+__device__ __forceinline__ double combine(double a, double b) {
+    if (KIND != AGS_CLIP_MAX) return a + b;
+    return b > a || b != b ? b : a;
+}
+
+template <int KIND>
+__device__ __forceinline__ double wave_reduce(double v) {
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) v = combine<KIND>(v, __shfl_xor(v, off, 64));
+    return v;
+}
+
+template <typename T>
+struct Load8;  // 8 consecutive elements at a 16-byte boundary, as fp32
+template <>
+struct Load8<float> {
+    static __device__ __forceinline__ void get(const float* p, float* x) {
+        const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+        x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+    }
+    static __device__ __forceinline__ float one(const float* p) { return *p; }
+    static __device__ __forceinline__ void put(float* p, const float* x) {
+        reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+        reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+    }
+    static __device__ __forceinline__ void put_one(float* p, float x) { *p = x; }
+};
+template <>
+struct Load8<unsigned short> {
+    static __device__ __forceinline__ void get(const unsigned short* p, float* x) {
+        const uint4 v = *reinterpret_cast<const uint4*>(p);
+        const unsigned w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = __uint_as_float(w[i] << 16);
+            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    }
+    static __device__ __forceinline__ float one(const unsigned short* p) { return bf16_value(*p); }
+    static __device__ __forceinline__ void put(unsigned short* p, const float* x) {
+        unsigned w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = bf16_round(x[2 * i]) | ((unsigned)bf16_round(x[2 * i + 1]) << 16);
+        *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    static __device__ __forceinline__ void put_one(unsigned short* p, float x) { *p = bf16_round(x); }
+};
+
+// Elements before p's next 16-byte boundary, at most n.
+template <typename T>
+__device__ __forceinline__ int head_elems(const T* p, int n) {
+    const int h = (int)((16u - ((unsigned)reinterpret_cast<uintptr_t>(p) & 15u)) & 15u) / (int)sizeof(T);
+    return min(h, n);
+}
+
+template <int KIND, typename T>
+__device__ __forceinline__ double piece_sum(const T* p, int n) {
+    const int tid = threadIdx.x, head = head_elems(p, n);
+    double acc = 0.0, acc2 = 0.0;
+    if (tid < head) acc = accumulate<KIND>(acc, Load8<T>::one(p + tid));
+    p += head;
+    n -= head;
+    const int groups = n / 8;
+    int i = tid;
+    for (; i + 3 * kClipBlock < groups; i += 4 * kClipBlock) {
+        float x[4][8];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) Load8<T>::get(p + (size_t)(i + u * kClipBlock) * 8, x[u]);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) {
+                acc = accumulate<KIND>(acc, x[u][j]);
+                acc2 = accumulate<KIND>(acc2, x[u][j + 1]);
+            }
+    }
+    for (; i < groups; i += kClipBlock) {
+        float x[8];
+        Load8<T>::get(p + (size_t)i * 8, x);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc = accumulate<KIND>(acc, x[j]);
+    }
+    const int tail = groups * 8 + tid;
+    if (tail < n) acc = accumulate<KIND>(acc, Load8<T>::one(p + tail));
+    return combine<KIND>(acc, acc2);
+}
+
+template <int KIND>
+__device__ __forceinline__ void write_group(const ClipArgs& a, int g, double sum) {
+    const double norm = KIND == AGS_CLIP_L2 ? sqrt(sum) : sum;
+    a.norms[g] = (float)norm;
+    const double r = a.max_norm / (norm + a.eps);
+    // c_g in two factors, so that one too small for a normal fp32 value keeps
+    // its 24 bits (fp32 gradients of a norm above 1e38); a NaN stays one.
+    const bool tiny = r < 0x1p-100;
+    a.coef[g] = r >= 1.0 ? make_float2(1.0f, 1.0f)
+                         : make_float2((float)(tiny ? r * 0x1p100 : r), tiny ? 0x1p-100f : 1.0f);
+}
+
+__device__ __forceinline__ const void* base_of(const ClipArgs& a, int i) {
+    return a.table ? a.table[i] : a.ptr[i];
+}
+
+template <int KIND>
+__global__ __launch_bounds__(kClipBlock) void clip_norm_kernel(ClipArgs a) {
+    __shared__ double sh[kWaves];
+    __shared__ int sh_last;
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    const ClipPiece pc = a.pieces[blockIdx.x];
+    const void* base = base_of(a, pc.in_base);
+    double v = pc.in_dt == AGS_F32
+                   ? piece_sum<KIND>(static_cast<const float*>(base) + pc.in_off, pc.count)
+                   : piece_sum<KIND>(static_cast<const unsigned short*>(base) + pc.in_off, pc.count);
+    v = wave_reduce<KIND>(v);
+    if (lane == 0) sh[wave] = v;
+    __syncthreads();
+    if (tid == 0) {
+        v = sh[0];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) v = combine<KIND>(v, sh[w]);
+        // The partial goes past the XCD's L2, and its store is complete
+        // before the count says so.
+        __hip_atomic_store(&a.partials[blockIdx.x], v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const unsigned n = __hip_atomic_fetch_add(a.done, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+        sh_last = n + 1 == (unsigned)a.n_pieces;
+    }
+    __syncthreads();
+    if (!sh_last) return;
+    // The last block: few groups take the whole block each, many a wave each.
+    const bool by_wave = a.n_groups >= kWaves;
+    const int first = by_wave ? wave : 0, stride = by_wave ? kWaves : 1;
+    const int t = by_wave ? lane : tid, nt = by_wave ? 64 : kClipBlock;
+    for (int g = first; g < a.n_groups; g += stride) {
+        const int b = a.group_begin[g], e = a.group_begin[g + 1];
+        double s = 0.0;
+        for (int i = b + t; i < e; i += nt)
+            s = combine<KIND>(s, __hip_atomic_load(&a.partials[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+        s = wave_reduce<KIND>(s);
+        if (by_wave) {
+            if (lane == 0) write_group<KIND>(a, g, s);
+            continue;
+        }
+        __syncthreads();
+        if (lane == 0) sh[wave] = s;
+        __syncthreads();
+        if (tid == 0) {
+            for (int w = 1; w < kWaves; ++w) s = combine<KIND>(s, sh[w]);
+            write_group<KIND>(a, g, s);
+        }
+    }
+    if (tid == 0) *a.done = 0u;
+}
+
+template <typename TI, typename TO>
+__device__ __forceinline__ void piece_scale(const TI* in, TO* out, int n, float2 c) {
+    const int tid = threadIdx.x, head = head_elems(in, n);
+    if ((reinterpret_cast<uintptr_t>(out + head) & 15u) != 0) {
+        // the two sides' boundaries differ: element by element
+        for (int i = tid; i < n; i += kClipBlock) Load8<TO>::put_one(out + i, Load8<TI>::one(in + i) * c.x * c.y);
+        return;
+    }
+    if (tid < head) Load8<TO>::put_one(out + tid, Load8<TI>::one(in + tid) * c.x * c.y);
+    in += head;
+    out += head;
+    n -= head;
+    const int groups = n / 8;
+    int i = tid;
+    for (; i + kClipBlock < groups; i += 2 * kClipBlock) {
+        float x[2][8];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) Load8<TI>::get(in + (size_t)(i + u * kClipBlock) * 8, x[u]);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[u][j] = x[u][j] * c.x * c.y;
+            Load8<TO>::put(out + (size_t)(i + u * kClipBlock) * 8, x[u]);
+        }
+    }
+    for (; i < groups; i += kClipBlock) {
+        float x[8];
+        Load8<TI>::get(in + (size_t)i * 8, x);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = x[j] * c.x * c.y;
+        Load8<TO>::put(out + (size_t)i * 8, x);
+    }
+    const int tail = groups * 8 + tid;
+    if (tail < n) Load8<TO>::put_one(out + tail, Load8<TI>::one(in + tail) * c.x * c.y);
+}
+
+__global__ __launch_bounds__(kClipBlock) void clip_scale_kernel(ClipArgs a) {
+    // Backwards: the norm's pass left its last pieces in the caches.
+    const ClipPiece pc = a.pieces[a.n_pieces - 1 - blockIdx.x];
+    const float2 c = a.coef[pc.group];
+    if (a.in_place && c.x == 1.0f && c.y == 1.0f) return;
+    const void* in = base_of(a, pc.in_base);
+    void* out = const_cast<void*>(a.in_place ? in : base_of(a, a.n_in + pc.out_base));
+    const int64_t oo = a.in_place ? pc.in_off : pc.out_off;
+    const int odt = a.in_place ? pc.in_dt : pc.out_dt;
+    if (pc.in_dt == AGS_F32) {
+        const float* p = static_cast<const float*>(in) + pc.in_off;
+        if (odt == AGS_F32) piece_scale(p, static_cast<float*>(out) + oo, pc.count, c);
+        else piece_scale(p, static_cast<unsigned short*>(out) + oo, pc.count, c);
+    } else {
+        const unsigned short* p = static_cast<const unsigned short*>(in) + pc.in_off;
+        if (odt == AGS_F32) piece_scale(p, static_cast<float*>(out) + oo, pc.count, c);
+        else piece_scale(p, static_cast<unsigned short*>(out) + oo, pc.count, c);
+    }
+}
+
+__global__ void clip_table_kernel(ClipTableArgs a) {
+    for (int i = threadIdx.x; i < a.count; i += blockDim.x) a.table[a.first + i] = a.ptr[i];
+}
+
+}  // namespace
+
+hipError_t launch_clip_table(const ClipTableArgs& a, hipStream_t s) {
+    hipLaunchKernelGGL(clip_table_kernel, dim3(1), dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_clip_norm(const ClipArgs& a, int kind, hipStream_t s) {
+    const dim3 grid(a.n_pieces), block(kClipBlock);
+    switch (kind) {
+        case AGS_CLIP_L2: hipLaunchKernelGGL(clip_norm_kernel<AGS_CLIP_L2>, grid, block, 0, s, a); break;
+        case AGS_CLIP_L1: hipLaunchKernelGGL(clip_norm_kernel<AGS_CLIP_L1>, grid, block, 0, s, a); break;
+        default: hipLaunchKernelGGL(clip_norm_kernel<AGS_CLIP_MAX>, grid, block, 0, s, a); break;
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_clip_scale(const ClipArgs& a, hipStream_t s) {
+    hipLaunchKernelGGL(clip_scale_kernel, dim3(a.n_pieces), dim3(kClipBlock), 0, s, a);
+    return hipGetLastError();
+}
+
+}  // namespace ags
