@@ -12,10 +12,13 @@ INCLUDE = os.path.join(ROOT, "include")
 LIBDIR = os.path.join(PKG, "_lib")
 LIB = os.path.join(LIBDIR, "libags.so")
 SOURCES = [os.path.join(CSRC, "ags_api.hip"), os.path.join(CSRC, "ags_kernels.hip"),
-           os.path.join(CSRC, "ags_plan.cpp"), os.path.join(CSRC, "ags_clip.hip")]
+           os.path.join(CSRC, "ags_plan.cpp"), os.path.join(CSRC, "ags_clip.hip"),
+           os.path.join(CSRC, "ags_mx_quant.hip"), os.path.join(CSRC, "ags_mx_product.hip")]
 HEADERS = [os.path.join(CSRC, "ags_internal.h"), os.path.join(INCLUDE, "ags.h"),
            os.path.join(INCLUDE, "ags_plan.h"), os.path.join(INCLUDE, "ags_clip.h"),
-           os.path.join(CSRC, "ags_clip_internal.h"), os.path.join(CSRC, "ags_clip_api.inc")]
+           os.path.join(CSRC, "ags_clip_internal.h"), os.path.join(CSRC, "ags_clip_api.inc"),
+           os.path.join(INCLUDE, "ags_mx.h"), os.path.join(CSRC, "ags_mx_internal.h"),
+           os.path.join(CSRC, "ags_mx_device.h"), os.path.join(CSRC, "ags_mx_api.inc")]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

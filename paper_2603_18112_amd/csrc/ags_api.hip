@@ -1389,3 +1389,4 @@ extern "C" ags_status ags_stats_noalloc(const ags_config* cfg, const float* d_w,
 // ------------------------------------------------------- further operators --
 
 #include "ags_clip_api.inc"
+#include "ags_mx_api.inc"

@@ -1,0 +1,312 @@
+"""Python binding of the libags 4-bit operators (include/ags_mx.h): argument
+marshalling only; storing, reading back and multiplying run in the HIP
+kernels of the library.
+"""
+from __future__ import annotations
+
+import ctypes
+
+from . import ags
+
+AGS_MX_BLOCK, AGS_MX_PAD = 32, 256
+EXPORTS = ("ags_mx_bytes", "ags_mx_quantize", "ags_mx_dequantize", "ags_mx_product_workspace",
+           "ags_mx_product", "ags_mx_linear_workspace", "ags_mx_linear")
+
+
+class ags_mx_tensor(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("cols", ctypes.c_int64)]
+
+
+_sig_done = False
+
+
+def _lib():
+    global _sig_done
+    lib = ags.load_library()
+    if not _sig_done:
+        P, vp, c_int, i32, i64, sz = (ctypes.POINTER, ctypes.c_void_p, ctypes.c_int, ctypes.c_int32,
+                                      ctypes.c_int64, ctypes.c_size_t)
+        T = P(ags_mx_tensor)
+        sig = {
+            "ags_mx_bytes": [i64, i64, P(sz), P(sz)],
+            "ags_mx_quantize": [vp, c_int, i64, i64, i64, vp, i64, T, T, vp],
+            "ags_mx_dequantize": [T, vp, c_int, i64, vp],
+            "ags_mx_product_workspace": [i64, i64, i64, P(sz)],
+            "ags_mx_product": [T, T, vp, c_int, i64, i32, vp, sz, vp],
+            "ags_mx_linear_workspace": [i64, i64, i64, P(sz)],
+            "ags_mx_linear": [vp, c_int, i64, i64, T, vp, c_int, i64, vp, sz, vp],
+        }
+        for name, args in sig.items():
+            f = getattr(lib, name)
+            f.restype = c_int
+            f.argtypes = args
+        _sig_done = True
+    return lib
+
+
+def _check(status):
+    if status != ags.AGS_OK:
+        raise ags.AGSError(status, ags.ags_last_error(None))
+
+
+# ------------------------------------------------------------ thin calls --
+# Same names and arguments as the C functions; pointers are ints.
+
+
+def ags_mx_bytes(rows: int, cols: int):
+    """(bytes of the codes, bytes of the scales)"""
+    c, s = ctypes.c_size_t(0), ctypes.c_size_t(0)
+    _check(_lib().ags_mx_bytes(int(rows), int(cols), ctypes.byref(c), ctypes.byref(s)))
+    return int(c.value), int(s.value)
+
+
+def ags_mx_quantize(d_x, dtype, rows, cols, row_stride, d_noise, noise_stride, q, qt, stream=0):
+    _check(_lib().ags_mx_quantize(d_x, dtype, rows, cols, row_stride, d_noise, noise_stride,
+                                  None if q is None else ctypes.byref(q),
+                                  None if qt is None else ctypes.byref(qt), stream))
+
+
+def ags_mx_dequantize(q, d_out, dtype, row_stride, stream=0):
+    _check(_lib().ags_mx_dequantize(ctypes.byref(q), d_out, dtype, row_stride, stream))
+
+
+def ags_mx_product_workspace(m: int, n: int, k: int) -> int:
+    b = ctypes.c_size_t(0)
+    _check(_lib().ags_mx_product_workspace(m, n, k, ctypes.byref(b)))
+    return b.value
+
+
+def ags_mx_product(a, b, d_out, dtype, row_stride, accumulate=0, d_workspace=None, workspace_bytes=0,
+                   stream=0):
+    _check(_lib().ags_mx_product(ctypes.byref(a), ctypes.byref(b), d_out, dtype, row_stride, accumulate,
+                                 d_workspace, workspace_bytes, stream))
+
+
+def ags_mx_linear_workspace(rows: int, n: int, k: int) -> int:
+    b = ctypes.c_size_t(0)
+    _check(_lib().ags_mx_linear_workspace(rows, n, k, ctypes.byref(b)))
+    return b.value
+
+
+def ags_mx_linear(d_x, dtype, rows, row_stride, w, d_y, y_dtype, y_stride, d_workspace=None,
+                  workspace_bytes=0, stream=0):
+    _check(_lib().ags_mx_linear(d_x, dtype, rows, row_stride, ctypes.byref(w), d_y, y_dtype, y_stride,
+                                d_workspace, workspace_bytes, stream))
+
+
+# ------------------------------------------------------- torch convenience --
+# Device memory and streams come from torch; work goes on the current stream
+# (choose another with torch.cuda.stream).
+
+_torch = None
+
+
+def _t():
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    return _torch
+
+
+def _dtype(dtype):
+    """(AGS_F32 or AGS_BF16, torch dtype) of "f32", "bf16" or a torch dtype."""
+    t = _t()
+    if dtype is t.bfloat16 or dtype == "bf16":
+        return ags.AGS_BF16, t.bfloat16
+    if dtype is t.float32 or dtype == "f32":
+        return ags.AGS_F32, t.float32
+    raise ValueError(f"dtype {dtype!r} is neither float32 nor bfloat16")
+
+
+def _stream(device):
+    return _t().cuda.current_stream(device).cuda_stream
+
+
+def _matrix(x, what):
+    """x as 2-D with unit column stride: (tensor, rows, cols, row stride)."""
+    if not x.is_cuda:
+        raise ValueError(f"{what} must be a CUDA tensor")
+    if x.dim() != 2:
+        if x.dim() == 0:
+            raise ValueError(f"{what} needs at least one dimension")
+        x = x.reshape(-1, x.shape[-1])
+    rows, cols = x.shape
+    if cols > 1 and x.stride(1) != 1:
+        raise ValueError(f"{what} must be contiguous along its last axis")
+    stride = x.stride(0) if rows > 1 else cols
+    if stride < cols:
+        raise ValueError(f"{what}'s rows overlap")
+    return x, rows, cols, stride
+
+
+def _device_guard(device):
+    t = _t()
+    if device.index is not None and device.index != t.cuda.current_device():
+        raise ValueError("the tensors are not on the current device")
+
+
+class MX4:
+    """A [rows, cols] tensor held in 4 bits, blocked along its columns."""
+
+    __slots__ = ("codes", "scales", "rows", "cols", "c")
+
+    def __init__(self, rows, cols, device=None):
+        t = _t()
+        nc, ns = ags_mx_bytes(rows, cols)
+        dev = t.device("cuda", t.cuda.current_device()) if device is None else device
+        self.codes = t.empty(nc, dtype=t.uint8, device=dev)
+        self.scales = t.empty(ns, dtype=t.uint8, device=dev)
+        self.rows, self.cols = int(rows), int(cols)
+        self.c = ags_mx_tensor(self.codes.data_ptr() or None, self.scales.data_ptr() or None, self.rows,
+                               self.cols)
+
+    @property
+    def shape(self):
+        return self.rows, self.cols
+
+
+def _quantize(x, noise, q, qt):
+    if x.dim() == 2 and x.stride(1) != 1 and x.stride(0) == 1 and x.shape[1] > 1:
+        # a transposed view: the two forms change places
+        qt, q = _quantize(x.t(), None if noise is None else noise.t().contiguous(), qt, q)
+        return q, qt
+    x, rows, cols, stride = _matrix(x, "x")
+    _device_guard(x.device)
+    dt = _dtype(x.dtype)[0]
+    n_ptr, n_stride = None, 0
+    if noise is not None:
+        noise, r, c, n_stride = _matrix(noise, "noise")
+        if noise.dtype is not _t().uint8 or (r, c) != (rows, cols):
+            raise ValueError("noise must hold one uint8 for each element of x")
+        n_ptr = noise.data_ptr()
+    if q is True:
+        q = MX4(rows, cols, x.device)
+    if qt is True:
+        qt = MX4(cols, rows, x.device)
+    ags_mx_quantize(x.data_ptr(), dt, rows, cols, stride, n_ptr, n_stride, q and q.c, qt and qt.c,
+                    _stream(x.device))
+    return q, qt
+
+
+def quantize(x, noise=None, out=None):
+    """x [..., cols] in 4 bits, blocked along its columns: an MX4 of
+    [rows, cols].  noise: random bytes (uint8, x's shape) for stochastic
+    rounding.  out: an MX4 to write."""
+    return _quantize(x, noise, True if out is None else out, None)[0]
+
+
+def quantize_t(x, noise=None, out=None):
+    """x transposed, blocked along the rows of x: an MX4 of [cols, rows]."""
+    return _quantize(x, noise, None, True if out is None else out)[1]
+
+
+def quantize_both(x, noise=None):
+    """(quantize(x), quantize_t(x)) in one pass over x."""
+    return _quantize(x, noise, True, True)
+
+
+def dequantize(q, dtype="f32"):
+    """The values q stands for, [rows, cols]."""
+    t = _t()
+    code, dt = _dtype(dtype)
+    out = t.empty((q.rows, q.cols), dtype=dt, device=q.codes.device)
+    _device_guard(out.device)
+    ags_mx_dequantize(q.c, out.data_ptr() or None, code, max(q.cols, 1), _stream(out.device))
+    return out
+
+
+def _workspace(nbytes, device):
+    return _t().empty(nbytes, dtype=_t().uint8, device=device) if nbytes else None
+
+
+def product(a, b, dtype="bf16", out=None, accumulate=False):
+    """a [m, k] times b' [k, n] (MX4s blocked along k): [m, n] of `dtype`, or
+    written to `out` (2-D, unit column stride), added to it with
+    `accumulate`."""
+    t = _t()
+    dev = a.codes.device
+    _device_guard(dev)
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs out")
+        code, dt = _dtype(dtype)
+        out = t.empty((a.rows, b.rows), dtype=dt, device=dev)
+        stride = b.rows
+    else:
+        code = _dtype(out.dtype)[0]
+        if tuple(out.shape) != (a.rows, b.rows):
+            raise ValueError(f"out must be [{a.rows}, {b.rows}]")
+        _, _, _, stride = _matrix(out, "out")
+    nbytes = ags_mx_product_workspace(a.rows, b.rows, a.cols)
+    ws = _workspace(nbytes, dev)
+    ags_mx_product(a.c, b.c, out.data_ptr() or None, code, max(stride, 1), int(accumulate),
+                   None if ws is None else ws.data_ptr(), nbytes, _stream(dev))
+    return out
+
+
+class Weight:
+    """A linear layer's weight w [n, k] in 4 bits, in the two forms its
+    products need: blocked along k (`forward`) and, transposed, along n
+    (`backward`).  :meth:`update` stores new values (after an optimizer
+    step) in the same buffers."""
+
+    def __init__(self, w, forward=True, backward=True):
+        w, n, k, _ = _matrix(w, "w")
+        self.n, self.k = n, k
+        self.rows = MX4(n, k, w.device) if forward else None
+        self.cols = MX4(k, n, w.device) if backward else None
+        if not forward and not backward:
+            raise ValueError("a weight needs a forward or a backward form")
+        self.update(w)
+
+    def update(self, w):
+        w, n, k, _ = _matrix(w, "w")
+        if (n, k) != (self.n, self.k):
+            raise ValueError(f"w must be [{self.n}, {self.k}]")
+        _quantize(w, None, self.rows, self.cols)
+
+
+def linear(x, w, dtype=None, save=False):
+    """y = x w' for x [..., k] and a Weight w [n, k]: [..., n] of `dtype` (x's
+    unless given).  save=True returns (y, saved): what linear_backward takes
+    in place of x, stored in the same pass over it."""
+    t = _t()
+    if w.rows is None:
+        raise ValueError("the weight has no forward form")
+    if x.shape[-1] != w.k:
+        raise ValueError(f"x must have {w.k} columns")
+    x2, rows, _, stride = _matrix(x, "x")
+    _device_guard(x2.device)
+    out_code, out_dt = _dtype(x.dtype if dtype is None else dtype)
+    shape = (*x.shape[:-1], w.n)
+    if save:
+        q, saved = _quantize(x2, None, True, True)
+        return product(q, w.rows, out_dt).view(shape), saved
+    y = t.empty(shape, dtype=out_dt, device=x.device)
+    nbytes = ags_mx_linear_workspace(rows, w.n, w.k)
+    ws = _workspace(nbytes, x.device)
+    ags_mx_linear(x2.data_ptr() or None, _dtype(x.dtype)[0], rows, max(stride, 1), w.rows.c,
+                  y.data_ptr() or None, out_code, max(w.n, 1), None if ws is None else ws.data_ptr(), nbytes,
+                  _stream(x.device))
+    return y
+
+
+def linear_backward(dy, x, w, noise=None, dw=None, dw_dtype="f32", accumulate=False, need_dx=True):
+    """The gradients of y = x w' given dy [..., n]: (dx [..., k] of dy's type,
+    dw [n, k]).  x: the layer's input, or what linear(save=True) returned.
+    noise: random bytes for dy's rounding (uint8, dy's shape).  dw: written
+    there (a view of a replica's row, say), added with `accumulate`; else a
+    new tensor of `dw_dtype`.  need_dx=False returns None for dx."""
+    if dy.shape[-1] != w.n:
+        raise ValueError(f"dy must have {w.n} columns")
+    if need_dx and w.cols is None:
+        raise ValueError("the weight has no backward form")
+    dy2, rows, _, _ = _matrix(dy, "dy")
+    xt = x if isinstance(x, MX4) else quantize_t(x)
+    if xt.shape != (w.k, rows):
+        raise ValueError(f"x and dy differ in rows, or x has not {w.k} columns")
+    q, qt = _quantize(dy2, noise, True if need_dx else None, True)
+    dx = product(q, w.cols, dy.dtype).view(*dy.shape[:-1], w.k) if need_dx else None
+    return dx, product(qt, xt, dw_dtype, dw, accumulate)

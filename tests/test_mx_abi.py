@@ -1,0 +1,146 @@
+"""libags 4-bit operators on the host: the binding's names, sizes and argument
+checks (no GPU; only calls that fail before any HIP call), and the reference
+the GPU tests use."""
+import ctypes
+import os
+import re
+
+import numpy as np
+import pytest
+
+import mx_reference as ref
+from paper_2603_18112_amd import _build, ags, mx
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+X, Y, Z, V, W = (0x1000000000 * (i + 1) for i in range(5))       # never dereferenced
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(_build.LIB):
+        _build.build()
+    return mx._lib()
+
+
+def test_header_declares_the_binding_names():
+    text = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "ags_mx.h")).read(), flags=re.S)
+    assert sorted(set(re.findall(r"\b(ags_[a-z_]+)\s*\(", text))) == sorted(mx.EXPORTS)
+    assert ctypes.sizeof(mx.ags_mx_tensor) == 32
+
+
+@pytest.mark.parametrize("rows,cols,codes,scales", [
+    (0, 0, 0, 0), (3, 0, 0, 0), (0, 5, 0, 0), (1, 1, 128, 8), (1, 256, 128, 8), (2, 257, 512, 32),
+    (4096, 25088, 4096 * 12544, 4096 * 784)])
+def test_bytes(lib, rows, cols, codes, scales):
+    assert mx.ags_mx_bytes(rows, cols) == (codes, scales)
+
+
+@pytest.mark.parametrize("rows,cols,status", [
+    (-1, 5, ags.AGS_E_ARG), (5, -1, ags.AGS_E_ARG), (1, (1 << 24) + 1, ags.AGS_E_LAYOUT),
+    ((1 << 26) + 1, 256, ags.AGS_E_LAYOUT), (1 << 62, 0, ags.AGS_E_LAYOUT), (1 << 62, 1, ags.AGS_E_LAYOUT)])
+def test_size_limits(lib, rows, cols, status):
+    with pytest.raises(ags.AGSError) as e:
+        mx.ags_mx_bytes(rows, cols)
+    assert e.value.status == status and ags.ags_last_error(None)
+
+
+def _raises(status, f, *args, **kw):
+    with pytest.raises(ags.AGSError) as e:
+        f(*args, **kw)
+    assert e.value.status == status, e.value
+
+
+def _t(rows, cols, codes=Y, scales=Z):
+    return mx.ags_mx_tensor(codes, scales, rows, cols)
+
+
+def test_quantize_refuses(lib):
+    q, bf = mx.ags_mx_quantize, ags.AGS_BF16
+    _raises(ags.AGS_E_ARG, q, X, 2, 4, 64, 64, None, 0, _t(4, 64), None)           # type
+    _raises(ags.AGS_E_ARG, q, X, bf, 4, 64, 64, None, 0, None, None)               # no output
+    _raises(ags.AGS_E_ARG, q, None, bf, 4, 64, 64, None, 0, _t(4, 64), None)
+    _raises(ags.AGS_E_ALIGN, q, X + 1, bf, 4, 64, 64, None, 0, _t(4, 64), None)
+    _raises(ags.AGS_E_ARG, q, X, bf, 4, 64, 63, None, 0, _t(4, 64), None)          # stride
+    _raises(ags.AGS_E_ARG, q, X, bf, 4, 64, 64, V, 63, _t(4, 64), None)            # noise stride
+    _raises(ags.AGS_E_ARG, q, X, bf, 4, 64, 64, None, 0, _t(4, 65), None)          # sizes differ
+    _raises(ags.AGS_E_ARG, q, X, bf, 4, 64, 64, None, 0, None, _t(4, 64))
+    _raises(ags.AGS_E_ALIGN, q, X, bf, 4, 64, 64, None, 0, _t(4, 64, Y + 8), None)
+    _raises(ags.AGS_E_ARG, q, X, bf, 4, 64, 64, None, 0, _t(4, 64, None), None)
+    _raises(ags.AGS_E_ARG, q, X, bf, 4, 64, 64, None, 0, _t(4, 64, X + 64), None)  # out over x
+    _raises(ags.AGS_E_ARG, q, X, bf, 4, 64, 64, None, 0, _t(4, 64, Y, Y), None)    # scales over codes
+    _raises(ags.AGS_E_ARG, q, X, bf, -1, 64, 64, None, 0, _t(-1, 64), None)
+    _raises(ags.AGS_E_LAYOUT, q, X, bf, 4, 1 << 25, 1 << 25, None, 0, _t(4, 1 << 25), None)
+    # the rows of a transposed form are padded too
+    _raises(ags.AGS_E_LAYOUT, q, X, bf, (1 << 24) + 1, 4, 4, None, 0, None, _t(4, (1 << 24) + 1))
+    q(X, bf, 0, 64, 64, None, 0, _t(0, 64), None)                                   # nothing to do
+
+
+def test_dequantize_refuses(lib):
+    d = mx.ags_mx_dequantize
+    _raises(ags.AGS_E_ARG, d, _t(4, 64), None, ags.AGS_F32, 64)
+    _raises(ags.AGS_E_ARG, d, _t(4, 64), X, 7, 64)
+    _raises(ags.AGS_E_ARG, d, _t(4, 64), X, ags.AGS_F32, 63)
+    _raises(ags.AGS_E_ALIGN, d, _t(4, 64), X + 2, ags.AGS_F32, 64)
+    _raises(ags.AGS_E_ARG, d, _t(4, 64), Y, ags.AGS_F32, 64)
+    assert lib.ags_mx_dequantize(None, X, 0, 64, None) == ags.AGS_E_ARG
+
+
+def test_product_and_linear_refuse(lib):
+    p, bf = mx.ags_mx_product, ags.AGS_BF16
+    a, b = _t(4, 64, Y, Z), _t(8, 64, V, W)
+    _raises(ags.AGS_E_ARG, p, a, _t(8, 65, V, W), X, bf, 8)
+    _raises(ags.AGS_E_ARG, p, a, b, X, 3, 8)
+    _raises(ags.AGS_E_ARG, p, a, b, X, bf, 7)
+    _raises(ags.AGS_E_ARG, p, a, b, None, bf, 8)
+    _raises(ags.AGS_E_ARG, p, a, b, X, bf, 8, accumulate=2)
+    _raises(ags.AGS_E_ARG, p, a, b, Y, bf, 8)                                       # out over a
+    _raises(ags.AGS_E_ALIGN, p, a, b, X + 1, bf, 8)
+    _raises(ags.AGS_E_LAYOUT, p, _t(1 << 20, 64, Y, Z), _t(1 << 20, 64, V, W), X, bf, 1 << 20)
+    lin = mx.ags_mx_linear
+    need = mx.ags_mx_linear_workspace(4, 8, 64)
+    assert need > 0
+    _raises(ags.AGS_E_ARG, lin, X, bf, 4, 64, b, Y, bf, 8, None, 0)                 # no workspace
+    _raises(ags.AGS_E_ARG, lin, X, bf, 4, 64, b, Y, bf, 8, Z, need - 1)
+    _raises(ags.AGS_E_ALIGN, lin, X, bf, 4, 64, b, Y, bf, 8, Z + 8, need)
+    _raises(ags.AGS_E_ARG, lin, X, bf, 4, 63, b, Y, bf, 8, Z, need)
+    _raises(ags.AGS_E_ARG, lin, X, bf, 4, 64, b, X, bf, 8, Z, need)
+    _raises(ags.AGS_E_ARG, lin, X, bf, 4, 64, b, Y, 5, 8, Z, need)
+    _raises(ags.AGS_E_ARG, mx.ags_mx_product_workspace, -1, 2, 3)
+    _raises(ags.AGS_E_LAYOUT, mx.ags_mx_linear_workspace, 1 << 20, 1 << 20, 64)
+    lin(X, bf, 0, 64, b, Y, bf, 8)                                                  # nothing to do
+
+
+def test_reference_nearest_by_hand():
+    x = np.zeros((1, 64))
+    x[0, :8] = [4.0, 0.25, -0.75, 1.25, 1.75, -2.5, 3.5, 5.0]       # every tie, scale 1
+    x[0, 32:38] = [7.99, -6.5, 0.2501, 0.2499, 5.0001, 0.7499]
+    v, e = ref.store_rows(x)
+    assert e.tolist() == [[0, 0]]
+    assert v[0, :8].tolist() == [4.0, 0.0, -1.0, 1.0, 2.0, -2.0, 4.0, 4.0]
+    assert v[0, 32:38].tolist() == [6.0, -6.0, 0.5, 0.0, 6.0, 0.5]
+
+
+def test_reference_stochastic_by_hand():
+    x = np.zeros((1, 32))
+    x[0, :5] = [6.5, 3.5, 1.0, 0.125, 0.25]                          # scale 2: 3.25 1.75 0.5 0.0625 0.125
+    r = np.zeros((1, 32))
+    r[0, :5] = [191, 128, 0, 223, 191]
+    v, e = ref.store_rows(x, r)
+    assert e[0, 0] == 1
+    # fractions .25, .5, 0, .125, .25 with (r + 1/2) / 256 = .748, .502, .002, .873, .748
+    assert v[0, :5].tolist() == [6.0, 4.0, 1.0, 0.0, 0.0]
+    r[0, :5] = [192, 127, 255, 224, 192]
+    v, _ = ref.store_rows(x, r)
+    assert v[0, :5].tolist() == [8.0, 3.0, 1.0, 1.0, 1.0]
+
+
+def test_reference_stochastic_is_unbiased():
+    """The mean over all 256 bytes is within half a byte's step."""
+    rng = np.random.default_rng(0)
+    x = rng.standard_normal((1, 32))
+    mean = np.zeros((1, 32))
+    for r in range(256):
+        v, e = ref.store_rows(x, np.full((1, 32), r))
+        mean += v / 256
+    step = np.where(np.abs(x) < 2 * 2.0 ** e[0, 0], 0.5, np.where(np.abs(x) < 4 * 2.0 ** e[0, 0], 1.0, 2.0))
+    assert np.all(np.abs(mean - x) <= step * 2.0 ** e[0, 0] / 512 + 1e-12)
