@@ -5,6 +5,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "ags_mx.h"
 
 namespace ags {
@@ -34,7 +36,24 @@ struct MxProductArgs {
     int64_t stride;
     int64_t m, n, kp;
     int32_t bf16, accumulate;
+    float* partials;  // [splits][m][n] sums over parts of the contracted axis, where splits > 1
+    int32_t splits;
 };
+
+// How a product is cut into blocks: tiles of 64 * tm x 64 * tn outputs, the
+// contracted axis into `splits` parts.
+struct MxShape {
+    int32_t tm, tn, splits;
+};
+inline MxShape mx_product_plan(int64_t m, int64_t n, int64_t kp) {
+    MxShape p{1, 1, 1};
+    auto tiles = [&](int64_t tm, int64_t tn) { return ((m + 64 * tm - 1) / (64 * tm)) * ((n + 64 * tn - 1) / (64 * tn)); };
+    if (tiles(4, 4) >= 192) p.tm = p.tn = 4;
+    else if (tiles(2, 2) >= 192) p.tm = p.tn = 2;
+    const int64_t t = tiles(p.tm, p.tn), stages = kp / 256;
+    if (t < 256) p.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(512 / t, stages / 4));
+    return p;
+}
 
 // Weak for the same reason as the clipping launchers.
 __attribute__((weak)) hipError_t launch_mx_quantize(const MxQuantArgs&, hipStream_t);

@@ -1,15 +1,25 @@
 // gfx950 kernels of the products of 4-bit operands (include/ags_mx.h).
 //
-// mx_product_kernel  one wave per 16 x 16 tile of the output, operands read
-//                    straight from memory.
+// mx_tile_kernel    a block of four waves takes a tile of the output; stages of
+//                   256 elements of the contracted axis go from memory straight
+//                   into LDS while the matrix cores work on the stage before.
+// mx_join_kernel    adds the partial sums of a contracted axis cut in parts.
+#include <algorithm>
+
 #include "ags_mx_device.h"
 #include "ags_mx_internal.h"
+
+#ifndef __gfx950__
+#ifdef __HIP_DEVICE_COMPILE__
+#error "gfx950 only: scaled matrix instructions and 16-byte loads into LDS"
+#endif
+#endif
 
 namespace ags {
 namespace {
 
 typedef int v8i __attribute__((ext_vector_type(8)));
-typedef float v4f __attribute__((ext_vector_type(4)));
+typedef float v16f __attribute__((ext_vector_type(16)));
 
 constexpr int kFp4 = 4;  // operand format of the scaled matrix instruction
 
@@ -23,45 +33,293 @@ __device__ __forceinline__ unsigned short bf16_round(float x) {
     return (unsigned short)((u + 0x7fffu + ((u >> 16) & 1u)) >> 16);
 }
 
-__device__ __forceinline__ void store_elem(const MxProductArgs& a, int64_t i, int64_t j, float v) {
-    const int64_t at = i * a.stride + j;
-    if (a.bf16) {
-        unsigned short* p = static_cast<unsigned short*>(a.out) + at;
-        if (a.accumulate) v += __uint_as_float((unsigned)*p << 16);
-        *p = bf16_round(v);
+// Where results go: the output, or one part's sums.
+struct Out {
+    char* p;
+    int64_t stride;
+    bool bf16, add, wide;  // wide: four elements are one aligned store
+};
+
+__device__ __forceinline__ Out output_of(const MxProductArgs& a, unsigned split) {
+    Out o{static_cast<char*>(a.out), a.stride, a.bf16 != 0, a.accumulate != 0, false};
+    if (a.splits > 1) o = Out{reinterpret_cast<char*>(a.partials + (int64_t)split * a.m * a.n), a.n, false, false, false};
+    const unsigned low = (unsigned)reinterpret_cast<uintptr_t>(o.p) | ((unsigned)o.stride * (o.bf16 ? 2u : 4u));
+    o.wide = (low & (o.bf16 ? 7u : 15u)) == 0;
+    return o;
+}
+
+__device__ __forceinline__ void store1(const Out& o, int64_t at, float v) {
+    if (o.bf16) {
+        unsigned short* p = reinterpret_cast<unsigned short*>(o.p) + at;
+        *p = bf16_round(o.add ? v + __uint_as_float((unsigned)*p << 16) : v);
     } else {
-        float* p = static_cast<float*>(a.out) + at;
-        if (a.accumulate) v += *p;
-        *p = v;
+        float* p = reinterpret_cast<float*>(o.p) + at;
+        *p = o.add ? v + *p : v;
     }
 }
 
-__global__ __launch_bounds__(64) void mx_product_kernel(MxProductArgs a, unsigned tiles_n) {
-    const int lane = threadIdx.x, r = lane & 15, q = lane >> 4;
-    const int64_t i0 = (int64_t)(blockIdx.x / tiles_n) * 16, j0 = (int64_t)(blockIdx.x % tiles_n) * 16;
-    // rows past the end repeat the last one; their results are not stored
-    const int64_t ia = min(i0 + r, a.m - 1), jb = min(j0 + r, a.n - 1);
-    const uint8_t* pa = a.a + ia * (a.kp / 2) + q * 16;
-    const uint8_t* pb = a.b + jb * (a.kp / 2) + q * 16;
-    const uint8_t* psa = a.sa + ia * (a.kp / 32) + q;
-    const uint8_t* psb = a.sb + jb * (a.kp / 32) + q;
-    v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int64_t k = 0; k < a.kp; k += 128) {
-        const uint4 x = *reinterpret_cast<const uint4*>(pa + k / 2), y = *reinterpret_cast<const uint4*>(pb + k / 2);
-        const int sx = psa[k / 32], sy = psb[k / 32];
-        acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(x), operand(y), acc, kFp4, kFp4, 0, sx, 0, sy);
+// Four results of a row from column j, as many as lie before column n.
+__device__ __forceinline__ void store4(const Out& o, int64_t i, int64_t j, float4 v, int64_t n) {
+    const int64_t at = i * o.stride + j;
+    if (o.wide && j + 4 <= n) {
+        if (o.bf16) {
+            uint2* p = reinterpret_cast<uint2*>(o.p + at * 2);
+            if (o.add) {
+                const uint2 u = *p;
+                v.x += __uint_as_float(u.x << 16), v.y += __uint_as_float(u.x & 0xffff0000u);
+                v.z += __uint_as_float(u.y << 16), v.w += __uint_as_float(u.y & 0xffff0000u);
+            }
+            *p = make_uint2(bf16_round(v.x) | ((unsigned)bf16_round(v.y) << 16),
+                            bf16_round(v.z) | ((unsigned)bf16_round(v.w) << 16));
+        } else {
+            float4* p = reinterpret_cast<float4*>(o.p + at * 4);
+            if (o.add) {
+                const float4 u = *p;
+                v.x += u.x, v.y += u.y, v.z += u.z, v.w += u.w;
+            }
+            *p = v;
+        }
+        return;
     }
+    const float e[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (i0 + q * 4 + i < a.m && j0 + r < a.n) store_elem(a, i0 + q * 4 + i, j0 + r, acc[i]);
+    for (int t = 0; t < 4; ++t)
+        if (j + t < n) store1(o, at + t, e[t]);
+}
+
+// ------------------------------------------------------------ tile kernel --
+
+constexpr int kXcds = 8;
+
+// Consecutive blocks go to the 8 XCDs in turn.  Each XCD takes a run of
+// consecutive tiles, and tiles are numbered in bands of kBand rows, so the
+// blocks that share an XCD's L2 read few rows and few columns.
+constexpr unsigned kBand = 8;
+
+__device__ __forceinline__ void tile_of_block(unsigned block, unsigned tm, unsigned tn, unsigned& i, unsigned& j) {
+    const unsigned total = tm * tn, xcd = block % kXcds, at = block / kXcds;
+    const unsigned base = total / kXcds, rest = total % kXcds;
+    const unsigned t = xcd * base + min(xcd, rest) + at;
+    const unsigned band = t / (kBand * tn), first = band * kBand, h = min(kBand, tm - first);
+    const unsigned in = t - band * kBand * tn;
+    i = first + in % h;
+    j = in / h;
+}
+
+typedef __attribute__((address_space(3))) void* lds_ptr;
+
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void block_barrier() {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// TM x TN: the tile in units of 64; four waves, two by two.
+template <int TM, int TN>
+__device__ __forceinline__ void tile_product(const MxProductArgs& a, unsigned tiles_m, unsigned tiles_n) {
+    constexpr int BM = 64 * TM, BN = 64 * TN;
+    constexpr int kStage = (BM + BN) * 128, kBuf = kStage + (BM + BN) * 8;
+    extern __shared__ char sm[];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const unsigned tiles = tiles_m * tiles_n;
+    const unsigned split = blockIdx.x / tiles;
+    unsigned ti, tj;
+    tile_of_block(blockIdx.x % tiles, tiles_m, tiles_n, ti, tj);
+    const int64_t i0 = (int64_t)ti * BM, j0 = (int64_t)tj * BN;
+    const unsigned pitch = (unsigned)(a.kp / 2), spitch = (unsigned)(a.kp / 32);
+    const int stages = (int)(a.kp / 256);
+    const int s0 = (int)((int64_t)stages * split / a.splits), s1 = (int)((int64_t)stages * (split + 1) / a.splits);
+    const int ma = (int)min((int64_t)BM, a.m - i0), nb = (int)min((int64_t)BN, a.n - j0);
+
+    const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<uint8_t*>(a.a + i0 * pitch), 0, (unsigned)ma * pitch, 0x00027000);
+    const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<uint8_t*>(a.b + j0 * pitch), 0, (unsigned)nb * pitch, 0x00027000);
+    const __amdgpu_buffer_rsrc_t rsa = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<uint8_t*>(a.sa + i0 * spitch), 0, (unsigned)ma * spitch, 0x00027000);
+    const __amdgpu_buffer_rsrc_t rsb = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<uint8_t*>(a.sb + j0 * spitch), 0, (unsigned)nb * spitch, 0x00027000);
+
+    // A wave's load takes 8 rows of 128 bytes.  LDS keeps rows of 128 bytes
+    // whose 16-byte pieces are permuted by the row's low three bits, so that
+    // the operand reads of 8 neighbouring lanes fall on 8 different places.
+    // Rows past the end repeat the last one; their results are not stored.
+    unsigned va[BM / 32], vb[BN / 32], vs[(BM + BN) / 128];
+    const unsigned piece = (unsigned)((lane & 7) ^ (lane >> 3)) * 16;
+#pragma unroll
+    for (int i = 0; i < BM / 32; ++i) va[i] = (unsigned)min((i * 4 + w) * 8 + (lane >> 3), ma - 1) * pitch + piece;
+#pragma unroll
+    for (int i = 0; i < BN / 32; ++i) vb[i] = (unsigned)min((i * 4 + w) * 8 + (lane >> 3), nb - 1) * pitch + piece;
+#pragma unroll
+    for (int i = 0; i < (BM + BN) / 128; ++i) {
+        const int d = (i * 4 + w) * 64 + lane;  // dword of the scales, A's then B's
+        const bool is_a = (i * 4 + w) * 64 < BM * 2;
+        const int row = is_a ? min(d / 2, ma - 1) : min(d / 2 - BM, nb - 1);
+        vs[i] = (unsigned)row * spitch + (d & 1) * 4;
+    }
+    auto load_stage = [&](int s, int buf) {
+        char* p = sm + buf * kBuf;
+#pragma unroll
+        for (int i = 0; i < BM / 32; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_ptr)(p + (i * 4 + w) * 1024), 16, va[i], s * 128, 0, 0);
+#pragma unroll
+        for (int i = 0; i < BN / 32; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_ptr)(p + BM * 128 + (i * 4 + w) * 1024), 16, vb[i],
+                                                     s * 128, 0, 0);
+#pragma unroll
+        for (int i = 0; i < (BM + BN) / 128; ++i) {
+            const bool is_a = (i * 4 + w) * 64 < BM * 2;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(is_a ? rsa : rsb, (lds_ptr)(p + kStage + (i * 4 + w) * 256), 4,
+                                                     vs[i], s * 8, 0, 0);
+        }
+    };
+
+    // Operands: lane l holds row l % 32; its half h = l / 32 takes the pieces
+    // 4 h + j of a stage in step j (the order of the contracted elements is
+    // free as long as both operands agree), so that the four scales of a
+    // stage are one dword.
+    constexpr int FM = TM, FN = TN;  // 32 x 32 fragments of a wave
+    const int r = lane & 31, h = lane >> 5, wm = w >> 1, wn = w & 1;
+    int off[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) off[j] = r * 128 + (((h * 4 + j) ^ (r & 7)) << 4);
+    const int oa = wm * (BM / 2) * 128, ob = BM * 128 + wn * (BN / 2) * 128;
+    const int osa = kStage + (wm * (BM / 2) + r) * 8 + h * 4, osb = kStage + (BM + wn * (BN / 2) + r) * 8 + h * 4;
+    uint4 fa[2][FM], fb[2][FN];
+    int ea[2][FM], eb[2][FN];
+    auto read_step = [&](int buf, int j, int to) {
+        const char* p = sm + buf * kBuf;
+#pragma unroll
+        for (int f = 0; f < FM; ++f) fa[to][f] = *reinterpret_cast<const uint4*>(p + oa + f * 4096 + off[j]);
+#pragma unroll
+        for (int f = 0; f < FN; ++f) fb[to][f] = *reinterpret_cast<const uint4*>(p + ob + f * 4096 + off[j]);
+    };
+    auto read_scales = [&](int buf, int to) {
+        const char* p = sm + buf * kBuf;
+#pragma unroll
+        for (int f = 0; f < FM; ++f) ea[to][f] = *reinterpret_cast<const int*>(p + osa + f * 256);
+#pragma unroll
+        for (int f = 0; f < FN; ++f) eb[to][f] = *reinterpret_cast<const int*>(p + osb + f * 256);
+    };
+
+    v16f acc[FM][FN];
+#pragma unroll
+    for (int x = 0; x < FM; ++x)
+#pragma unroll
+        for (int y = 0; y < FN; ++y)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[x][y][i] = 0.0f;
+
+#define MX_STEP(J, FROM, SCALES)                                                                              \
+    _Pragma("unroll") for (int x = 0; x < FM; ++x) _Pragma("unroll") for (int y = 0; y < FN; ++y)             \
+        acc[x][y] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(fa[FROM][x]), operand(fb[FROM][y]), \
+                                                                    acc[x][y], kFp4, kFp4, J, ea[SCALES][x], J, \
+                                                                    eb[SCALES][y]);
+
+    // One stage; its first step's operands are in registers.  In its last
+    // step the next stage has arrived and the block's reads of this one are
+    // done, so one barrier serves both buffers.
+    auto stage = [&](int s, int cur) {
+        read_step(cur, 1, 1);
+        MX_STEP(0, 0, 0)
+        read_step(cur, 2, 0);
+        MX_STEP(1, 1, 0)
+        read_step(cur, 3, 1);
+        MX_STEP(2, 0, 0)
+        if (s + 1 < s1) {
+            wait_loads();
+            block_barrier();
+            read_step(cur ^ 1, 0, 0);
+            read_scales(cur ^ 1, 1);
+            if (s + 2 < s1) load_stage(s + 2, cur);
+        }
+        MX_STEP(3, 1, 0)
+#pragma unroll
+        for (int f = 0; f < FM; ++f) ea[0][f] = ea[1][f];
+#pragma unroll
+        for (int f = 0; f < FN; ++f) eb[0][f] = eb[1][f];
+    };
+
+    if (s0 < s1) {
+        load_stage(s0, 0);
+        wait_loads();
+        if (s0 + 1 < s1) load_stage(s0 + 1, 1);
+        block_barrier();
+        read_step(0, 0, 0);
+        read_scales(0, 0);
+        for (int s = s0; s < s1; ++s) stage(s, (s - s0) & 1);
+    }
+#undef MX_STEP
+
+    // A strip of 32 rows at a time goes through the wave's own part of LDS, so
+    // that the stores are of whole rows.  Fragment element i of lane l: row
+    // 8 (i / 4) + 4 h + i % 4, column l % 32.
+    block_barrier();
+    constexpr int kWide = BN / 2, kRow = kWide + 4;
+    float* strip = reinterpret_cast<float*>(sm) + w * 32 * kRow;
+    const Out o = output_of(a, split);
+#pragma unroll
+    for (int x = 0; x < FM; ++x) {
+#pragma unroll
+        for (int y = 0; y < FN; ++y)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) strip[((i / 4) * 8 + h * 4 + i % 4) * kRow + y * 32 + r] = acc[x][y][i];
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        constexpr int kLanes = kWide / 4, kRows = 64 / kLanes;  // lanes of a row, rows of a store
+        const int c = (lane % kLanes) * 4;
+        const int64_t col = j0 + wn * kWide + c;
+        for (int t = lane / kLanes; t < 32; t += kRows) {
+            const int64_t row = i0 + wm * (BM / 2) + x * 32 + t;
+            const float4 v = *reinterpret_cast<const float4*>(strip + t * kRow + c);
+            if (row < a.m && col < a.n) store4(o, row, col, v, a.n);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+}
+
+template <int TM, int TN>
+__global__ __launch_bounds__(256, 1) void mx_tile_kernel(MxProductArgs a, unsigned tiles_m, unsigned tiles_n) {
+    tile_product<TM, TN>(a, tiles_m, tiles_n);
+}
+
+__global__ __launch_bounds__(256) void mx_join_kernel(MxProductArgs a) {
+    const int64_t total = a.m * a.n;
+    const Out o{static_cast<char*>(a.out), a.stride, a.bf16 != 0, a.accumulate != 0, false};
+    for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < total; t += (int64_t)gridDim.x * 256) {
+        float v = 0.0f;
+        for (int s = 0; s < a.splits; ++s) v += a.partials[s * total + t];
+        store1(o, t / a.n * a.stride + t % a.n, v);
+    }
+}
+
+template <int TM, int TN>
+hipError_t launch_tile(const MxProductArgs& a, hipStream_t s) {
+    constexpr int lds = 2 * (64 * TM + 64 * TN) * 136;
+    const unsigned tm = (unsigned)((a.m + 64 * TM - 1) / (64 * TM)), tn = (unsigned)((a.n + 64 * TN - 1) / (64 * TN));
+    if (lds > 65536) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(mx_tile_kernel<TM, TN>),
+                                                 hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL((mx_tile_kernel<TM, TN>), dim3(tm * tn * (unsigned)a.splits), dim3(256), lds, s, a, tm, tn);
+    return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_mx_product(const MxProductArgs& a, hipStream_t s) {
-    const unsigned tiles_n = (unsigned)((a.n + 15) / 16), tiles_m = (unsigned)((a.m + 15) / 16);
-    hipLaunchKernelGGL(mx_product_kernel, dim3(tiles_n * tiles_m), dim3(64), 0, s, a, tiles_n);
-    return hipGetLastError();
+hipError_t launch_mx_product(const MxProductArgs& args, hipStream_t s) {
+    MxProductArgs a = args;
+    const MxShape p = mx_product_plan(a.m, a.n, a.kp);
+    a.splits = p.splits;
+    hipError_t e = p.tm == 4 ? launch_tile<4, 4>(a, s) : p.tm == 2 ? launch_tile<2, 2>(a, s) : launch_tile<1, 1>(a, s);
+    if (e == hipSuccess && a.splits > 1) {
+        const unsigned blocks = (unsigned)std::min<int64_t>((a.m * a.n + 255) / 256, 4096);
+        hipLaunchKernelGGL(mx_join_kernel, dim3(blocks), dim3(256), 0, s, a);
+        e = hipGetLastError();
+    }
+    return e;
 }
 
 }  // namespace ags

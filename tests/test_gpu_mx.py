@@ -194,7 +194,8 @@ def whole(rows, cols, seed, dtype="f32", pad=0):
 PRODUCTS = [(1, 1, 1), (1, 17, 32), (1, 4096, 640), (2, 100, 257), (7, 33, 96), (13, 1000, 512), (16, 16, 128),
             (17, 65, 1000), (24, 250, 4096), (31, 129, 256), (33, 64, 8192), (63, 65, 300), (64, 512, 2048),
             (100, 96, 800), (128, 128, 128), (129, 257, 511), (250, 1000, 96), (255, 300, 260), (256, 256, 256),
-            (257, 511, 1024), (300, 77, 2050), (1000, 40, 64), (520, 1030, 320), (5, 2100, 1300)]
+            (257, 511, 1024), (300, 77, 2050), (1000, 40, 64), (520, 1030, 320), (5, 2100, 1300),
+            (1801, 1811, 520), (3601, 3587, 300), (3600, 3840, 260)]
 
 
 @pytest.mark.parametrize("m,n,k", PRODUCTS)
