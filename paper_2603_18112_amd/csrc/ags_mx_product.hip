@@ -5,6 +5,7 @@
 //                   into LDS while the matrix cores work on the stage before.
 // mx_join_kernel    adds the partial sums of a contracted axis cut in parts.
 #include <algorithm>
+#include <type_traits>
 
 #include "ags_mx_device.h"
 #include "ags_mx_internal.h"
@@ -27,11 +28,17 @@ __device__ __forceinline__ v8i operand(uint4 v) {
     return v8i{(int)v.x, (int)v.y, (int)v.z, (int)v.w, 0, 0, 0, 0};
 }
 
-__device__ __forceinline__ unsigned short bf16_round(float x) {
-    const unsigned u = __float_as_uint(x);
-    if ((u & 0x7fffffffu) > 0x7f800000u) return (unsigned short)((u >> 16) | 0x40u);
-    return (unsigned short)((u + 0x7fffu + ((u >> 16) & 1u)) >> 16);
+typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+typedef float v2f __attribute__((ext_vector_type(2)));
+
+// To nearest even, by the hardware's converter.
+__device__ __forceinline__ unsigned pack_bf16(float x, float y) {
+    const v2bf v = __builtin_convertvector((v2f{x, y}), v2bf);
+    unsigned u;
+    __builtin_memcpy(&u, &v, 4);
+    return u;
 }
+__device__ __forceinline__ unsigned short bf16_round(float x) { return (unsigned short)pack_bf16(x, 0.0f); }
 
 // Where results go: the output, or one part's sums.
 struct Out {
@@ -69,8 +76,7 @@ __device__ __forceinline__ void store4(const Out& o, int64_t i, int64_t j, float
                 v.x += __uint_as_float(u.x << 16), v.y += __uint_as_float(u.x & 0xffff0000u);
                 v.z += __uint_as_float(u.y << 16), v.w += __uint_as_float(u.y & 0xffff0000u);
             }
-            *p = make_uint2(bf16_round(v.x) | ((unsigned)bf16_round(v.y) << 16),
-                            bf16_round(v.z) | ((unsigned)bf16_round(v.w) << 16));
+            *p = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
         } else {
             float4* p = reinterpret_cast<float4*>(o.p + at * 4);
             if (o.add) {
@@ -106,7 +112,20 @@ __device__ __forceinline__ void tile_of_block(unsigned block, unsigned tm, unsig
     j = in / h;
 }
 
-typedef __attribute__((address_space(3))) void* lds_ptr;
+// Loads from memory straight into LDS: 64 lanes of 16 (or 4) bytes, lane after
+// lane from LDS byte `to`.  Written out because the compiler would wait for
+// all of them before the next LDS read; wait_loads() does so once a stage.
+// (m0 is reserved: the compiler sets it anew where it needs it itself.)
+__device__ __forceinline__ void load_lds16(__amdgpu_buffer_rsrc_t r, unsigned to, unsigned lane_off, unsigned off) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(lane_off),
+                 "s"(r), "s"(off)
+                 : "memory");
+}
+__device__ __forceinline__ void load_lds4(__amdgpu_buffer_rsrc_t r, unsigned to, unsigned lane_off, unsigned off) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(to), "v"(lane_off),
+                 "s"(r), "s"(off)
+                 : "memory");
+}
 
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ void block_barrier() {
@@ -116,6 +135,45 @@ __device__ __forceinline__ void block_barrier() {
 }
 
 // TM x TN: the tile in units of 64; four waves, two by two.
+// 32 rows of WIDE results from LDS (rows of WIDE + 4 floats) to the output, all
+// of them inside it.
+template <int WIDE>
+__device__ __forceinline__ void store_strip(const Out& o, const float* strip, int lane, int64_t row0, int64_t col0) {
+    if (o.bf16) {
+        constexpr int kLanes = WIDE / 8, kRows = 64 / kLanes;  // lanes of a row, rows of a store
+        const int c = (lane % kLanes) * 8, t0 = lane / kLanes;
+        char* p = o.p + ((row0 + t0) * o.stride + col0 + c) * 2;
+#pragma unroll
+        for (int t = 0; t < 32; t += kRows) {
+            const float4* v = reinterpret_cast<const float4*>(strip + (t0 + t) * (WIDE + 4) + c);
+            const float4 u = v[0], w = v[1];
+            *reinterpret_cast<uint4*>(p + t * o.stride * 2) =
+                make_uint4(pack_bf16(u.x, u.y), pack_bf16(u.z, u.w), pack_bf16(w.x, w.y), pack_bf16(w.z, w.w));
+        }
+    } else {
+        constexpr int kLanes = WIDE / 4, kRows = 64 / kLanes;
+        const int c = (lane % kLanes) * 4, t0 = lane / kLanes;
+        char* p = o.p + ((row0 + t0) * o.stride + col0 + c) * 4;
+#pragma unroll
+        for (int t = 0; t < 32; t += kRows)
+            *reinterpret_cast<float4*>(p + t * o.stride * 4) =
+                *reinterpret_cast<const float4*>(strip + (t0 + t) * (WIDE + 4) + c);
+    }
+}
+
+// The same where rows or columns end inside, or results are added.
+template <int WIDE>
+__device__ __forceinline__ void store_edge(const Out& o, const float* strip, int lane, int64_t row0, int64_t col0,
+                                           int64_t m, int64_t n) {
+    constexpr int kLanes = WIDE / 4, kRows = 64 / kLanes;
+    const int c = (lane % kLanes) * 4;
+#pragma unroll 1
+    for (int t = lane / kLanes; t < 32; t += kRows) {
+        const float4 v = *reinterpret_cast<const float4*>(strip + t * (WIDE + 4) + c);
+        if (row0 + t < m && col0 + c < n) store4(o, row0 + t, col0 + c, v, n);
+    }
+}
+
 template <int TM, int TN>
 __device__ __forceinline__ void tile_product(const MxProductArgs& a, unsigned tiles_m, unsigned tiles_n) {
     constexpr int BM = 64 * TM, BN = 64 * TN;
@@ -159,21 +217,24 @@ __device__ __forceinline__ void tile_product(const MxProductArgs& a, unsigned ti
         const int row = is_a ? min(d / 2, ma - 1) : min(d / 2 - BM, nb - 1);
         vs[i] = (unsigned)row * spitch + (d & 1) * 4;
     }
-    auto load_stage = [&](int s, int buf) {
-        char* p = sm + buf * kBuf;
-#pragma unroll
-        for (int i = 0; i < BM / 32; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_ptr)(p + (i * 4 + w) * 1024), 16, va[i], s * 128, 0, 0);
-#pragma unroll
-        for (int i = 0; i < BN / 32; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_ptr)(p + BM * 128 + (i * 4 + w) * 1024), 16, vb[i],
-                                                     s * 128, 0, 0);
-#pragma unroll
-        for (int i = 0; i < (BM + BN) / 128; ++i) {
-            const bool is_a = (i * 4 + w) * 64 < BM * 2;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(is_a ? rsa : rsb, (lds_ptr)(p + kStage + (i * 4 + w) * 256), 4,
-                                                     vs[i], s * 8, 0, 0);
+    const unsigned lds0 = (unsigned)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)sm);
+    constexpr int kLoads = BM / 32 + BN / 32 + (BM + BN) / 128;
+    auto load_one = [&](int i, int s, int buf) {  // load i of a stage
+        const unsigned p = lds0 + buf * kBuf;
+        if (i < BM / 32) {
+            load_lds16(ra, p + (i * 4 + w) * 1024, va[i], s * 128);
+        } else if (i < BM / 32 + BN / 32) {
+            const int t = i - BM / 32;
+            load_lds16(rb, p + BM * 128 + (t * 4 + w) * 1024, vb[t], s * 128);
+        } else {
+            const int t = i - BM / 32 - BN / 32;
+            const bool is_a = (t * 4 + w) * 64 < BM * 2;
+            load_lds4(is_a ? rsa : rsb, p + kStage + (t * 4 + w) * 256, vs[t], s * 8);
         }
+    };
+    auto load_stage = [&](int s, int buf) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) load_one(i, s, buf);
     };
 
     // Operands: lane l holds row l % 32; its half h = l / 32 takes the pieces
@@ -189,12 +250,20 @@ __device__ __forceinline__ void tile_product(const MxProductArgs& a, unsigned ti
     const int osa = kStage + (wm * (BM / 2) + r) * 8 + h * 4, osb = kStage + (BM + wn * (BN / 2) + r) * 8 + h * 4;
     uint4 fa[2][FM], fb[2][FN];
     int ea[2][FM], eb[2][FN];
-    auto read_step = [&](int buf, int j, int to) {
+    // Read i of a step's operands, in the order they are needed: A's first
+    // fragment, all of B's, the rest of A's.
+    auto read_one = [&](int i, int buf, int j, int to) {
         const char* p = sm + buf * kBuf;
+        if (i >= 1 && i <= FN) {
+            fb[to][i - 1] = *reinterpret_cast<const uint4*>(p + ob + (i - 1) * 4096 + off[j]);
+        } else {
+            const int f = i ? i - FN : 0;
+            fa[to][f] = *reinterpret_cast<const uint4*>(p + oa + f * 4096 + off[j]);
+        }
+    };
+    auto read_step = [&](int buf, int j, int to) {
 #pragma unroll
-        for (int f = 0; f < FM; ++f) fa[to][f] = *reinterpret_cast<const uint4*>(p + oa + f * 4096 + off[j]);
-#pragma unroll
-        for (int f = 0; f < FN; ++f) fb[to][f] = *reinterpret_cast<const uint4*>(p + ob + f * 4096 + off[j]);
+        for (int i = 0; i < FM + FN; ++i) read_one(i, buf, j, to);
     };
     auto read_scales = [&](int buf, int to) {
         const char* p = sm + buf * kBuf;
@@ -212,30 +281,50 @@ __device__ __forceinline__ void tile_product(const MxProductArgs& a, unsigned ti
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[x][y][i] = 0.0f;
 
-#define MX_STEP(J, FROM, SCALES)                                                                              \
-    _Pragma("unroll") for (int x = 0; x < FM; ++x) _Pragma("unroll") for (int y = 0; y < FN; ++y)             \
-        acc[x][y] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(fa[FROM][x]), operand(fb[FROM][y]), \
-                                                                    acc[x][y], kFp4, kFp4, J, ea[SCALES][x], J, \
-                                                                    eb[SCALES][y]);
+#define MX_MULTIPLY(X, J, FROM)                                                                             \
+    _Pragma("unroll") for (int y = 0; y < FN; ++y) acc[X][y] =                                              \
+        __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(fa[FROM][X]), operand(fb[FROM][y]), acc[X][y], \
+                                                        kFp4, kFp4, J, ea[0][X], J, eb[0][y]);
+
+    // A step: rows x of its fragments, the next step's operand reads between
+    // them, none before the last row (sched_barrier keeps this order).
+    constexpr int kReads = FM > 1 ? (FM + FN + FM - 2) / (FM > 1 ? FM - 1 : 1) : FM + FN;
+    constexpr int kRowLoads = (kLoads + FM - 1) / FM;
+#define MX_STEP(J, FROM, BUF)                                                                                 \
+    _Pragma("unroll") for (int x = 0; x < FM; ++x) {                                                          \
+        _Pragma("unroll") for (int i = x * kReads; i < (x + 1) * kReads && i < FM + FN; ++i)                  \
+            read_one(i, BUF, J + 1, 1 - FROM);                                                                \
+        MX_MULTIPLY(x, J, FROM)                                                                               \
+        __builtin_amdgcn_sched_barrier(0);                                                                    \
+    }
 
     // One stage; its first step's operands are in registers.  In its last
     // step the next stage has arrived and the block's reads of this one are
     // done, so one barrier serves both buffers.
-    auto stage = [&](int s, int cur) {
-        read_step(cur, 1, 1);
-        MX_STEP(0, 0, 0)
-        read_step(cur, 2, 0);
-        MX_STEP(1, 1, 0)
-        read_step(cur, 3, 1);
-        MX_STEP(2, 0, 0)
-        if (s + 1 < s1) {
+    // LEFT: stages after this one, 2 standing for more (the loop's body has no
+    // branches, over which the compiler would move the products).
+    auto stage = [&](auto left, int s, int cur) {
+        constexpr bool more = decltype(left)::value > 0, load = decltype(left)::value > 1;
+        MX_STEP(0, 0, cur)
+        MX_STEP(1, 1, cur)
+        MX_STEP(2, 0, cur)
+        if (more) {
             wait_loads();
             block_barrier();
             read_step(cur ^ 1, 0, 0);
             read_scales(cur ^ 1, 1);
-            if (s + 2 < s1) load_stage(s + 2, cur);
         }
-        MX_STEP(3, 1, 0)
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int x = 0; x < FM; ++x) {
+            MX_MULTIPLY(x, 3, 1)
+            __builtin_amdgcn_sched_barrier(0);
+            if (load) {
+#pragma unroll
+                for (int i = x * kRowLoads; i < (x + 1) * kRowLoads && i < kLoads; ++i) load_one(i, s + 2, cur);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
 #pragma unroll
         for (int f = 0; f < FM; ++f) ea[0][f] = ea[1][f];
 #pragma unroll
@@ -249,9 +338,16 @@ __device__ __forceinline__ void tile_product(const MxProductArgs& a, unsigned ti
         block_barrier();
         read_step(0, 0, 0);
         read_scales(0, 0);
-        for (int s = s0; s < s1; ++s) stage(s, (s - s0) & 1);
+        int s = s0, cur = 0;
+        for (; s + 2 < s1; ++s, cur ^= 1) stage(std::integral_constant<int, 2>{}, s, cur);
+        if (s + 1 < s1) {
+            stage(std::integral_constant<int, 1>{}, s, cur);
+            cur ^= 1;
+        }
+        stage(std::integral_constant<int, 0>{}, s, cur);
     }
 #undef MX_STEP
+#undef MX_MULTIPLY
 
     // A strip of 32 rows at a time goes through the wave's own part of LDS, so
     // that the stores are of whole rows.  Fragment element i of lane l: row
@@ -260,6 +356,7 @@ __device__ __forceinline__ void tile_product(const MxProductArgs& a, unsigned ti
     constexpr int kWide = BN / 2, kRow = kWide + 4;
     float* strip = reinterpret_cast<float*>(sm) + w * 32 * kRow;
     const Out o = output_of(a, split);
+    const bool whole = o.wide && !o.add && i0 + BM <= a.m && j0 + BN <= a.n;
 #pragma unroll
     for (int x = 0; x < FM; ++x) {
 #pragma unroll
@@ -267,14 +364,9 @@ __device__ __forceinline__ void tile_product(const MxProductArgs& a, unsigned ti
 #pragma unroll
             for (int i = 0; i < 16; ++i) strip[((i / 4) * 8 + h * 4 + i % 4) * kRow + y * 32 + r] = acc[x][y][i];
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        constexpr int kLanes = kWide / 4, kRows = 64 / kLanes;  // lanes of a row, rows of a store
-        const int c = (lane % kLanes) * 4;
-        const int64_t col = j0 + wn * kWide + c;
-        for (int t = lane / kLanes; t < 32; t += kRows) {
-            const int64_t row = i0 + wm * (BM / 2) + x * 32 + t;
-            const float4 v = *reinterpret_cast<const float4*>(strip + t * kRow + c);
-            if (row < a.m && col < a.n) store4(o, row, col, v, a.n);
-        }
+        const int64_t row0 = i0 + wm * (BM / 2) + x * 32, col0 = j0 + wn * kWide;
+        if (whole) store_strip<kWide>(o, strip, lane, row0, col0);
+        else store_edge<kWide>(o, strip, lane, row0, col0, a.m, a.n);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
 }
