@@ -26,7 +26,11 @@
  *
  * Storage of a [rows, cols] tensor: cols is padded to a multiple of
  * AGS_MX_PAD; codes are [rows][padded / 2] bytes, element 2i in the low half
- * of byte i; scales are [rows][padded / 32] bytes.  Padding holds zeros.
+ * of byte i, padding 0.  Scales are [padded / 256][rows'][8] bytes, rows' the
+ * rows rounded up to AGS_MX_ROWS: the 8 scales of 256 columns, row after row
+ * (a product reads the scales of many rows and few columns at a time; row by
+ * row they would lie one to a cache line).  Scales of padding columns are 0,
+ * those of padding rows undefined.
  *
  * Products contract the blocked axis of both operands:
  *
@@ -57,6 +61,7 @@ extern "C" {
 
 #define AGS_MX_BLOCK 32
 #define AGS_MX_PAD 256
+#define AGS_MX_ROWS 16
 
 /* rows >= 0, cols >= 0 are the logical sizes (an empty tensor has no
  * buffers; its product is zero).  codes and scales are device memory of

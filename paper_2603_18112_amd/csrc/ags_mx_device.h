@@ -10,6 +10,12 @@
 namespace ags {
 namespace mx {
 
+// Where the scale of (row, column c) stands.
+__device__ __forceinline__ int64_t scale_at(int64_t rows, int64_t row, int64_t c) {
+    const int64_t rp = (rows + AGS_MX_ROWS - 1) / AGS_MX_ROWS * AGS_MX_ROWS;
+    return ((c >> 8) * rp + row) * 8 + ((c >> 5) & 7);
+}
+
 // The scale byte (e + 127) of a block whose largest magnitude has these fp32
 // bits.  The bits of magnitudes order like their values, infinities and NaN
 // above all others.

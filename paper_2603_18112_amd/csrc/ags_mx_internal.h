@@ -13,12 +13,16 @@ namespace ags {
 
 constexpr int64_t mx_padded(int64_t cols) { return (cols + AGS_MX_PAD - 1) / AGS_MX_PAD * AGS_MX_PAD; }
 
+// Scales: rows rounded up, bytes between chunks of 256 columns.
+constexpr int64_t mx_scale_rows(int64_t rows) { return (rows + AGS_MX_ROWS - 1) / AGS_MX_ROWS * AGS_MX_ROWS; }
+constexpr int64_t mx_scale_bytes(int64_t rows, int64_t cols) { return mx_padded(cols) / 32 * mx_scale_rows(rows); }
+
 struct MxQuantArgs {
     const void* x;
     const uint8_t* noise;  // NULL: to nearest
     int64_t rows, cols, stride, noise_stride;
-    uint8_t *codes, *scales;      // [rows][padded cols / 2], NULL: not wanted
-    uint8_t *codes_t, *scales_t;  // [cols][padded rows / 2]
+    uint8_t *codes, *scales;      // of x, NULL: not wanted
+    uint8_t *codes_t, *scales_t;  // of x transposed
     int32_t bf16;
     int32_t aligned;  // rows of x (and of the noise) start at 16 (8) bytes
 };
@@ -31,7 +35,7 @@ struct MxDequantArgs {
 };
 
 struct MxProductArgs {
-    const uint8_t *a, *sa, *b, *sb;  // codes and scales, [m][kp / 2], [n][kp / 2]
+    const uint8_t *a, *sa, *b, *sb;  // codes and scales of [m, kp] and [n, kp]
     void* out;
     int64_t stride;
     int64_t m, n, kp;

@@ -44,14 +44,16 @@ __device__ __forceinline__ unsigned short bf16_round(float x) { return (unsigned
 struct Out {
     char* p;
     int64_t stride;
-    bool bf16, add, wide;  // wide: four elements are one aligned store
+    bool bf16, add;
+    bool wide, wide16;  // rows start where 4 elements, or 16 bytes, are one aligned store
 };
 
 __device__ __forceinline__ Out output_of(const MxProductArgs& a, unsigned split) {
-    Out o{static_cast<char*>(a.out), a.stride, a.bf16 != 0, a.accumulate != 0, false};
-    if (a.splits > 1) o = Out{reinterpret_cast<char*>(a.partials + (int64_t)split * a.m * a.n), a.n, false, false, false};
+    Out o{static_cast<char*>(a.out), a.stride, a.bf16 != 0, a.accumulate != 0, false, false};
+    if (a.splits > 1) o = Out{reinterpret_cast<char*>(a.partials + (int64_t)split * a.m * a.n), a.n, false, false, false, false};
     const unsigned low = (unsigned)reinterpret_cast<uintptr_t>(o.p) | ((unsigned)o.stride * (o.bf16 ? 2u : 4u));
     o.wide = (low & (o.bf16 ? 7u : 15u)) == 0;
+    o.wide16 = (low & 15u) == 0;
     return o;
 }
 
@@ -135,41 +137,28 @@ __device__ __forceinline__ void block_barrier() {
 }
 
 // TM x TN: the tile in units of 64; four waves, two by two.
-// 32 rows of WIDE results from LDS (rows of WIDE + 4 floats) to the output, all
-// of them inside it.
-template <int WIDE>
-__device__ __forceinline__ void store_strip(const Out& o, const float* strip, int lane, int64_t row0, int64_t col0) {
-    if (o.bf16) {
-        constexpr int kLanes = WIDE / 8, kRows = 64 / kLanes;  // lanes of a row, rows of a store
-        const int c = (lane % kLanes) * 8, t0 = lane / kLanes;
-        char* p = o.p + ((row0 + t0) * o.stride + col0 + c) * 2;
+// 32 rows of BYTES bytes from LDS (PITCH apart) to memory, all inside the output.
+template <int BYTES, int PITCH>
+__device__ __forceinline__ void store_strip(const char* strip, int lane, char* to, int64_t stride) {
+    constexpr int kLanes = BYTES / 16, kRows = 64 / kLanes;  // lanes of a row, rows of a store
+    const int c = (lane % kLanes) * 16, t0 = lane / kLanes;
+    strip += t0 * PITCH + c;
+    to += t0 * stride + c;
 #pragma unroll
-        for (int t = 0; t < 32; t += kRows) {
-            const float4* v = reinterpret_cast<const float4*>(strip + (t0 + t) * (WIDE + 4) + c);
-            const float4 u = v[0], w = v[1];
-            *reinterpret_cast<uint4*>(p + t * o.stride * 2) =
-                make_uint4(pack_bf16(u.x, u.y), pack_bf16(u.z, u.w), pack_bf16(w.x, w.y), pack_bf16(w.z, w.w));
-        }
-    } else {
-        constexpr int kLanes = WIDE / 4, kRows = 64 / kLanes;
-        const int c = (lane % kLanes) * 4, t0 = lane / kLanes;
-        char* p = o.p + ((row0 + t0) * o.stride + col0 + c) * 4;
-#pragma unroll
-        for (int t = 0; t < 32; t += kRows)
-            *reinterpret_cast<float4*>(p + t * o.stride * 4) =
-                *reinterpret_cast<const float4*>(strip + (t0 + t) * (WIDE + 4) + c);
-    }
+    for (int t = 0; t < 32; t += kRows)
+        *reinterpret_cast<uint4*>(to + t * stride) = *reinterpret_cast<const uint4*>(strip + t * PITCH);
 }
 
-// The same where rows or columns end inside, or results are added.
-template <int WIDE>
-__device__ __forceinline__ void store_edge(const Out& o, const float* strip, int lane, int64_t row0, int64_t col0,
+// 32 rows of WIDE fp32 results where rows or columns end inside, or results
+// are added.
+template <int WIDE, int PITCH>
+__device__ __forceinline__ void store_edge(const Out& o, const char* strip, int lane, int64_t row0, int64_t col0,
                                            int64_t m, int64_t n) {
     constexpr int kLanes = WIDE / 4, kRows = 64 / kLanes;
     const int c = (lane % kLanes) * 4;
 #pragma unroll 1
     for (int t = lane / kLanes; t < 32; t += kRows) {
-        const float4 v = *reinterpret_cast<const float4*>(strip + t * (WIDE + 4) + c);
+        const float4 v = *reinterpret_cast<const float4*>(strip + t * PITCH + c * 4);
         if (row0 + t < m && col0 + c < n) store4(o, row0 + t, col0 + c, v, n);
     }
 }
@@ -186,50 +175,55 @@ __device__ __forceinline__ void tile_product(const MxProductArgs& a, unsigned ti
     unsigned ti, tj;
     tile_of_block(blockIdx.x % tiles, tiles_m, tiles_n, ti, tj);
     const int64_t i0 = (int64_t)ti * BM, j0 = (int64_t)tj * BN;
-    const unsigned pitch = (unsigned)(a.kp / 2), spitch = (unsigned)(a.kp / 32);
+    const unsigned pitch = (unsigned)(a.kp / 2);
     const int stages = (int)(a.kp / 256);
     const int s0 = (int)((int64_t)stages * split / a.splits), s1 = (int)((int64_t)stages * (split + 1) / a.splits);
     const int ma = (int)min((int64_t)BM, a.m - i0), nb = (int)min((int64_t)BN, a.n - j0);
 
-    const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<uint8_t*>(a.a + i0 * pitch), 0, (unsigned)ma * pitch, 0x00027000);
-    const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<uint8_t*>(a.b + j0 * pitch), 0, (unsigned)nb * pitch, 0x00027000);
-    const __amdgpu_buffer_rsrc_t rsa = __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<uint8_t*>(a.sa + i0 * spitch), 0, (unsigned)ma * spitch, 0x00027000);
-    const __amdgpu_buffer_rsrc_t rsb = __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<uint8_t*>(a.sb + j0 * spitch), 0, (unsigned)nb * spitch, 0x00027000);
+    // Buffers of the tile's rows; of no bytes for a stage past the last.
+    auto buffer = [&](const uint8_t* p, unsigned bytes, int s) {
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, s < s1 ? bytes : 0u, 0x00027000);
+    };
+    const uint8_t *const ca = a.a + i0 * pitch, *const cb = a.b + j0 * pitch;
+    const unsigned pa = (unsigned)mx_scale_rows(a.m) * 8, pb = (unsigned)mx_scale_rows(a.n) * 8;
+    const unsigned chunks = (unsigned)(a.kp / 256);
+    const uint8_t *const sca = a.sa + i0 * 8, *const scb = a.sb + j0 * 8;
+    const unsigned sza = chunks * pa - (unsigned)i0 * 8, szb = chunks * pb - (unsigned)j0 * 8;
 
     // A wave's load takes 8 rows of 128 bytes.  LDS keeps rows of 128 bytes
-    // whose 16-byte pieces are permuted by the row's low three bits, so that
-    // the operand reads of 8 neighbouring lanes fall on 8 different places.
+    // whose 16-byte pieces c stand at c ^ ((row / 2) % 8): the operand reads of
+    // any 16 rows that differ modulo 16 then fall on the 16 places of the 64
+    // banks (with c ^ (row % 8) rows 8 apart met on the same banks).
     // Rows past the end repeat the last one; their results are not stored.
-    unsigned va[BM / 32], vb[BN / 32], vs[(BM + BN) / 128];
-    const unsigned piece = (unsigned)((lane & 7) ^ (lane >> 3)) * 16;
+    // A stage's scales are 8 bytes a row, A's rows then B's.
+    constexpr int kScale = (BM + BN) * 8 % 4096 == 0 ? 16 : 4, kScaleLoads = (BM + BN) * 8 / (256 * kScale);
+    unsigned vs[kScaleLoads];
+    const unsigned piece = (unsigned)((lane & 7) ^ ((4 * w + (lane >> 4)) & 7)) * 16;  // (i * 4 + w) * 8 + lane / 8
+    unsigned first = (unsigned)(w * 8 + (lane >> 3)) * pitch + piece;
+    const unsigned last_a = (unsigned)(ma - 1) * pitch + piece, last_b = (unsigned)(nb - 1) * pitch + piece;
 #pragma unroll
-    for (int i = 0; i < BM / 32; ++i) va[i] = (unsigned)min((i * 4 + w) * 8 + (lane >> 3), ma - 1) * pitch + piece;
-#pragma unroll
-    for (int i = 0; i < BN / 32; ++i) vb[i] = (unsigned)min((i * 4 + w) * 8 + (lane >> 3), nb - 1) * pitch + piece;
-#pragma unroll
-    for (int i = 0; i < (BM + BN) / 128; ++i) {
-        const int d = (i * 4 + w) * 64 + lane;  // dword of the scales, A's then B's
-        const bool is_a = (i * 4 + w) * 64 < BM * 2;
-        const int row = is_a ? min(d / 2, ma - 1) : min(d / 2 - BM, nb - 1);
-        vs[i] = (unsigned)row * spitch + (d & 1) * 4;
+    for (int i = 0; i < kScaleLoads; ++i) {
+        const int at = ((i * 4 + w) * 64 + lane) * kScale;  // byte of A's, then of B's
+        const bool is_a = (i * 4 + w) * 64 * kScale < BM * 8;
+        // (the last pair of rows may hold a padding row)
+        vs[i] = is_a ? (unsigned)min(at, (ma - 1) * 8 / 16 * 16 + (at & 15)) : (unsigned)min(at - BM * 8, (nb - 1) * 8 / 16 * 16 + (at & 15));
     }
     const unsigned lds0 = (unsigned)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)sm);
-    constexpr int kLoads = BM / 32 + BN / 32 + (BM + BN) / 128;
+    constexpr int kLoads = BM / 32 + BN / 32 + kScaleLoads;
     auto load_one = [&](int i, int s, int buf) {  // load i of a stage
         const unsigned p = lds0 + buf * kBuf;
         if (i < BM / 32) {
-            load_lds16(ra, p + (i * 4 + w) * 1024, va[i], s * 128);
+            load_lds16(buffer(ca, ma * pitch, s), p + (i * 4 + w) * 1024, min(first + i * 32 * pitch, last_a), s * 128);
         } else if (i < BM / 32 + BN / 32) {
             const int t = i - BM / 32;
-            load_lds16(rb, p + BM * 128 + (t * 4 + w) * 1024, vb[t], s * 128);
+            load_lds16(buffer(cb, nb * pitch, s), p + BM * 128 + (t * 4 + w) * 1024, min(first + t * 32 * pitch, last_b), s * 128);
         } else {
             const int t = i - BM / 32 - BN / 32;
-            const bool is_a = (t * 4 + w) * 64 < BM * 2;
-            load_lds4(is_a ? rsa : rsb, p + kStage + (t * 4 + w) * 256, vs[t], s * 8);
+            const bool is_a = (t * 4 + w) * 64 * kScale < BM * 8;
+            const unsigned to = p + kStage + (t * 4 + w) * 64 * kScale, off = s * (is_a ? pa : pb);
+            const __amdgpu_buffer_rsrc_t rs = buffer(is_a ? sca : scb, is_a ? sza : szb, s);
+            if (kScale == 16) load_lds16(rs, to, vs[t], off);
+            else load_lds4(rs, to, vs[t], off);
         }
     };
     auto load_stage = [&](int s, int buf) {
@@ -237,15 +231,15 @@ __device__ __forceinline__ void tile_product(const MxProductArgs& a, unsigned ti
         for (int i = 0; i < kLoads; ++i) load_one(i, s, buf);
     };
 
-    // Operands: lane l holds row l % 32; its half h = l / 32 takes the pieces
-    // 4 h + j of a stage in step j (the order of the contracted elements is
-    // free as long as both operands agree), so that the four scales of a
-    // stage are one dword.
-    constexpr int FM = TM, FN = TN;  // 32 x 32 fragments of a wave
+    // Operands: lane l holds row r = l % 32 of a fragment; its half h = l / 32
+    // takes the pieces 4 h + j of a stage in step j of four (the order of the
+    // contracted elements is free as long as both operands agree), so that a
+    // stage's four scales are one dword.
+    constexpr int FM = BM / 64, FN = BN / 64;  // 32 x 32 fragments of a wave
     const int r = lane & 31, h = lane >> 5, wm = w >> 1, wn = w & 1;
     int off[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) off[j] = r * 128 + (((h * 4 + j) ^ (r & 7)) << 4);
+    for (int j = 0; j < 4; ++j) off[j] = r * 128 + (((h * 4 + j) ^ ((r >> 1) & 7)) << 4);
     const int oa = wm * (BM / 2) * 128, ob = BM * 128 + wn * (BN / 2) * 128;
     const int osa = kStage + (wm * (BM / 2) + r) * 8 + h * 4, osb = kStage + (BM + wn * (BN / 2) + r) * 8 + h * 4;
     uint4 fa[2][FM], fb[2][FN];
@@ -261,10 +255,6 @@ __device__ __forceinline__ void tile_product(const MxProductArgs& a, unsigned ti
             fa[to][f] = *reinterpret_cast<const uint4*>(p + oa + f * 4096 + off[j]);
         }
     };
-    auto read_step = [&](int buf, int j, int to) {
-#pragma unroll
-        for (int i = 0; i < FM + FN; ++i) read_one(i, buf, j, to);
-    };
     auto read_scales = [&](int buf, int to) {
         const char* p = sm + buf * kBuf;
 #pragma unroll
@@ -273,6 +263,8 @@ __device__ __forceinline__ void tile_product(const MxProductArgs& a, unsigned ti
         for (int f = 0; f < FN; ++f) eb[to][f] = *reinterpret_cast<const int*>(p + osb + f * 256);
     };
 
+    // B's fragments are the instruction's first operand: four results of a
+    // lane are then neighbours in a row of the output.
     v16f acc[FM][FN];
 #pragma unroll
     for (int x = 0; x < FM; ++x)
@@ -281,50 +273,45 @@ __device__ __forceinline__ void tile_product(const MxProductArgs& a, unsigned ti
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[x][y][i] = 0.0f;
 
-#define MX_MULTIPLY(X, J, FROM)                                                                             \
-    _Pragma("unroll") for (int y = 0; y < FN; ++y) acc[X][y] =                                              \
-        __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(fa[FROM][X]), operand(fb[FROM][y]), acc[X][y], \
-                                                        kFp4, kFp4, J, ea[0][X], J, eb[0][y]);
+#define MX_MULTIPLY(X, J)                                                                                     \
+    _Pragma("unroll") for (int y = 0; y < FN; ++y) acc[X][y] =                                                \
+        __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(fb[(J) & 1][y]), operand(fa[(J) & 1][X]),     \
+                                                        acc[X][y], kFp4, kFp4, J, eb[0][y], J, ea[0][X]);     \
+    __builtin_amdgcn_sched_barrier(0);
 
-    // A step: rows x of its fragments, the next step's operand reads between
-    // them, none before the last row (sched_barrier keeps this order).
+    // A stage's loads are spread over the steps in which its buffer is free
+    // and time is left for them to arrive: the last step of the stage two
+    // before and the first two of the next.  sched_barrier keeps the order.
+    constexpr int kSlots = 3 * FM;
+#define MX_LOADS(SLOT, S, BUF)                                                                       \
+    _Pragma("unroll") for (int i = (SLOT) * kLoads / kSlots; i < ((SLOT) + 1) * kLoads / kSlots; ++i) \
+        load_one(i, S, BUF);                                                                         \
+    __builtin_amdgcn_sched_barrier(0);
+
+    // Step J: products of one row of fragments after the other, the next
+    // step's reads between them, none before the last row.
     constexpr int kReads = FM > 1 ? (FM + FN + FM - 2) / (FM > 1 ? FM - 1 : 1) : FM + FN;
-    constexpr int kRowLoads = (kLoads + FM - 1) / FM;
-#define MX_STEP(J, FROM, BUF)                                                                                 \
-    _Pragma("unroll") for (int x = 0; x < FM; ++x) {                                                          \
-        _Pragma("unroll") for (int i = x * kReads; i < (x + 1) * kReads && i < FM + FN; ++i)                  \
-            read_one(i, BUF, J + 1, 1 - FROM);                                                                \
-        MX_MULTIPLY(x, J, FROM)                                                                               \
-        __builtin_amdgcn_sched_barrier(0);                                                                    \
+#define MX_STEP(J, NEXT_BUF, SLOT, LOAD_STAGE, LOAD_BUF)                                              \
+    _Pragma("unroll") for (int x = 0; x < FM; ++x) {                                                  \
+        _Pragma("unroll") for (int i = x * kReads; i < (x + 1) * kReads && i < FM + FN; ++i)          \
+            read_one(i, NEXT_BUF, ((J) + 1) & 3, ((J) + 1) & 1);                                      \
+        MX_MULTIPLY(x, J)                                                                             \
+        if ((SLOT) < 3) { MX_LOADS((SLOT) * FM + x, LOAD_STAGE, LOAD_BUF) }                           \
     }
 
-    // One stage; its first step's operands are in registers.  In its last
-    // step the next stage has arrived and the block's reads of this one are
-    // done, so one barrier serves both buffers.
-    // LEFT: stages after this one, 2 standing for more (the loop's body has no
-    // branches, over which the compiler would move the products).
-    auto stage = [&](auto left, int s, int cur) {
-        constexpr bool more = decltype(left)::value > 0, load = decltype(left)::value > 1;
-        MX_STEP(0, 0, cur)
-        MX_STEP(1, 1, cur)
-        MX_STEP(2, 0, cur)
-        if (more) {
-            wait_loads();
-            block_barrier();
-            read_step(cur ^ 1, 0, 0);
-            read_scales(cur ^ 1, 1);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int x = 0; x < FM; ++x) {
-            MX_MULTIPLY(x, 3, 1)
-            __builtin_amdgcn_sched_barrier(0);
-            if (load) {
-#pragma unroll
-                for (int i = x * kRowLoads; i < (x + 1) * kRowLoads && i < kLoads; ++i) load_one(i, s + 2, cur);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-        }
+    // One stage; the operands of its first step are in registers.  Before its
+    // last step the next stage has arrived and the block's reads of this one
+    // are done, so one barrier serves both buffers.  The body has no branches,
+    // over which the compiler would move the products: past the last stage the
+    // loads find a buffer of no bytes, and operands are read that nothing uses.
+    auto stage = [&](int s, int cur) {
+        MX_STEP(0, cur, 1, s + 1, cur ^ 1)
+        MX_STEP(1, cur, 2, s + 1, cur ^ 1)
+        MX_STEP(2, cur, 3, 0, 0)
+        wait_loads();
+        block_barrier();
+        read_scales(cur ^ 1, 1);
+        MX_STEP(3, cur ^ 1, 0, s + 2, cur)
 #pragma unroll
         for (int f = 0; f < FM; ++f) ea[0][f] = ea[1][f];
 #pragma unroll
@@ -334,39 +321,56 @@ __device__ __forceinline__ void tile_product(const MxProductArgs& a, unsigned ti
     if (s0 < s1) {
         load_stage(s0, 0);
         wait_loads();
-        if (s0 + 1 < s1) load_stage(s0 + 1, 1);
+#pragma unroll
+        for (int x = 0; x < FM; ++x) { MX_LOADS(x, s0 + 1, 1) }
         block_barrier();
-        read_step(0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < FM + FN; ++i) read_one(i, 0, 0, 0);
         read_scales(0, 0);
-        int s = s0, cur = 0;
-        for (; s + 2 < s1; ++s, cur ^= 1) stage(std::integral_constant<int, 2>{}, s, cur);
-        if (s + 1 < s1) {
-            stage(std::integral_constant<int, 1>{}, s, cur);
-            cur ^= 1;
-        }
-        stage(std::integral_constant<int, 0>{}, s, cur);
+        for (int s = s0, cur = 0; s < s1; ++s, cur ^= 1) stage(s, cur);
+        wait_loads();
     }
 #undef MX_STEP
+#undef MX_LOADS
 #undef MX_MULTIPLY
 
-    // A strip of 32 rows at a time goes through the wave's own part of LDS, so
-    // that the stores are of whole rows.  Fragment element i of lane l: row
-    // 8 (i / 4) + 4 h + i % 4, column l % 32.
+    // 32 rows at a time go through the wave's own part of LDS, so that the
+    // stores are of whole rows.  Lane l holds row l % 32 of a fragment, and of
+    // each 8 columns the four from 4 (l / 32).
     block_barrier();
-    constexpr int kWide = BN / 2, kRow = kWide + 4;
-    float* strip = reinterpret_cast<float*>(sm) + w * 32 * kRow;
+    constexpr int kWide = BN / 2;
+    char* strip = sm + w * 32 * (kWide * 4 + 16);
     const Out o = output_of(a, split);
-    const bool whole = o.wide && !o.add && i0 + BM <= a.m && j0 + BN <= a.n;
+    const bool whole = o.wide16 && !o.add && i0 + BM <= a.m && j0 + BN <= a.n;
 #pragma unroll
     for (int x = 0; x < FM; ++x) {
-#pragma unroll
-        for (int y = 0; y < FN; ++y)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) strip[((i / 4) * 8 + h * 4 + i % 4) * kRow + y * 32 + r] = acc[x][y][i];
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         const int64_t row0 = i0 + wm * (BM / 2) + x * 32, col0 = j0 + wn * kWide;
-        if (whole) store_strip<kWide>(o, strip, lane, row0, col0);
-        else store_edge<kWide>(o, strip, lane, row0, col0, a.m, a.n);
+        if (whole && o.bf16) {
+            constexpr int kPitch = kWide * 2 + 16;
+#pragma unroll
+            for (int y = 0; y < FN; ++y)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const v16f v = acc[x][y];
+                    *reinterpret_cast<uint2*>(strip + r * kPitch + y * 64 + g * 16 + h * 8) =
+                        make_uint2(pack_bf16(v[4 * g], v[4 * g + 1]), pack_bf16(v[4 * g + 2], v[4 * g + 3]));
+                }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            store_strip<kWide * 2, kPitch>(strip, lane, o.p + (row0 * o.stride + col0) * 2, o.stride * 2);
+        } else {
+            constexpr int kPitch = kWide * 4 + 16;
+#pragma unroll
+            for (int y = 0; y < FN; ++y)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const v16f v = acc[x][y];
+                    *reinterpret_cast<float4*>(strip + r * kPitch + y * 128 + g * 32 + h * 16) =
+                        make_float4(v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]);
+                }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            if (whole) store_strip<kWide * 4, kPitch>(strip, lane, o.p + (row0 * o.stride + col0) * 4, o.stride * 4);
+            else store_edge<kWide, kPitch>(o, strip, lane, row0, col0, a.m, a.n);
+        }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
 }
@@ -378,7 +382,7 @@ __global__ __launch_bounds__(256, 1) void mx_tile_kernel(MxProductArgs a, unsign
 
 __global__ __launch_bounds__(256) void mx_join_kernel(MxProductArgs a) {
     const int64_t total = a.m * a.n;
-    const Out o{static_cast<char*>(a.out), a.stride, a.bf16 != 0, a.accumulate != 0, false};
+    const Out o{static_cast<char*>(a.out), a.stride, a.bf16 != 0, a.accumulate != 0, false, false};
     for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < total; t += (int64_t)gridDim.x * 256) {
         float v = 0.0f;
         for (int s = 0; s < a.splits; ++s) v += a.partials[s * total + t];

@@ -73,7 +73,7 @@ __global__ __launch_bounds__(kQBlock) void mx_rows_kernel(MxQuantArgs a, int64_t
     }
     const int64_t kp = (int64_t)per_row * 256;
     *reinterpret_cast<unsigned*>(a.codes + (int64_t)row * (kp / 2) + c / 2) = codes;
-    if ((lane & 3) == 0) a.scales[(int64_t)row * (kp / 32) + c / 32] = (uint8_t)b;
+    if ((lane & 3) == 0) a.scales[mx::scale_at(a.rows, row, c)] = (uint8_t)b;
 }
 
 // One block: 256 rows (the padding unit of the transposed form) of 16
@@ -117,7 +117,7 @@ __global__ __launch_bounds__(kQBlock) void mx_cols_kernel(MxQuantArgs a, unsigne
     }
     const int64_t kp = (int64_t)row_tiles * 256;
     *reinterpret_cast<uint2*>(a.codes_t + col * (kp / 2) + (r0 + part * 16) / 2) = make_uint2(codes[0], codes[1]);
-    if ((part & 1) == 0) a.scales_t[col * (kp / 32) + (r0 + part * 16) / 32] = (uint8_t)b;
+    if ((part & 1) == 0) a.scales_t[mx::scale_at(a.cols, col, r0 + part * 16)] = (uint8_t)b;
 }
 
 __global__ __launch_bounds__(kQBlock) void mx_dequant_kernel(MxDequantArgs a, int64_t units, unsigned per_row) {
@@ -126,7 +126,7 @@ __global__ __launch_bounds__(kQBlock) void mx_dequant_kernel(MxDequantArgs a, in
     const unsigned row = (unsigned)u / per_row, chunk = (unsigned)u % per_row;
     const int64_t c = (int64_t)chunk * 256 + (threadIdx.x & 31) * 8, kp = (int64_t)per_row * 256;
     const unsigned codes = *reinterpret_cast<const unsigned*>(a.codes + (int64_t)row * (kp / 2) + c / 2);
-    const unsigned b = a.scales[(int64_t)row * (kp / 32) + c / 32];
+    const unsigned b = a.scales[mx::scale_at(a.rows, row, c)];
     // 2^e in two steps of normal values; the product is exact in both types
     const float s1 = __uint_as_float(b == 255u ? 0x7fc00000u : ((b >> 1) + 64u) << 23);
     const float s2 = __uint_as_float((b - (b >> 1) + 63u) << 23);

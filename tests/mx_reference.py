@@ -44,12 +44,17 @@ def store_rows(x, noise=None):
     return v.reshape(rows, nb * 32)[:, :cols], np.where(bad, 128, e)
 
 
+def scale_rows(scales, rows, cols):
+    """Scale bytes [rows][padded / 32] of the stored [padded / 256][rows'][8]."""
+    kp, rp = -(-cols // 256) * 256, -(-rows // 16) * 16
+    return scales.reshape(kp // 256, rp, 8).transpose(1, 0, 2).reshape(rp, kp // 32)[:rows]
+
+
 def unpack(codes, scales, rows, cols):
-    """Values of packed bytes (codes [rows][padded / 2], scales [rows][padded / 32])."""
+    """Values of packed bytes, padding columns included."""
     kp = -(-cols // 256) * 256
     c = codes.reshape(rows, kp // 2)
     n = np.stack([c & 15, c >> 4], axis=2).reshape(rows, kp)
-    e = scales.reshape(rows, kp // 32).astype(np.float64) - 127.0
-    v = GRID[n & 7] * np.where(n & 8, -1.0, 1.0) * np.repeat(np.exp2(e), 32, axis=1)
-    v = np.where(np.repeat(scales.reshape(rows, kp // 32) == 255, 32, axis=1), np.nan, v)
-    return v
+    s = scale_rows(scales, rows, cols)
+    v = GRID[n & 7] * np.where(n & 8, -1.0, 1.0) * np.repeat(np.exp2(s.astype(np.float64) - 127.0), 32, axis=1)
+    return np.where(np.repeat(s == 255, 32, axis=1), np.nan, v)

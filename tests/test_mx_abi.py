@@ -29,7 +29,7 @@ def test_header_declares_the_binding_names():
 
 
 @pytest.mark.parametrize("rows,cols,codes,scales", [
-    (0, 0, 0, 0), (3, 0, 0, 0), (0, 5, 0, 0), (1, 1, 128, 8), (1, 256, 128, 8), (2, 257, 512, 32),
+    (0, 0, 0, 0), (3, 0, 0, 0), (0, 5, 0, 0), (1, 1, 128, 128), (1, 256, 128, 128), (17, 257, 17 * 256, 32 * 16),
     (4096, 25088, 4096 * 12544, 4096 * 784)])
 def test_bytes(lib, rows, cols, codes, scales):
     assert mx.ags_mx_bytes(rows, cols) == (codes, scales)
