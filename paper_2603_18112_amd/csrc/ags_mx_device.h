@@ -49,37 +49,35 @@ __device__ __forceinline__ unsigned codes_nearest(const float* x, unsigned byte)
     return r;
 }
 
-// One code with a random byte, in integers.  y = |x| 2^-e is exact and below
-// 8.  From 1 up the grid has one bit after the leading one, so adding
-// (r + 1/2) / 256 of that bit to the fp32 pattern carries into it, and over
-// the binade's end, as the rule asks; below 1 the grid is 1/2 and y a
-// fixed-point number with 24 bits after the point (its lower bits cannot
-// reach a threshold, all of which are multiples of 2^-10).
-__device__ __forceinline__ unsigned code_stochastic(float x, float inv, unsigned r) {
-    const unsigned sign = (__float_as_uint(x) >> 28) & 8u;
-    const float y = fabsf(x) * inv;
-    const unsigned up = (__float_as_uint(y) + ((2u * r + 1u) << 13)) >> 22;  // code + 252
-    const unsigned low = ((unsigned)(y * 0x1p24f) + ((2u * r + 1u) << 14)) >> 23;
-    return sign | (y >= 1.0f ? min(up - 252u, 7u) : low);
+// |x| 2^-e taken to a neighbour on the grid by a random byte r, with x's sign.
+// y = |x| 2^-e is exact and below 8.  From 1 up the grid has one bit after the
+// leading one, so adding (r + 1/2) / 256 of that bit to the fp32 pattern
+// carries into it, and over the binade's end, as the rule asks; what is below
+// the bit is then cut off.  Below 1 the grid is 1/2, that of the binade of
+// 1 + y.  That sum may round: y keeps 11 significant bits first (no threshold,
+// all multiples of 2^-10, lies between y and what is left of it), so the sum is
+// exact down to y = 2^-13, below which no byte rounds up.  bf16 values have 8.
+template <bool BF16>
+__device__ __forceinline__ float round_stochastic(float x, float inv, unsigned r) {
+    unsigned u = __float_as_uint(fabsf(x) * inv);
+    if (!BF16) u &= 0xffffe000u;
+    const float y = __uint_as_float(u), one = y < 1.0f ? 1.0f : 0.0f;
+    const unsigned up = (__float_as_uint(y + one) + ((r << 14) | 0x2000u)) & 0xffc00000u;
+    return copysignf(__uint_as_float(up) - one, x);
 }
 
-__device__ __forceinline__ unsigned codes_stochastic(const float* x, unsigned byte, const unsigned char* r) {
+// Codes of 8 elements and their random bytes; the converter has nothing left
+// to round, 8 becomes 6.
+template <bool BF16>
+__device__ __forceinline__ unsigned codes_stochastic(const float* x, unsigned byte, const unsigned* r) {
     const float inv = scale_inverse(byte);
-    unsigned c = 0;
+    float v[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) c |= code_stochastic(x[i], inv, r[i]) << (4 * i);
-    return c;
+    for (int i = 0; i < 8; ++i) v[i] = round_stochastic<BF16>(x[i], inv, r[i]);
+    return codes_nearest(v, 127u);
 }
 
 __device__ __forceinline__ unsigned magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
-
-// A code's value times 2: 0, 1, 2, 3, 4, 6, 8, 12, with its sign.
-__device__ __forceinline__ float code_value(unsigned c) {
-    const unsigned m = c & 7u;
-    const unsigned v = m < 4 ? m : (2u + (m & 1u)) << ((m >> 1) - 1);
-    const float f = 0.5f * (float)v;
-    return c & 8u ? -f : f;
-}
 
 }  // namespace mx
 }  // namespace ags

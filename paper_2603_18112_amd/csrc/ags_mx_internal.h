@@ -24,7 +24,6 @@ struct MxQuantArgs {
     uint8_t *codes, *scales;      // of x, NULL: not wanted
     uint8_t *codes_t, *scales_t;  // of x transposed
     int32_t bf16;
-    int32_t aligned;  // rows of x (and of the noise) start at 16 (8) bytes
 };
 
 struct MxDequantArgs {

@@ -1,13 +1,15 @@
 // gfx950 kernels that store tensors in 4 bits and read them back
 // (include/ags_mx.h).
 //
-// mx_rows_kernel   blocks along the rows: 32 lanes take 256 consecutive
-//                  elements, 8 each; 4 lanes share a block's scale.
-// mx_cols_kernel   blocks along the columns (the transposed form): a tile
-//                  goes through LDS, a thread takes 32 rows of a column.
+// mx_rows_kernel     blocks along the rows: 32 lanes take 256 consecutive
+//                    elements, 8 each; 4 lanes share a block's scale.
+// mx_transpose_kernel     blocks along the columns (the transposed form), and those
+//                    along the rows in the same pass: a tile of 128 x 128 goes
+//                    through LDS, a thread takes 32 rows of two columns.
 // mx_dequant_kernel  8 codes a thread.
 //
-// All stream from HBM and use no matrix cores.
+// All stream from HBM and use no matrix cores.  Rows may start anywhere: the
+// 16-byte accesses below need their element's alignment only.
 #include "ags_mx_device.h"
 #include "ags_mx_internal.h"
 
@@ -15,159 +17,350 @@ namespace ags {
 namespace {
 
 constexpr int kQBlock = 256;
+constexpr int kXcds = 8;
 
-__device__ __forceinline__ float load_elem(const void* x, bool bf16, int64_t i) {
-    if (bf16) return __uint_as_float((unsigned)static_cast<const unsigned short*>(x)[i] << 16);
-    return static_cast<const float*>(x)[i];
-}
+template <typename T, int N, int ALIGN>
+struct __attribute__((packed, aligned(ALIGN))) Unaligned {
+    T v[N];
+};
 
-// 8 elements from column c of a row that starts at element `at`; columns past
-// the end read as zero.
-__device__ __forceinline__ void load8(const MxQuantArgs& a, int64_t at, int64_t c, float* x) {
-    if (a.aligned && c + 8 <= a.cols) {
-        if (a.bf16) {
-            const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const unsigned short*>(a.x) + at + c);
-            const unsigned w[4] = {v.x, v.y, v.z, v.w};
+// 8 elements as fp32 from p; `left` of them lie inside the row, the rest read
+// as zero.
+__device__ __forceinline__ void load8(const unsigned short* p, int64_t left, float* x) {
+    if (left >= 8) {
+        const auto w = *reinterpret_cast<const Unaligned<unsigned, 4, 2>*>(p);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                x[2 * i] = __uint_as_float(w[i] << 16);
-                x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-            }
-        } else {
-            const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(a.x) + at + c);
-            const float4 u = p[0], v = p[1];
-            x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w, x[4] = v.x, x[5] = v.y, x[6] = v.z, x[7] = v.w;
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = __uint_as_float(w.v[i] << 16);
+            x[2 * i + 1] = __uint_as_float(w.v[i] & 0xffff0000u);
         }
         return;
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = c + i < a.cols ? load_elem(a.x, a.bf16, at + c + i) : 0.0f;
+    for (int i = 0; i < 8; ++i) x[i] = i < left ? __uint_as_float((unsigned)p[i] << 16) : 0.0f;
+}
+__device__ __forceinline__ void load8(const float* p, int64_t left, float* x) {
+    if (left >= 8) {
+        const auto w = *reinterpret_cast<const Unaligned<float, 8, 4>*>(p);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = w.v[i];
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = i < left ? p[i] : 0.0f;
+}
+__device__ __forceinline__ void load_noise8(const uint8_t* p, int64_t left, unsigned* r) {
+    if (left >= 8) {
+        const auto w = *reinterpret_cast<const Unaligned<unsigned, 2, 1>*>(p);
+        r[0] = w.v[0], r[1] = w.v[1];
+        return;
+    }
+    r[0] = r[1] = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < left) r[i >> 2] |= (unsigned)p[i] << (8 * (i & 3));
 }
 
+// r: the elements' random bytes.
+template <typename T, bool STOCHASTIC>
+__device__ __forceinline__ unsigned codes8(const float* x, unsigned byte, const unsigned* r) {
+    const unsigned c = STOCHASTIC ? mx::codes_stochastic<sizeof(T) == 2>(x, byte, r) : mx::codes_nearest(x, byte);
+    return byte == 255u ? 0u : c;
+}
+
+// The 8 bytes of two dwords.
+__device__ __forceinline__ void bytes8(const unsigned* w, unsigned* r) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = (w[i >> 2] >> (8 * (i & 3))) & 255u;
+}
+
+// The scale byte of 4 neighbouring lanes' 32 elements.
 template <bool STOCHASTIC>
-__global__ __launch_bounds__(kQBlock) void mx_rows_kernel(MxQuantArgs a, int64_t units, unsigned per_row) {
-    const int64_t u = (int64_t)blockIdx.x * (kQBlock / 32) + threadIdx.x / 32;
-    if (u >= units) return;  // whole half-waves
-    const unsigned row = (unsigned)u / per_row, chunk = (unsigned)u % per_row;
-    const int lane = threadIdx.x & 31;
-    const int64_t c = (int64_t)chunk * 256 + lane * 8;
-    float x[8];
-    load8(a, (int64_t)row * a.stride, c, x);
+__device__ __forceinline__ unsigned scale_of_quad(const float* x) {
     unsigned m = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) m = max(m, mx::magnitude(x[i]));
     m = max(m, (unsigned)__shfl_xor((int)m, 1, 64));
     m = max(m, (unsigned)__shfl_xor((int)m, 2, 64));
-    const unsigned b = mx::scale_byte<STOCHASTIC>(m);
-    unsigned codes = 0;
-    if (b != 255u) {
-        if (STOCHASTIC) {
-            unsigned char r[8];
-            const uint8_t* p = a.noise + (int64_t)row * a.noise_stride + c;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) r[i] = c + i < a.cols ? p[i] : 0;
-            codes = mx::codes_stochastic(x, b, r);
-        } else {
-            codes = mx::codes_nearest(x, b);
-        }
+    return mx::scale_byte<STOCHASTIC>(m);
+}
+
+template <typename T, bool STOCHASTIC>
+__global__ __launch_bounds__(kQBlock) void mx_rows_kernel(MxQuantArgs a, unsigned units, unsigned per_row) {
+    const unsigned u = blockIdx.x * (kQBlock / 32) + threadIdx.x / 32;
+    if (u >= units) return;  // whole half-waves
+    const unsigned row = u / per_row, chunk = u % per_row;
+    const int lane = threadIdx.x & 31;
+    const int64_t c = (int64_t)chunk * 256 + lane * 8;
+    float x[8];
+    load8(static_cast<const T*>(a.x) + row * a.stride + c, a.cols - c, x);
+    unsigned w[2], r[8];
+    if (STOCHASTIC) {
+        load_noise8(a.noise + row * a.noise_stride + c, a.cols - c, w);
+        bytes8(w, r);
     }
+    const unsigned b = scale_of_quad<STOCHASTIC>(x);
     const int64_t kp = (int64_t)per_row * 256;
-    *reinterpret_cast<unsigned*>(a.codes + (int64_t)row * (kp / 2) + c / 2) = codes;
+    *reinterpret_cast<unsigned*>(a.codes + row * (kp / 2) + c / 2) = codes8<T, STOCHASTIC>(x, b, r);
     if ((lane & 3) == 0) a.scales[mx::scale_at(a.rows, row, c)] = (uint8_t)b;
 }
 
-// One block: 256 rows (the padding unit of the transposed form) of 16
-// columns.  Thread t loads row t; then thread t = column * 16 + part takes
-// 32 rows of one column, two threads to a block of the format... each of the
-// 16 parts is half a block: 16 rows.
-constexpr int kTileCols = 16;
+// ------------------------------------------------------------ tile kernel --
 
-template <bool STOCHASTIC>
-__global__ __launch_bounds__(kQBlock) void mx_cols_kernel(MxQuantArgs a, unsigned row_tiles) {
-    __shared__ float sx[kTileCols][257];
-    __shared__ uint8_t sr[kTileCols][260];
-    const int tid = threadIdx.x;
-    const int64_t r0 = (int64_t)(blockIdx.x % row_tiles) * 256, c0 = (int64_t)(blockIdx.x / row_tiles) * kTileCols;
-    const int64_t row = r0 + tid;
-#pragma unroll
-    for (int j = 0; j < kTileCols; ++j) {
-        const bool in = row < a.rows && c0 + j < a.cols;
-        sx[j][tid] = in ? load_elem(a.x, a.bf16, row * a.stride + c0 + j) : 0.0f;
-        if (STOCHASTIC) sr[j][tid] = in ? a.noise[row * a.noise_stride + c0 + j] : 0;
-    }
-    __syncthreads();
-    const int j = tid >> 4, part = tid & 15;
-    const int64_t col = c0 + j;
-    float x[16];
-    unsigned m = 0;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        x[i] = sx[j][part * 16 + i];
-        m = max(m, mx::magnitude(x[i]));
-    }
-    m = max(m, (unsigned)__shfl_xor((int)m, 1, 64));
-    if (col >= a.cols) return;
-    const unsigned b = mx::scale_byte<STOCHASTIC>(m);
-    unsigned codes[2] = {0, 0};
-    if (b != 255u) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-            codes[h] = STOCHASTIC ? mx::codes_stochastic(x + 8 * h, b, &sr[j][part * 16 + 8 * h])
-                                  : mx::codes_nearest(x + 8 * h, b);
-    }
-    const int64_t kp = (int64_t)row_tiles * 256;
-    *reinterpret_cast<uint2*>(a.codes_t + col * (kp / 2) + (r0 + part * 16) / 2) = make_uint2(codes[0], codes[1]);
-    if ((part & 1) == 0) a.scales_t[mx::scale_at(a.cols, col, r0 + part * 16)] = (uint8_t)b;
+constexpr int kTile = 128;
+// Bytes between the columns' codes in LDS: 16-byte writes of 8 neighbouring
+// column pairs fall on different banks.
+constexpr int kCodePitch = kTile / 2 + 16;
+
+// The larger of two pairs of 16-bit magnitudes.
+__device__ __forceinline__ unsigned max_pairs(unsigned a, unsigned b) {
+    typedef unsigned short u2 __attribute__((ext_vector_type(2)));
+    const u2 m = __builtin_elementwise_max(__builtin_bit_cast(u2, a), __builtin_bit_cast(u2, b));
+    return __builtin_bit_cast(unsigned, m);
 }
 
-__global__ __launch_bounds__(kQBlock) void mx_dequant_kernel(MxDequantArgs a, int64_t units, unsigned per_row) {
-    const int64_t u = (int64_t)blockIdx.x * (kQBlock / 32) + threadIdx.x / 32;
-    if (u >= units) return;
-    const unsigned row = (unsigned)u / per_row, chunk = (unsigned)u % per_row;
-    const int64_t c = (int64_t)chunk * 256 + (threadIdx.x & 31) * 8, kp = (int64_t)per_row * 256;
-    const unsigned codes = *reinterpret_cast<const unsigned*>(a.codes + (int64_t)row * (kp / 2) + c / 2);
-    const unsigned b = a.scales[mx::scale_at(a.rows, row, c)];
-    // 2^e in two steps of normal values; the product is exact in both types
-    const float s1 = __uint_as_float(b == 255u ? 0x7fc00000u : ((b >> 1) + 64u) << 23);
-    const float s2 = __uint_as_float((b - (b >> 1) + 63u) << 23);
+// Two neighbouring columns' 32 values from LDS, and their magnitudes' maxima
+// (as fp32 bits).
+template <typename T>
+struct ColumnPair;
+template <>
+struct ColumnPair<unsigned short> {
+    unsigned w[32];  // both columns of a row
+    __device__ __forceinline__ void load(const unsigned short* p) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        if (c + i >= a.cols) break;
-        const float v = mx::code_value((codes >> (4 * i)) & 15u) * s1 * s2;
-        if (a.bf16)
-            static_cast<unsigned short*>(a.out)[(int64_t)row * a.stride + c + i] =
-                (unsigned short)(__float_as_uint(v) >> 16);
-        else
-            static_cast<float*>(a.out)[(int64_t)row * a.stride + c + i] = v;
+        for (int i = 0; i < 32; ++i) w[i] = *reinterpret_cast<const unsigned*>(p + i * kTile);
     }
+    __device__ __forceinline__ void maxima(unsigned* m) const {
+        unsigned t = 0;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) t = max_pairs(t, w[i] & 0x7fff7fffu);
+        m[0] = t << 16, m[1] = t & 0xffff0000u;
+    }
+    __device__ __forceinline__ float value(int c, int i) const {
+        return __uint_as_float(c ? w[i] & 0xffff0000u : w[i] << 16);
+    }
+};
+template <>
+struct ColumnPair<float> {
+    float2 w[32];
+    __device__ __forceinline__ void load(const float* p) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) w[i] = *reinterpret_cast<const float2*>(p + i * kTile);
+    }
+    __device__ __forceinline__ void maxima(unsigned* m) const {
+        m[0] = m[1] = 0;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            m[0] = max(m[0], mx::magnitude(w[i].x));
+            m[1] = max(m[1], mx::magnitude(w[i].y));
+        }
+    }
+    __device__ __forceinline__ float value(int c, int i) const { return c ? w[i].y : w[i].x; }
+};
+
+// One tile.  ROWS: the form along the rows is wanted too.  The grid covers
+// the padded rows and columns, since padding is stored as zeros.
+template <typename T, bool STOCHASTIC, bool ROWS>
+__global__ __launch_bounds__(kQBlock) void mx_transpose_kernel(MxQuantArgs a, unsigned tiles_c, unsigned tiles) {
+    __shared__ alignas(16) T tile[kTile * kTile];
+    __shared__ alignas(16) uint8_t noise[STOCHASTIC ? kTile * kTile : 8];
+    // The codes and scales of the columns take the tile's place once it has
+    // been read (with fp32 values and random bytes two blocks just fit a CU).
+    uint8_t *const codes = reinterpret_cast<uint8_t*>(tile), *const col_scale = codes + kTile * kCodePitch;
+    static_assert(kTile * (kCodePitch + 4) <= (int)sizeof(tile), "codes and scales fit");
+    // Consecutive blocks go to the 8 XCDs in turn; each XCD takes a run of
+    // tiles, so that both halves of a line of codes meet in one L2.
+    const unsigned xcd = blockIdx.x % kXcds, base = tiles / kXcds, rest = tiles % kXcds;
+    const unsigned t = xcd * base + min(xcd, rest) + blockIdx.x / kXcds;
+    const int64_t r0 = (int64_t)(t / tiles_c) * kTile, c0 = (int64_t)(t % tiles_c) * kTile;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int64_t kp = (int64_t)tiles_c * kTile;
+
+    // 16 threads take a row, 8 elements each; 16 rows at a time.
+    const int c = (tid & 15) * 8;
+    const int64_t left = a.cols - c0 - c;
+    const T* px = static_cast<const T*>(a.x) + c0 + c;
+    const uint8_t* pn = a.noise + c0 + c;
+    constexpr int kAhead = 4;  // rows of a thread in flight
+#pragma unroll
+    for (int i0 = 0; i0 < kTile / 16; i0 += kAhead) {
+        float x[kAhead][8];
+        unsigned r[kAhead][2];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int64_t row = r0 + (i0 + i) * 16 + (tid >> 4);
+            const int64_t l = row < a.rows ? left : 0;
+            load8(px + row * a.stride, l, x[i]);
+            if (STOCHASTIC) load_noise8(pn + row * a.noise_stride, l, r[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int lr = (i0 + i) * 16 + (tid >> 4);
+            if constexpr (sizeof(T) == 2) {
+                unsigned w[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    w[j] = (__float_as_uint(x[i][2 * j]) >> 16) | (__float_as_uint(x[i][2 * j + 1]) & 0xffff0000u);
+                *reinterpret_cast<uint4*>(&tile[lr * kTile + c]) = make_uint4(w[0], w[1], w[2], w[3]);
+            } else {
+                float4* p = reinterpret_cast<float4*>(&tile[lr * kTile + c]);
+                p[0] = make_float4(x[i][0], x[i][1], x[i][2], x[i][3]);
+                p[1] = make_float4(x[i][4], x[i][5], x[i][6], x[i][7]);
+            }
+            if (STOCHASTIC) *reinterpret_cast<uint2*>(&noise[lr * kTile + c]) = make_uint2(r[i][0], r[i][1]);
+            if (ROWS) {
+                const unsigned b = scale_of_quad<STOCHASTIC>(x[i]);
+                unsigned bytes[8];
+                if (STOCHASTIC) bytes8(r[i], bytes);
+                const unsigned v = codes8<T, STOCHASTIC>(x[i], b, bytes);
+                // the row's four scales as one dword
+                unsigned all = b << (2 * (tid & 12));
+                all |= (unsigned)__shfl_xor((int)all, 4, 64);
+                all |= (unsigned)__shfl_xor((int)all, 8, 64);
+                if (r0 + lr < a.rows) {
+                    *reinterpret_cast<unsigned*>(a.codes + (r0 + lr) * (kp / 2) + (c0 + c) / 2) = v;
+                    if ((tid & 15) == 0) *reinterpret_cast<unsigned*>(&a.scales[mx::scale_at(a.rows, r0 + lr, c0)]) = all;
+                }
+            }
+        }
+    }
+    __syncthreads();
+
+    // A wave takes 32 rows, a lane two columns.
+    const int rb = tid >> 6, cc = lane * 2;
+    ColumnPair<T> v;
+    v.load(&tile[rb * 32 * kTile + cc]);
+    unsigned m[2], cs[2][4];
+    uint8_t sc[2];
+    v.maxima(m);
+    unsigned nz[32];
+    if (STOCHASTIC) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+            nz[i] = *reinterpret_cast<const unsigned short*>(&noise[(rb * 32 + i) * kTile + cc]);
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const unsigned b = mx::scale_byte<STOCHASTIC>(m[k]);
+        sc[k] = (uint8_t)b;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            float x[8];
+            unsigned r[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                x[i] = v.value(k, 8 * g + i);
+                if (STOCHASTIC) r[i] = (nz[8 * g + i] >> (8 * k)) & 255u;
+            }
+            cs[k][g] = codes8<T, STOCHASTIC>(x, b, r);
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        *reinterpret_cast<uint4*>(codes + (cc + k) * kCodePitch + rb * 16) =
+            make_uint4(cs[k][0], cs[k][1], cs[k][2], cs[k][3]);
+        col_scale[(cc + k) * 4 + rb] = sc[k];
+    }
+    __syncthreads();
+    // Whole columns of the tile: 64 bytes each, four threads to a column.
+    const int64_t kpt = mx_padded(a.rows);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int col = i * 64 + (tid >> 2), part = (tid & 3) * 16;
+        if (c0 + col < a.cols)
+            *reinterpret_cast<uint4*>(a.codes_t + (c0 + col) * (kpt / 2) + r0 / 2 + part) =
+                *reinterpret_cast<const uint4*>(codes + col * kCodePitch + part);
+    }
+    if (tid < kTile && c0 + tid < a.cols)
+        *reinterpret_cast<unsigned*>(&a.scales_t[mx::scale_at(a.cols, c0 + tid, r0)]) =
+            *reinterpret_cast<const unsigned*>(&col_scale[tid * 4]);
+}
+
+// ---------------------------------------------------------------- reading --
+
+typedef float v2f __attribute__((ext_vector_type(2)));
+
+template <typename T>
+__global__ __launch_bounds__(kQBlock) void mx_dequant_kernel(MxDequantArgs a, unsigned units, unsigned per_row) {
+    const unsigned u = blockIdx.x * (kQBlock / 32) + threadIdx.x / 32;
+    if (u >= units) return;
+    const unsigned row = u / per_row, chunk = u % per_row;
+    const int64_t c = (int64_t)chunk * 256 + (threadIdx.x & 31) * 8, kp = (int64_t)per_row * 256;
+    const int64_t left = a.cols - c;
+    if (left <= 0) return;
+    const unsigned codes = *reinterpret_cast<const unsigned*>(a.codes + row * (kp / 2) + c / 2);
+    const unsigned b = a.scales[mx::scale_at(a.rows, row, c)];
+    const float s = mx::scale_value(b == 255u ? 0u : b);
+    float x[8];
+#define MX_PAIR(I)                                                                  \
+    {                                                                               \
+        const v2f v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, s, I);        \
+        x[2 * I] = v[0], x[2 * I + 1] = v[1];                                       \
+    }
+    MX_PAIR(0) MX_PAIR(1) MX_PAIR(2) MX_PAIR(3)
+#undef MX_PAIR
+    if (b == 255u) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(0x7fc00000u);
+    }
+    T* p = static_cast<T*>(a.out) + row * a.stride + c;
+    if constexpr (sizeof(T) == 2) {  // every value is exact in bf16
+        if (left >= 8) {
+            Unaligned<unsigned, 4, 2> w;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                w.v[i] = (__float_as_uint(x[2 * i]) >> 16) | (__float_as_uint(x[2 * i + 1]) & 0xffff0000u);
+            *reinterpret_cast<Unaligned<unsigned, 4, 2>*>(p) = w;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < left) p[i] = (unsigned short)(__float_as_uint(x[i]) >> 16);
+        }
+    } else {
+        if (left >= 8) {
+            Unaligned<float, 8, 4> w;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w.v[i] = x[i];
+            *reinterpret_cast<Unaligned<float, 8, 4>*>(p) = w;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < left) p[i] = x[i];
+        }
+    }
+}
+
+template <typename T, bool STOCHASTIC>
+hipError_t launch_quantize(const MxQuantArgs& a, hipStream_t s) {
+    if (!a.codes_t) {
+        const unsigned per_row = (unsigned)(mx_padded(a.cols) / 256), units = (unsigned)a.rows * per_row;
+        hipLaunchKernelGGL((mx_rows_kernel<T, STOCHASTIC>), dim3((units + kQBlock / 32 - 1) / (kQBlock / 32)),
+                           dim3(kQBlock), 0, s, a, units, per_row);
+        return hipGetLastError();
+    }
+    const unsigned tiles_c = (unsigned)(mx_padded(a.cols) / kTile);
+    const unsigned tiles = tiles_c * (unsigned)(mx_padded(a.rows) / kTile);
+    if (a.codes)
+        hipLaunchKernelGGL((mx_transpose_kernel<T, STOCHASTIC, true>), dim3(tiles), dim3(kQBlock), 0, s, a, tiles_c, tiles);
+    else
+        hipLaunchKernelGGL((mx_transpose_kernel<T, STOCHASTIC, false>), dim3(tiles), dim3(kQBlock), 0, s, a, tiles_c, tiles);
+    return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_mx_quantize(const MxQuantArgs& a, hipStream_t s) {
-    if (a.codes) {
-        const unsigned per_row = (unsigned)(mx_padded(a.cols) / 256);
-        const int64_t units = a.rows * per_row;
-        const dim3 grid((unsigned)((units + kQBlock / 32 - 1) / (kQBlock / 32)));
-        if (a.noise) hipLaunchKernelGGL(mx_rows_kernel<true>, grid, dim3(kQBlock), 0, s, a, units, per_row);
-        else hipLaunchKernelGGL(mx_rows_kernel<false>, grid, dim3(kQBlock), 0, s, a, units, per_row);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
-    if (a.codes_t) {
-        const unsigned row_tiles = (unsigned)(mx_padded(a.rows) / 256);
-        const dim3 grid(row_tiles * (unsigned)((a.cols + kTileCols - 1) / kTileCols));
-        if (a.noise) hipLaunchKernelGGL(mx_cols_kernel<true>, grid, dim3(kQBlock), 0, s, a, row_tiles);
-        else hipLaunchKernelGGL(mx_cols_kernel<false>, grid, dim3(kQBlock), 0, s, a, row_tiles);
-    }
-    return hipGetLastError();
+    if (a.bf16)
+        return a.noise ? launch_quantize<unsigned short, true>(a, s) : launch_quantize<unsigned short, false>(a, s);
+    return a.noise ? launch_quantize<float, true>(a, s) : launch_quantize<float, false>(a, s);
 }
 
 hipError_t launch_mx_dequantize(const MxDequantArgs& a, hipStream_t s) {
-    const unsigned per_row = (unsigned)(mx_padded(a.cols) / 256);
-    const int64_t units = a.rows * per_row;
-    const dim3 grid((unsigned)((units + kQBlock / 32 - 1) / (kQBlock / 32)));
-    hipLaunchKernelGGL(mx_dequant_kernel, grid, dim3(kQBlock), 0, s, a, units, per_row);
+    const unsigned per_row = (unsigned)(mx_padded(a.cols) / 256), units = (unsigned)a.rows * per_row;
+    const dim3 grid((units + kQBlock / 32 - 1) / (kQBlock / 32));
+    if (a.bf16) hipLaunchKernelGGL(mx_dequant_kernel<unsigned short>, grid, dim3(kQBlock), 0, s, a, units, per_row);
+    else hipLaunchKernelGGL(mx_dequant_kernel<float>, grid, dim3(kQBlock), 0, s, a, units, per_row);
     return hipGetLastError();
 }
 
