@@ -139,6 +139,22 @@ __device__ __forceinline__ const void* base_of(const ClipArgs& a, int i) {
     return a.table ? a.table[i] : a.ptr[i];
 }
 
+// Counts this thread's block in and returns the count before it.  The order
+// between a block's partial and the count, and between the count and what the
+// last block loads, needs no fences (which write back and invalidate an XCD's
+// L2) on gfx950: agent-scope stores write through, and vmcnt reaches 0 once
+// they have reached the level every XCD reads them from; the loads come after
+// a branch on the count, so after the atomic's reply, and go past the L2.
+#if defined(__HIP_DEVICE_COMPILE__) && !defined(__gfx950__)
+#error "the order that count_in relies on is argued for gfx950 only"
+#endif
+__device__ __forceinline__ unsigned count_in(unsigned* p) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    const unsigned before = __hip_atomic_fetch_add(p, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    asm volatile("" ::: "memory");
+    return before;
+}
+
 template <int KIND>
 __global__ __launch_bounds__(kClipBlock) void clip_norm_kernel(ClipArgs a) {
     __shared__ double sh[kWaves];
@@ -156,11 +172,11 @@ __global__ __launch_bounds__(kClipBlock) void clip_norm_kernel(ClipArgs a) {
         v = sh[0];
 #pragma unroll
         for (int w = 1; w < kWaves; ++w) v = combine<KIND>(v, sh[w]);
-        // The partial goes past the XCD's L2, and its store is complete
-        // before the count says so.
         __hip_atomic_store(&a.partials[blockIdx.x], v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        const unsigned n = __hip_atomic_fetch_add(a.done, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
-        sh_last = n + 1 == (unsigned)a.n_pieces;
+        const unsigned n = (unsigned)a.n_pieces, c = blockIdx.x % kClipCounters;
+        const unsigned mine = (n - c + kClipCounters - 1) / kClipCounters;  // blocks on this counter
+        sh_last = count_in(a.done + (c + 1) * kClipCounterStride) + 1 == mine &&
+                  count_in(a.done) + 1 == min(n, (unsigned)kClipCounters);
     }
     __syncthreads();
     if (!sh_last) return;
@@ -186,7 +202,7 @@ __global__ __launch_bounds__(kClipBlock) void clip_norm_kernel(ClipArgs a) {
             write_group<KIND>(a, g, s);
         }
     }
-    if (tid == 0) *a.done = 0u;
+    if (tid <= kClipCounters) a.done[tid * kClipCounterStride] = 0u;
 }
 
 template <typename TI, typename TO>

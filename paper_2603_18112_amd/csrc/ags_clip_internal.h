@@ -26,6 +26,13 @@ constexpr int kClipBlock = 256;
 constexpr int64_t kClipMinPiece = 8192;
 constexpr int64_t kClipPieces = 4096;
 
+// Blocks count themselves in on kClipCounters counters, each in a line of its
+// own, and the last on each of those on a root: with all blocks on one counter
+// the additions, some 14 ns each, took longer than the reads (MI355X, 25.6
+// million bf16 in 3251 pieces: 46.7 us).
+constexpr int kClipCounters = 64, kClipCounterStride = 64;  // dwords
+constexpr size_t kClipCounterBytes = (kClipCounters + 1) * kClipCounterStride * sizeof(unsigned);
+
 // Device pointers that travel in a kernel's arguments (a kernel takes at
 // most 4 KiB of them); larger sets go through a table in the workspace.
 constexpr int kClipArgPtrs = 440;
@@ -37,7 +44,7 @@ struct ClipArgs {
     const int32_t* group_begin;  // [n_groups + 1] piece ranges
     double* partials;            // [n_pieces]
     float2* coef;                // [n_groups] c_g as a product
-    unsigned* done;              // pieces finished, 0 between calls
+    unsigned* done;              // finished pieces' counters, 0 between calls
     float* norms;                // [n_groups], the caller's
     double max_norm, eps;
     int32_t n_in, n_groups, n_pieces;
