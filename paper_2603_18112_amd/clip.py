@@ -4,6 +4,7 @@ the HIP kernels of the library.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 from operator import attrgetter
 
@@ -94,12 +95,12 @@ def ags_clip_init(cfg, stream: int = 0):
 
 
 def ags_clip_norm(handle, d_in, d_norms: int, stream: int = 0):
-    """d_in: a ctypes array of device pointers."""
+    """d_in: host address of an array of device pointers (or a ctypes array)."""
     _check(_lib().ags_clip_norm(handle, d_in, d_norms, stream))
 
 
 def ags_clip_apply(handle, d_in, d_out, max_norm: float, d_norms: int, stream: int = 0):
-    """d_out: a ctypes array of device pointers, or None for in place."""
+    """d_in, d_out: as in ags_clip_norm; d_out None: in place."""
     _check(_lib().ags_clip_apply(handle, d_in, d_out, float(max_norm), d_norms, stream))
 
 
@@ -149,8 +150,6 @@ class GradClip:
                 raise ValueError(f"{base} out of range")
             if np.any((seg[off] + seg["numel"] > np.asarray(sizes)[seg[base]]) & (seg["numel"] > 0)):
                 raise ValueError(f"a segment ends past its tensor ({off})")
-        self._ptrs_in = ctypes.c_void_p * max(len(self.in_numels), 1)
-        self._ptrs_out = ctypes.c_void_p * max(len(self.out_numels), 1)
         self.device = torch.device("cuda", torch.cuda.current_device())
         self.handle = ags_clip_init(self.cfg, self._stream(stream))
 
@@ -202,7 +201,11 @@ class GradClip:
             stream = self.torch.cuda.current_stream(self.device)
         return int(stream.cuda_stream) if hasattr(stream, "cuda_stream") else int(stream)
 
-    def _pointers(self, what, tensors, numels, dtypes, array, longer=False):
+    def _pointers(self, what, tensors, numels, dtypes, longer=False):
+        """Host array of the tensors' addresses (the library checks that they
+        lie in device memory).  One pass of a C function over the list for each
+        property: written as a loop the checks of 161 tensors take longer than
+        the kernels."""
         T = self.torch.Tensor
         sizes = list(map(T.numel, tensors))
         if sizes != numels and not (longer and len(sizes) == len(numels)
@@ -210,9 +213,9 @@ class GradClip:
             raise ValueError(f"{what} differ in number or size from the handle's")
         if list(map(attrgetter("dtype"), tensors)) != dtypes:
             raise ValueError(f"{what} differ in type from the handle's")
-        if not all(map(T.is_contiguous, tensors)) or not all(map(attrgetter("is_cuda"), tensors)):
-            raise ValueError(f"{what} must be contiguous CUDA tensors")
-        return array(*map(T.data_ptr, tensors))
+        if not all(map(T.is_contiguous, tensors)):
+            raise ValueError(f"{what} must be contiguous")
+        return array.array("Q", map(T.data_ptr, tensors))
 
     def _norms(self, stream):
         t = self.torch
@@ -226,20 +229,20 @@ class GradClip:
 
     def norm(self, tensors, stream=None):
         """The norm of each group, fp32 [n_groups] on the device."""
-        p = self._pointers("the gradients", tensors, self.in_numels, self.in_dtypes, self._ptrs_in)
+        p = self._pointers("the gradients", tensors, self.in_numels, self.in_dtypes)
         norms = self._norms(stream)
-        ags_clip_norm(self.handle, p, norms.data_ptr(), self._stream(stream))
+        ags_clip_norm(self.handle, p.buffer_info()[0], norms.data_ptr(), self._stream(stream))
         return norms
 
     def clip(self, tensors, max_norm, out=None, stream=None):
         """Scale each group by min(1, max_norm / (norm + eps)), in place or
         into the tensors of `out`; returns the norms."""
-        p = self._pointers("the gradients", tensors, self.in_numels, self.in_dtypes, self._ptrs_in)
+        p = self._pointers("the gradients", tensors, self.in_numels, self.in_dtypes)
         q = None
         if out is not None:
-            q = self._pointers("the outputs", out, self.out_numels, self.out_dtypes, self._ptrs_out, True)
+            q = self._pointers("the outputs", out, self.out_numels, self.out_dtypes, True)
         norms = self._norms(stream)
-        ags_clip_apply(self.handle, p, q, max_norm, norms.data_ptr(), self._stream(stream))
+        ags_clip_apply(self.handle, p.buffer_info()[0], q and q.buffer_info()[0], max_norm, norms.data_ptr(), self._stream(stream))
         return norms
 
     def close(self):

@@ -91,19 +91,24 @@ __device__ __forceinline__ int head_elems(const T* p, int n) {
     return min(h, n);
 }
 
-template <int KIND, typename T>
-__device__ __forceinline__ double piece_sum(const T* p, int n) {
-    const int tid = threadIdx.x, head = head_elems(p, n);
+__device__ __forceinline__ const void* base_of(const ClipArgs& a, int i) {
+    return a.table ? a.table[i] : a.ptr[i];
+}
+
+// The sum over n elements by NT threads, this one's share.
+template <int KIND, int NT, typename T>
+__device__ __forceinline__ double piece_sum(const T* p, int n, int tid) {
+    const int head = head_elems(p, n);
     double acc = 0.0, acc2 = 0.0;
     if (tid < head) acc = accumulate<KIND>(acc, Load8<T>::one(p + tid));
     p += head;
     n -= head;
     const int groups = n / 8;
     int i = tid;
-    for (; i + 3 * kClipBlock < groups; i += 4 * kClipBlock) {
+    for (; i + 3 * NT < groups; i += 4 * NT) {
         float x[4][8];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) Load8<T>::get(p + (size_t)(i + u * kClipBlock) * 8, x[u]);
+        for (int u = 0; u < 4; ++u) Load8<T>::get(p + (size_t)(i + u * NT) * 8, x[u]);
 #pragma unroll
         for (int u = 0; u < 4; ++u)
 #pragma unroll
@@ -112,7 +117,7 @@ __device__ __forceinline__ double piece_sum(const T* p, int n) {
                 acc2 = accumulate<KIND>(acc2, x[u][j + 1]);
             }
     }
-    for (; i < groups; i += kClipBlock) {
+    for (; i < groups; i += NT) {
         float x[8];
         Load8<T>::get(p + (size_t)i * 8, x);
 #pragma unroll
@@ -121,6 +126,14 @@ __device__ __forceinline__ double piece_sum(const T* p, int n) {
     const int tail = groups * 8 + tid;
     if (tail < n) acc = accumulate<KIND>(acc, Load8<T>::one(p + tail));
     return combine<KIND>(acc, acc2);
+}
+
+template <int KIND, int NT>
+__device__ __forceinline__ double sum_of(const ClipArgs& a, const ClipPiece& pc, int tid) {
+    const void* base = base_of(a, pc.in_base);
+    return pc.in_dt == AGS_F32
+               ? piece_sum<KIND, NT>(static_cast<const float*>(base) + pc.in_off, pc.count, tid)
+               : piece_sum<KIND, NT>(static_cast<const unsigned short*>(base) + pc.in_off, pc.count, tid);
 }
 
 template <int KIND>
@@ -133,10 +146,6 @@ __device__ __forceinline__ void write_group(const ClipArgs& a, int g, double sum
     const bool tiny = r < 0x1p-100;
     a.coef[g] = r >= 1.0 ? make_float2(1.0f, 1.0f)
                          : make_float2((float)(tiny ? r * 0x1p100 : r), tiny ? 0x1p-100f : 1.0f);
-}
-
-__device__ __forceinline__ const void* base_of(const ClipArgs& a, int i) {
-    return a.table ? a.table[i] : a.ptr[i];
 }
 
 // Counts this thread's block in and returns the count before it.  The order
@@ -161,11 +170,7 @@ __global__ __launch_bounds__(kClipBlock) void clip_norm_kernel(ClipArgs a) {
     __shared__ int sh_last;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const ClipPiece pc = a.pieces[blockIdx.x];
-    const void* base = base_of(a, pc.in_base);
-    double v = pc.in_dt == AGS_F32
-                   ? piece_sum<KIND>(static_cast<const float*>(base) + pc.in_off, pc.count)
-                   : piece_sum<KIND>(static_cast<const unsigned short*>(base) + pc.in_off, pc.count);
-    v = wave_reduce<KIND>(v);
+    double v = wave_reduce<KIND>(sum_of<KIND, kClipBlock>(a, pc, tid));
     if (lane == 0) sh[wave] = v;
     __syncthreads();
     if (tid == 0) {
@@ -205,12 +210,12 @@ __global__ __launch_bounds__(kClipBlock) void clip_norm_kernel(ClipArgs a) {
     if (tid <= kClipCounters) a.done[tid * kClipCounterStride] = 0u;
 }
 
-template <typename TI, typename TO>
-__device__ __forceinline__ void piece_scale(const TI* in, TO* out, int n, float2 c) {
-    const int tid = threadIdx.x, head = head_elems(in, n);
+template <int NT, typename TI, typename TO>
+__device__ __forceinline__ void piece_scale(const TI* in, TO* out, int n, float2 c, int tid) {
+    const int head = head_elems(in, n);
     if ((reinterpret_cast<uintptr_t>(out + head) & 15u) != 0) {
         // the two sides' boundaries differ: element by element
-        for (int i = tid; i < n; i += kClipBlock) Load8<TO>::put_one(out + i, Load8<TI>::one(in + i) * c.x * c.y);
+        for (int i = tid; i < n; i += NT) Load8<TO>::put_one(out + i, Load8<TI>::one(in + i) * c.x * c.y);
         return;
     }
     if (tid < head) Load8<TO>::put_one(out + tid, Load8<TI>::one(in + tid) * c.x * c.y);
@@ -219,18 +224,18 @@ __device__ __forceinline__ void piece_scale(const TI* in, TO* out, int n, float2
     n -= head;
     const int groups = n / 8;
     int i = tid;
-    for (; i + kClipBlock < groups; i += 2 * kClipBlock) {
+    for (; i + NT < groups; i += 2 * NT) {
         float x[2][8];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) Load8<TI>::get(in + (size_t)(i + u * kClipBlock) * 8, x[u]);
+        for (int u = 0; u < 2; ++u) Load8<TI>::get(in + (size_t)(i + u * NT) * 8, x[u]);
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) x[u][j] = x[u][j] * c.x * c.y;
-            Load8<TO>::put(out + (size_t)(i + u * kClipBlock) * 8, x[u]);
+            Load8<TO>::put(out + (size_t)(i + u * NT) * 8, x[u]);
         }
     }
-    for (; i < groups; i += kClipBlock) {
+    for (; i < groups; i += NT) {
         float x[8];
         Load8<TI>::get(in + (size_t)i * 8, x);
 #pragma unroll
@@ -241,10 +246,8 @@ __device__ __forceinline__ void piece_scale(const TI* in, TO* out, int n, float2
     if (tail < n) Load8<TO>::put_one(out + tail, Load8<TI>::one(in + tail) * c.x * c.y);
 }
 
-__global__ __launch_bounds__(kClipBlock) void clip_scale_kernel(ClipArgs a) {
-    // Backwards: the norm's pass left its last pieces in the caches.
-    const ClipPiece pc = a.pieces[a.n_pieces - 1 - blockIdx.x];
-    const float2 c = a.coef[pc.group];
+template <int NT>
+__device__ __forceinline__ void scale_piece(const ClipArgs& a, const ClipPiece& pc, float2 c, int tid) {
     if (a.in_place && c.x == 1.0f && c.y == 1.0f) return;
     const void* in = base_of(a, pc.in_base);
     void* out = const_cast<void*>(a.in_place ? in : base_of(a, a.n_in + pc.out_base));
@@ -252,12 +255,43 @@ __global__ __launch_bounds__(kClipBlock) void clip_scale_kernel(ClipArgs a) {
     const int odt = a.in_place ? pc.in_dt : pc.out_dt;
     if (pc.in_dt == AGS_F32) {
         const float* p = static_cast<const float*>(in) + pc.in_off;
-        if (odt == AGS_F32) piece_scale(p, static_cast<float*>(out) + oo, pc.count, c);
-        else piece_scale(p, static_cast<unsigned short*>(out) + oo, pc.count, c);
+        if (odt == AGS_F32) piece_scale<NT>(p, static_cast<float*>(out) + oo, pc.count, c, tid);
+        else piece_scale<NT>(p, static_cast<unsigned short*>(out) + oo, pc.count, c, tid);
     } else {
         const unsigned short* p = static_cast<const unsigned short*>(in) + pc.in_off;
-        if (odt == AGS_F32) piece_scale(p, static_cast<float*>(out) + oo, pc.count, c);
-        else piece_scale(p, static_cast<unsigned short*>(out) + oo, pc.count, c);
+        if (odt == AGS_F32) piece_scale<NT>(p, static_cast<float*>(out) + oo, pc.count, c, tid);
+        else piece_scale<NT>(p, static_cast<unsigned short*>(out) + oo, pc.count, c, tid);
+    }
+}
+
+__global__ __launch_bounds__(kClipBlock) void clip_scale_kernel(ClipArgs a) {
+    // Backwards: the norm's pass left its last pieces in the caches.
+    const ClipPiece pc = a.pieces[a.n_pieces - 1 - blockIdx.x];
+    scale_piece<kClipBlock>(a, pc, a.coef[pc.group], threadIdx.x);
+}
+
+// Both passes over a small set in one block, a wave to a piece.
+template <int KIND>
+__global__ __launch_bounds__(1024) void clip_small_kernel(ClipArgs a, int scale) {
+    __shared__ double sums[kClipSmallPieces];
+    constexpr int kW = 16;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    for (int i = wave; i < a.n_pieces; i += kW) {
+        const double v = wave_reduce<KIND>(sum_of<KIND, 64>(a, a.pieces[i], lane));
+        if (lane == 0) sums[i] = v;
+    }
+    __syncthreads();
+    for (int g = wave; g < a.n_groups; g += kW) {
+        double s = 0.0;
+        for (int i = a.group_begin[g] + lane; i < a.group_begin[g + 1]; i += 64) s = combine<KIND>(s, sums[i]);
+        s = wave_reduce<KIND>(s);
+        if (lane == 0) write_group<KIND>(a, g, s);
+    }
+    if (!scale) return;
+    __syncthreads();
+    for (int i = wave; i < a.n_pieces; i += kW) {
+        const ClipPiece pc = a.pieces[i];
+        scale_piece<64>(a, pc, a.coef[pc.group], lane);
     }
 }
 
@@ -278,6 +312,17 @@ hipError_t launch_clip_norm(const ClipArgs& a, int kind, hipStream_t s) {
         case AGS_CLIP_L2: hipLaunchKernelGGL(clip_norm_kernel<AGS_CLIP_L2>, grid, block, 0, s, a); break;
         case AGS_CLIP_L1: hipLaunchKernelGGL(clip_norm_kernel<AGS_CLIP_L1>, grid, block, 0, s, a); break;
         default: hipLaunchKernelGGL(clip_norm_kernel<AGS_CLIP_MAX>, grid, block, 0, s, a); break;
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_clip_small(const ClipArgs& a, int kind, bool scale, hipStream_t s) {
+    const dim3 grid(1), block(1024);
+    const int sc = scale ? 1 : 0;
+    switch (kind) {
+        case AGS_CLIP_L2: hipLaunchKernelGGL(clip_small_kernel<AGS_CLIP_L2>, grid, block, 0, s, a, sc); break;
+        case AGS_CLIP_L1: hipLaunchKernelGGL(clip_small_kernel<AGS_CLIP_L1>, grid, block, 0, s, a, sc); break;
+        default: hipLaunchKernelGGL(clip_small_kernel<AGS_CLIP_MAX>, grid, block, 0, s, a, sc); break;
     }
     return hipGetLastError();
 }

@@ -26,6 +26,10 @@ constexpr int kClipBlock = 256;
 constexpr int64_t kClipMinPiece = 8192;
 constexpr int64_t kClipPieces = 4096;
 
+// A set this small goes through one block in one launch.
+constexpr int64_t kClipSmallElems = 32768;
+constexpr int kClipSmallPieces = 128;
+
 // Blocks count themselves in on kClipCounters counters, each in a line of its
 // own, and the last on each of those on a root: with all blocks on one counter
 // the additions, some 14 ns each, took longer than the reads (MI355X, 25.6
@@ -62,6 +66,7 @@ struct ClipTableArgs {
 // the host code alone (a sanitizer build) links; a launch there is an error.
 __attribute__((weak)) hipError_t launch_clip_table(const ClipTableArgs&, hipStream_t);
 __attribute__((weak)) hipError_t launch_clip_norm(const ClipArgs&, int kind, hipStream_t);
+__attribute__((weak)) hipError_t launch_clip_small(const ClipArgs&, int kind, bool scale, hipStream_t);
 __attribute__((weak)) hipError_t launch_clip_scale(const ClipArgs&, hipStream_t);
 
 }  // namespace ags

@@ -295,7 +295,7 @@ def test_refusals():
     h = clip.GradClip.for_tensors(g)
     for bad in ([g[0]], [g[1], g[0]], [g[0], g[0]], [g[0], g[1].float()], [g[0].cpu(), g[1]],
                 [torch.zeros(200, device="cuda")[::2], g[1]]):
-        with pytest.raises(ValueError):
+        with pytest.raises((ValueError, ags.AGSError)):
             h.norm(bad)
     for bound in (0.0, -1.0, float("nan"), float("inf")):
         with pytest.raises(ags.AGSError) as e:
