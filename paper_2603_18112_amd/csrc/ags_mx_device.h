@@ -79,5 +79,35 @@ __device__ __forceinline__ unsigned codes_stochastic(const float* x, unsigned by
 
 __device__ __forceinline__ unsigned magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 
+template <typename T, int N, int ALIGN>
+struct __attribute__((packed, aligned(ALIGN))) Unaligned {
+    T v[N];
+};
+
+// 8 elements as fp32 from p; `left` of them lie inside the row, the rest read
+// as zero.
+__device__ __forceinline__ void load8(const unsigned short* p, int64_t left, float* x) {
+    if (left >= 8) {
+        const auto w = *reinterpret_cast<const Unaligned<unsigned, 4, 2>*>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = __uint_as_float(w.v[i] << 16);
+            x[2 * i + 1] = __uint_as_float(w.v[i] & 0xffff0000u);
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = i < left ? __uint_as_float((unsigned)p[i] << 16) : 0.0f;
+}
+__device__ __forceinline__ void load8(const float* p, int64_t left, float* x) {
+    if (left >= 8) {
+        const auto w = *reinterpret_cast<const Unaligned<float, 8, 4>*>(p);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = w.v[i];
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = i < left ? p[i] : 0.0f;
+}
 }  // namespace mx
 }  // namespace ags

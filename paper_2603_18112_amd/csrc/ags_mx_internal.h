@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <cmath>
 
 #include "ags_mx.h"
 
@@ -44,23 +45,65 @@ struct MxProductArgs {
 };
 
 // How a product is cut into blocks: tiles of 64 * tm x 64 * tn outputs, the
-// contracted axis into `splits` parts.
+// contracted axis into `splits` parts; or few: the kernel for few rows of a.
 struct MxShape {
-    int32_t tm, tn, splits;
+    int32_t tm, tn, splits, few;
 };
+
+// The kernel for few rows reads x's codes from the caches once for each 16 rows
+// of w, so beyond 16 rows it is for small products only: 32 rows 4096 x 4096
+// 9.8 us against 14.3 in tiles of 64 x 64 (which need a second launch to join
+// the parts), 24 rows 4096 x 25088 19.5 against 16.6, 32 rows 16384 x 16384
+// 50.7 against some 38.
+inline bool mx_few(int64_t m, int64_t n, int64_t kp) { return m <= 16 || (m <= 32 && n * kp <= ((int64_t)1 << 26)); }
+
+// Does ags_mx_linear take x to 4 bits in the product's kernel?  Every block
+// does so then; it keeps x in LDS.
+inline bool mx_linear_fused(int64_t rows, int64_t k) { return rows <= 16 && rows * k <= 16384; }
+
+
+// The tile and the split with the least estimated time in us.  A stage (256
+// columns) of a tile of 64, 128 or 256 squared takes 0.55, 0.68 or 1.35 on an
+// idle CU (1.9 with all CUs at work, at the clock the power limit leaves);
+// four small tiles on a CU take twice as long as one, two of the middle ones
+// as long as one after the other; prologue and epilogue 2, 3 or 5; a split
+// costs the launch that joins the parts (5) and their bytes at 4 TB/s.
+// Measured against every shape and split (bf16 results, us): 64 x 4096 x 4096
+// small 10.2, middle 12.7, in two parts 14.4; 64 x 16384 x 16384 small 38.2, in
+// two parts 29.3, in three 30.4; 256 x 4096 x 25088 small 53.4, middle in four
+// parts 30.3, large in eight 36.0; 1024 x 4096 x 4096 small 18.4, middle 16.1,
+// large 25.0; 2048 x 4096 x 4096 32.5, 24.7, 28.6; 100 x 500 x 20000 small 26.7,
+// in six parts 14.7.  256 x 128 tiles were not the fastest anywhere by more
+// than a twentieth.
 inline MxShape mx_product_plan(int64_t m, int64_t n, int64_t kp) {
-    MxShape p{1, 1, 1};
-    auto tiles = [&](int64_t tm, int64_t tn) { return ((m + 64 * tm - 1) / (64 * tm)) * ((n + 64 * tn - 1) / (64 * tn)); };
-    if (tiles(4, 4) >= 192) p.tm = p.tn = 4;
-    else if (tiles(2, 2) >= 192) p.tm = p.tn = 2;
-    const int64_t t = tiles(p.tm, p.tn), stages = kp / 256;
-    if (t < 256) p.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(512 / t, stages / 4));
-    return p;
+    if (mx_few(m, n, kp)) return MxShape{1, 1, 1, 1};
+    MxShape best{1, 1, 1, 0};
+    double least = 1e30;
+    const double stages = (double)(kp / 256);
+    for (int t = 1; t <= 4; t *= 2) {
+        const double tiles = (double)((m + 64 * t - 1) / (64 * t)) * (double)((n + 64 * t - 1) / (64 * t));
+        for (int s : {1, 2, 3, 4, 6, 8, 12, 16}) {
+            if (s > 1 && stages < 4 * s) break;
+            const double load = tiles * s / 256;  // blocks of a CU
+            double us = stages / s;
+            if (t == 1) us = us * 0.55 * std::max(1.0, 0.5 * load) + 2 * std::max(1.0, load / 4);
+            else if (t == 2) us = us * 0.68 * std::max(1.0, load) + 3 * std::max(1.0, load / 2);
+            else us = (us * (load > 0.75 ? 1.9 : 1.35) + 5) * std::max(1.0, std::ceil(load));
+            if (s > 1) us += 5 + 8e-6 * (double)m * (double)n / 4 * s;
+            if (us < least) {
+                least = us;
+                best = MxShape{t, t, s, 0};
+            }
+        }
+    }
+    return best;
 }
 
 // Weak for the same reason as the clipping launchers.
 __attribute__((weak)) hipError_t launch_mx_quantize(const MxQuantArgs&, hipStream_t);
 __attribute__((weak)) hipError_t launch_mx_dequantize(const MxDequantArgs&, hipStream_t);
 __attribute__((weak)) hipError_t launch_mx_product(const MxProductArgs&, hipStream_t);
+__attribute__((weak)) hipError_t launch_mx_linear(const MxProductArgs&, const void* x, bool bf16, int64_t stride,
+                                                  int64_t k, hipStream_t);
 
 }  // namespace ags

@@ -4,6 +4,8 @@
 //                   256 elements of the contracted axis go from memory straight
 //                   into LDS while the matrix cores work on the stage before.
 // mx_join_kernel    adds the partial sums of a contracted axis cut in parts.
+// mx_few_kernel     few rows (tokens): a block of sixteen waves takes 16 rows
+//                   of the weights, the waves share the contracted axis.
 #include <algorithm>
 #include <type_traits>
 
@@ -20,6 +22,7 @@ namespace ags {
 namespace {
 
 typedef int v8i __attribute__((ext_vector_type(8)));
+typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 
 constexpr int kFp4 = 4;  // operand format of the scaled matrix instruction
@@ -45,15 +48,11 @@ struct Out {
     char* p;
     int64_t stride;
     bool bf16, add;
-    bool wide, wide16;  // rows start where 4 elements, or 16 bytes, are one aligned store
 };
 
 __device__ __forceinline__ Out output_of(const MxProductArgs& a, unsigned split) {
-    Out o{static_cast<char*>(a.out), a.stride, a.bf16 != 0, a.accumulate != 0, false, false};
-    if (a.splits > 1) o = Out{reinterpret_cast<char*>(a.partials + (int64_t)split * a.m * a.n), a.n, false, false, false, false};
-    const unsigned low = (unsigned)reinterpret_cast<uintptr_t>(o.p) | ((unsigned)o.stride * (o.bf16 ? 2u : 4u));
-    o.wide = (low & (o.bf16 ? 7u : 15u)) == 0;
-    o.wide16 = (low & 15u) == 0;
+    Out o{static_cast<char*>(a.out), a.stride, a.bf16 != 0, a.accumulate != 0};
+    if (a.splits > 1) o = Out{reinterpret_cast<char*>(a.partials + (int64_t)split * a.m * a.n), a.n, false, false};
     return o;
 }
 
@@ -70,25 +69,6 @@ __device__ __forceinline__ void store1(const Out& o, int64_t at, float v) {
 // Four results of a row from column j, as many as lie before column n.
 __device__ __forceinline__ void store4(const Out& o, int64_t i, int64_t j, float4 v, int64_t n) {
     const int64_t at = i * o.stride + j;
-    if (o.wide && j + 4 <= n) {
-        if (o.bf16) {
-            uint2* p = reinterpret_cast<uint2*>(o.p + at * 2);
-            if (o.add) {
-                const uint2 u = *p;
-                v.x += __uint_as_float(u.x << 16), v.y += __uint_as_float(u.x & 0xffff0000u);
-                v.z += __uint_as_float(u.y << 16), v.w += __uint_as_float(u.y & 0xffff0000u);
-            }
-            *p = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
-        } else {
-            float4* p = reinterpret_cast<float4*>(o.p + at * 4);
-            if (o.add) {
-                const float4 u = *p;
-                v.x += u.x, v.y += u.y, v.z += u.z, v.w += u.w;
-            }
-            *p = v;
-        }
-        return;
-    }
     const float e[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
     for (int t = 0; t < 4; ++t)
@@ -137,26 +117,51 @@ __device__ __forceinline__ void block_barrier() {
 }
 
 // TM x TN: the tile in units of 64; four waves, two by two.
-// 32 rows of BYTES bytes from LDS (PITCH apart) to memory, all inside the output.
-template <int BYTES, int PITCH>
-__device__ __forceinline__ void store_strip(const char* strip, int lane, char* to, int64_t stride) {
-    constexpr int kLanes = BYTES / 16, kRows = 64 / kLanes;  // lanes of a row, rows of a store
+// 32 rows of BYTES bytes from LDS (PITCH apart) to memory, those of the first
+// `rows` rows and `bytes` bytes.  T: the elements, whose alignment is all that
+// the 16-byte accesses to memory need.
+template <typename T, int BYTES, int PITCH, bool ADD>
+__device__ __forceinline__ void store_strip(const char* strip, int lane, char* to, int64_t stride, int64_t rows,
+                                            int64_t bytes) {
+    constexpr int kLanes = BYTES / 16, kRows = 64 / kLanes, kN = 16 / sizeof(T);  // lanes of a row, rows of a store
+    typedef mx::Unaligned<T, kN, sizeof(T)> Piece;
     const int c = (lane % kLanes) * 16, t0 = lane / kLanes;
+    if (c >= bytes) return;
+    const bool all = c + 16 <= bytes;
     strip += t0 * PITCH + c;
     to += t0 * stride + c;
 #pragma unroll
-    for (int t = 0; t < 32; t += kRows)
-        *reinterpret_cast<uint4*>(to + t * stride) = *reinterpret_cast<const uint4*>(strip + t * PITCH);
+    for (int t = 0; t < 32; t += kRows) {
+        if (t0 + t >= rows) continue;
+        const uint4 raw = *reinterpret_cast<const uint4*>(strip + t * PITCH);
+        Piece v = __builtin_bit_cast(Piece, raw);
+        char* p = to + t * stride;
+        if (all) {
+            if constexpr (ADD) {
+                const Piece u = *reinterpret_cast<const Piece*>(p);
+#pragma unroll
+                for (int i = 0; i < kN; ++i) v.v[i] += u.v[i];
+            }
+            *reinterpret_cast<Piece*>(p) = v;
+        } else {
+#pragma unroll
+            for (int i = 0; i < kN; ++i) {
+                T* e = reinterpret_cast<T*>(p) + i;
+                if (c + (i + 1) * (int)sizeof(T) > bytes) continue;
+                if constexpr (ADD) v.v[i] += *e;
+                *e = v.v[i];
+            }
+        }
+    }
 }
 
-// 32 rows of WIDE fp32 results where rows or columns end inside, or results
-// are added.
+// 32 rows of WIDE fp32 results added to bf16.
 template <int WIDE, int PITCH>
-__device__ __forceinline__ void store_edge(const Out& o, const char* strip, int lane, int64_t row0, int64_t col0,
+__device__ __forceinline__ void store_added(const Out& o, const char* strip, int lane, int64_t row0, int64_t col0,
                                            int64_t m, int64_t n) {
     constexpr int kLanes = WIDE / 4, kRows = 64 / kLanes;
     const int c = (lane % kLanes) * 4;
-#pragma unroll 1
+#pragma unroll 2
     for (int t = lane / kLanes; t < 32; t += kRows) {
         const float4 v = *reinterpret_cast<const float4*>(strip + t * PITCH + c * 4);
         if (row0 + t < m && col0 + c < n) store4(o, row0 + t, col0 + c, v, n);
@@ -341,11 +346,11 @@ __device__ __forceinline__ void tile_product(const MxProductArgs& a, unsigned ti
     constexpr int kWide = BN / 2;
     char* strip = sm + w * 32 * (kWide * 4 + 16);
     const Out o = output_of(a, split);
-    const bool whole = o.wide16 && !o.add && i0 + BM <= a.m && j0 + BN <= a.n;
 #pragma unroll
     for (int x = 0; x < FM; ++x) {
         const int64_t row0 = i0 + wm * (BM / 2) + x * 32, col0 = j0 + wn * kWide;
-        if (whole && o.bf16) {
+        const int64_t rows = a.m - row0, cols = a.n - col0;
+        if (o.bf16 && !o.add) {
             constexpr int kPitch = kWide * 2 + 16;
 #pragma unroll
             for (int y = 0; y < FN; ++y)
@@ -356,7 +361,8 @@ __device__ __forceinline__ void tile_product(const MxProductArgs& a, unsigned ti
                         make_uint2(pack_bf16(v[4 * g], v[4 * g + 1]), pack_bf16(v[4 * g + 2], v[4 * g + 3]));
                 }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            store_strip<kWide * 2, kPitch>(strip, lane, o.p + (row0 * o.stride + col0) * 2, o.stride * 2);
+            store_strip<unsigned short, kWide * 2, kPitch, false>(
+                strip, lane, o.p + (row0 * o.stride + col0) * 2, o.stride * 2, rows, cols * 2);
         } else {
             constexpr int kPitch = kWide * 4 + 16;
 #pragma unroll
@@ -368,8 +374,12 @@ __device__ __forceinline__ void tile_product(const MxProductArgs& a, unsigned ti
                         make_float4(v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]);
                 }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            if (whole) store_strip<kWide * 4, kPitch>(strip, lane, o.p + (row0 * o.stride + col0) * 4, o.stride * 4);
-            else store_edge<kWide, kPitch>(o, strip, lane, row0, col0, a.m, a.n);
+            char* to = o.p + (row0 * o.stride + col0) * 4;
+            if (!o.bf16 && o.add)
+                store_strip<float, kWide * 4, kPitch, true>(strip, lane, to, o.stride * 4, rows, cols * 4);
+            else if (!o.bf16)
+                store_strip<float, kWide * 4, kPitch, false>(strip, lane, to, o.stride * 4, rows, cols * 4);
+            else store_added<kWide, kPitch>(o, strip, lane, row0, col0, a.m, a.n);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
@@ -382,12 +392,140 @@ __global__ __launch_bounds__(256, 1) void mx_tile_kernel(MxProductArgs a, unsign
 
 __global__ __launch_bounds__(256) void mx_join_kernel(MxProductArgs a) {
     const int64_t total = a.m * a.n;
-    const Out o{static_cast<char*>(a.out), a.stride, a.bf16 != 0, a.accumulate != 0, false, false};
+    const Out o{static_cast<char*>(a.out), a.stride, a.bf16 != 0, a.accumulate != 0};
     for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < total; t += (int64_t)gridDim.x * 256) {
         float v = 0.0f;
         for (int s = 0; s < a.splits; ++s) v += a.partials[s * total + t];
         store1(o, t / a.n * a.stride + t % a.n, v);
     }
+}
+
+// ------------------------------------------------------------- few rows --
+
+// Up to 16 * MT rows of x against all of w: every weight is read once, straight
+// into registers, so the kernel is bound by the weights' bytes.  A block takes
+// 16 rows of w; of each 16 chunks of 256 columns a wave takes one; the waves'
+// sums meet in LDS, in a fixed order.  T: x's type where the block takes up to
+// 16 rows of x to 4 bits itself (each block anew: one launch instead of two,
+// for few elements of x), or void where x is stored already.
+constexpr int kFewWaves = 16;
+
+struct FewX {
+    const void* x;  // x, or its codes
+    const uint8_t* scales;
+    int64_t stride;  // of x
+    int64_t k;
+};
+
+// The codes of 32 elements of x, columns past the end zero; returns the scale.
+template <typename T>
+__device__ __forceinline__ unsigned store32(const T* p, int64_t left, uint4* codes) {
+    float x[4][8];
+    unsigned m = 0;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        mx::load8(p + 8 * g, left - 8 * g, x[g]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = max(m, mx::magnitude(x[g][i]));
+    }
+    const unsigned b = mx::scale_byte<false>(m);
+    *codes = make_uint4(mx::codes_nearest(x[0], b), mx::codes_nearest(x[1], b), mx::codes_nearest(x[2], b),
+                        mx::codes_nearest(x[3], b));
+    if (b == 255u) *codes = make_uint4(0u, 0u, 0u, 0u);
+    return b;
+}
+
+// One chunk of a wave is in flight at a time: with four, for which one block
+// fits a CU instead of two, 1 row took 30 us instead of 26 (16384 x 16384).
+template <int MT, typename T>
+__device__ __forceinline__ void few_rows(const MxProductArgs& a, const FewX& fx) {
+    constexpr bool kStore = !std::is_void<T>::value;
+    // x's codes, [chunk][row][128] with pieces permuted as in the tile kernel,
+    // and its scales, [chunk][row][8].
+    extern __shared__ char sm[];
+    __shared__ float red[kFewWaves][MT][4][64];
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, r = lane & 15, q = lane >> 4;
+    const int m = (int)a.m, chunks = (int)(a.kp / 256);
+    uint8_t *const xs = reinterpret_cast<uint8_t*>(sm), *const xe = xs + chunks * m * 128;
+    if constexpr (kStore) {
+        const int blocks = chunks * 8;  // of a row
+        for (int b = tid; b < blocks * m; b += kFewWaves * 64) {
+            const int xr = b / blocks, blk = b % blocks, at = (blk >> 3) * m + xr;
+            const int64_t col = (int64_t)blk * 32;
+            uint4 codes;
+            const unsigned e = store32(static_cast<const T*>(fx.x) + xr * fx.stride + col, fx.k - col, &codes);
+            *reinterpret_cast<uint4*>(&xs[at * 128 + (((blk & 7) ^ ((xr >> 1) & 7)) << 4)]) = codes;
+            xe[at * 8 + (blk & 7)] = (uint8_t)e;
+        }
+        __syncthreads();
+    }
+    // Lane l holds row r = l % 16 of both operands; it takes the pieces 2 q and
+    // 2 q + 1 of a chunk, q = l / 16, so that their scales are neighbours.
+    const int64_t n0 = (int64_t)blockIdx.x * 16, row = min(n0 + r, a.n - 1), pitch = a.kp / 2;
+    const uint8_t* pw = a.b + row * pitch + q * 32;
+    const int64_t pb = mx_scale_rows(a.n) * 8, pa = mx_scale_rows(a.m) * 8;
+    const uint8_t* pe = a.sb + row * 8 + q * 2;
+    v4f acc[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) acc[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int c = w; c < chunks; c += kFewWaves) {
+        const uint4 w0 = *reinterpret_cast<const uint4*>(pw + (int64_t)c * 128);
+        const uint4 w1 = *reinterpret_cast<const uint4*>(pw + (int64_t)c * 128 + 16);
+        const int we = *reinterpret_cast<const uint16_t*>(pe + c * pb);
+        uint4 xv[MT][2] = {};
+        int xw[MT] = {};
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            const int xr = t * 16 + r;
+            if (xr >= m) continue;  // rows past the end multiply zeros
+            if constexpr (kStore) {
+                const int at = c * m + xr;
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    xv[t][j] = *reinterpret_cast<const uint4*>(&xs[at * 128 + (((q * 2 + j) ^ ((xr >> 1) & 7)) << 4)]);
+                xw[t] = *reinterpret_cast<const uint16_t*>(&xe[at * 8 + q * 2]);
+            } else {
+                const uint8_t* p = static_cast<const uint8_t*>(fx.x) + xr * pitch + (int64_t)c * 128 + q * 32;
+                xv[t][0] = *reinterpret_cast<const uint4*>(p);
+                xv[t][1] = *reinterpret_cast<const uint4*>(p + 16);
+                xw[t] = *reinterpret_cast<const uint16_t*>(fx.scales + c * pa + xr * 8 + q * 2);
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(w0), operand(xv[t][0]), acc[t], kFp4, kFp4, 0,
+                                                                      we, 0, xw[t]);
+            acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(w1), operand(xv[t][1]), acc[t], kFp4, kFp4, 1,
+                                                                      we, 1, xw[t]);
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) red[w][t][i][lane] = acc[t][i];
+    __syncthreads();
+    // Element (t, i, l): row 16 t + l % 16 of x, column 4 (l / 16) + i.
+    const Out o = output_of(a, 0);
+    for (int e = tid; e < MT * 256; e += kFewWaves * 64) {
+        const int t = e >> 8, l = (e >> 2) & 63, i = e & 3;
+        float v = 0.0f;
+#pragma unroll
+        for (int k = 0; k < kFewWaves; ++k) v += red[k][t][i][l];
+        const int64_t xr = t * 16 + (l & 15), col = n0 + (l >> 4) * 4 + i;
+        if (xr < a.m && col < a.n) store1(o, xr * o.stride + col, v);
+    }
+}
+
+template <int MT, typename T>
+__global__ __launch_bounds__(kFewWaves * 64) void mx_few_kernel(MxProductArgs a, FewX x) {
+    few_rows<MT, T>(a, x);
+}
+
+hipError_t launch_few(const MxProductArgs& a, const FewX& x, hipStream_t s) {
+    const dim3 grid((unsigned)((a.n + 15) / 16)), block(kFewWaves * 64);
+    if (a.m <= 16) hipLaunchKernelGGL((mx_few_kernel<1, void>), grid, block, 0, s, a, x);
+    else hipLaunchKernelGGL((mx_few_kernel<2, void>), grid, block, 0, s, a, x);
+    return hipGetLastError();
 }
 
 template <int TM, int TN>
@@ -409,6 +547,7 @@ hipError_t launch_mx_product(const MxProductArgs& args, hipStream_t s) {
     MxProductArgs a = args;
     const MxShape p = mx_product_plan(a.m, a.n, a.kp);
     a.splits = p.splits;
+    if (p.few) return launch_few(a, FewX{a.a, a.sa, 0, 0}, s);
     hipError_t e = p.tm == 4 ? launch_tile<4, 4>(a, s) : p.tm == 2 ? launch_tile<2, 2>(a, s) : launch_tile<1, 1>(a, s);
     if (e == hipSuccess && a.splits > 1) {
         const unsigned blocks = (unsigned)std::min<int64_t>((a.m * a.n + 255) / 256, 4096);
@@ -416,6 +555,15 @@ hipError_t launch_mx_product(const MxProductArgs& args, hipStream_t s) {
         e = hipGetLastError();
     }
     return e;
+}
+
+hipError_t launch_mx_linear(const MxProductArgs& a, const void* x, bool bf16, int64_t stride, int64_t k, hipStream_t s) {
+    const FewX f{x, nullptr, stride, k};
+    const dim3 grid((unsigned)((a.n + 15) / 16)), block(kFewWaves * 64);
+    const unsigned lds = (unsigned)(a.kp / 256 * a.m * 136);
+    if (bf16) hipLaunchKernelGGL((mx_few_kernel<1, unsigned short>), grid, block, lds, s, a, f);
+    else hipLaunchKernelGGL((mx_few_kernel<1, float>), grid, block, lds, s, a, f);
+    return hipGetLastError();
 }
 
 }  // namespace ags

@@ -19,39 +19,9 @@ namespace {
 constexpr int kQBlock = 256;
 constexpr int kXcds = 8;
 
-template <typename T, int N, int ALIGN>
-struct __attribute__((packed, aligned(ALIGN))) Unaligned {
-    T v[N];
-};
-
-// 8 elements as fp32 from p; `left` of them lie inside the row, the rest read
-// as zero.
-__device__ __forceinline__ void load8(const unsigned short* p, int64_t left, float* x) {
-    if (left >= 8) {
-        const auto w = *reinterpret_cast<const Unaligned<unsigned, 4, 2>*>(p);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[2 * i] = __uint_as_float(w.v[i] << 16);
-            x[2 * i + 1] = __uint_as_float(w.v[i] & 0xffff0000u);
-        }
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = i < left ? __uint_as_float((unsigned)p[i] << 16) : 0.0f;
-}
-__device__ __forceinline__ void load8(const float* p, int64_t left, float* x) {
-    if (left >= 8) {
-        const auto w = *reinterpret_cast<const Unaligned<float, 8, 4>*>(p);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = w.v[i];
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = i < left ? p[i] : 0.0f;
-}
 __device__ __forceinline__ void load_noise8(const uint8_t* p, int64_t left, unsigned* r) {
     if (left >= 8) {
-        const auto w = *reinterpret_cast<const Unaligned<unsigned, 2, 1>*>(p);
+        const auto w = *reinterpret_cast<const mx::Unaligned<unsigned, 2, 1>*>(p);
         r[0] = w.v[0], r[1] = w.v[1];
         return;
     }
@@ -93,7 +63,7 @@ __global__ __launch_bounds__(kQBlock) void mx_rows_kernel(MxQuantArgs a, unsigne
     const int lane = threadIdx.x & 31;
     const int64_t c = (int64_t)chunk * 256 + lane * 8;
     float x[8];
-    load8(static_cast<const T*>(a.x) + row * a.stride + c, a.cols - c, x);
+    mx::load8(static_cast<const T*>(a.x) + row * a.stride + c, a.cols - c, x);
     unsigned w[2], r[8];
     if (STOCHASTIC) {
         load_noise8(a.noise + row * a.noise_stride + c, a.cols - c, w);
@@ -190,7 +160,7 @@ __global__ __launch_bounds__(kQBlock) void mx_transpose_kernel(MxQuantArgs a, un
         for (int i = 0; i < kAhead; ++i) {
             const int64_t row = r0 + (i0 + i) * 16 + (tid >> 4);
             const int64_t l = row < a.rows ? left : 0;
-            load8(px + row * a.stride, l, x[i]);
+            mx::load8(px + row * a.stride, l, x[i]);
             if (STOCHASTIC) load_noise8(pn + row * a.noise_stride, l, r[i]);
         }
 #pragma unroll
@@ -307,11 +277,11 @@ __global__ __launch_bounds__(kQBlock) void mx_dequant_kernel(MxDequantArgs a, un
     T* p = static_cast<T*>(a.out) + row * a.stride + c;
     if constexpr (sizeof(T) == 2) {  // every value is exact in bf16
         if (left >= 8) {
-            Unaligned<unsigned, 4, 2> w;
+            mx::Unaligned<unsigned, 4, 2> w;
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 w.v[i] = (__float_as_uint(x[2 * i]) >> 16) | (__float_as_uint(x[2 * i + 1]) & 0xffff0000u);
-            *reinterpret_cast<Unaligned<unsigned, 4, 2>*>(p) = w;
+            *reinterpret_cast<mx::Unaligned<unsigned, 4, 2>*>(p) = w;
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
@@ -319,10 +289,10 @@ __global__ __launch_bounds__(kQBlock) void mx_dequant_kernel(MxDequantArgs a, un
         }
     } else {
         if (left >= 8) {
-            Unaligned<float, 8, 4> w;
+            mx::Unaligned<float, 8, 4> w;
 #pragma unroll
             for (int i = 0; i < 8; ++i) w.v[i] = x[i];
-            *reinterpret_cast<Unaligned<float, 8, 4>*>(p) = w;
+            *reinterpret_cast<mx::Unaligned<float, 8, 4>*>(p) = w;
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i)

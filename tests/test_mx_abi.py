@@ -97,11 +97,12 @@ def test_product_and_linear_refuse(lib):
     _raises(ags.AGS_E_ALIGN, p, a, b, X + 1, bf, 8)
     _raises(ags.AGS_E_LAYOUT, p, _t(1 << 20, 64, Y, Z), _t(1 << 20, 64, V, W), X, bf, 1 << 20)
     lin = mx.ags_mx_linear
-    need = mx.ags_mx_linear_workspace(4, 8, 64)
+    assert mx.ags_mx_linear_workspace(4, 8, 64) == 0                               # few rows: one kernel
+    need = mx.ags_mx_linear_workspace(40, 8, 64)
     assert need > 0
-    _raises(ags.AGS_E_ARG, lin, X, bf, 4, 64, b, Y, bf, 8, None, 0)                 # no workspace
-    _raises(ags.AGS_E_ARG, lin, X, bf, 4, 64, b, Y, bf, 8, Z, need - 1)
-    _raises(ags.AGS_E_ALIGN, lin, X, bf, 4, 64, b, Y, bf, 8, Z + 8, need)
+    _raises(ags.AGS_E_ARG, lin, X, bf, 40, 64, b, Y, bf, 8, None, 0)                # no workspace
+    _raises(ags.AGS_E_ARG, lin, X, bf, 40, 64, b, Y, bf, 8, Z, need - 1)
+    _raises(ags.AGS_E_ALIGN, lin, X, bf, 40, 64, b, Y, bf, 8, Z + 8, need)
     _raises(ags.AGS_E_ARG, lin, X, bf, 4, 63, b, Y, bf, 8, Z, need)
     _raises(ags.AGS_E_ARG, lin, X, bf, 4, 64, b, X, bf, 8, Z, need)
     _raises(ags.AGS_E_ARG, lin, X, bf, 4, 64, b, Y, 5, 8, Z, need)
