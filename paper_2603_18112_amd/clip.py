@@ -198,6 +198,9 @@ class GradClip:
 
     def _stream(self, stream):
         if stream is None:
+            raw = getattr(self.torch._C, "_cuda_getCurrentRawStream", None)
+            if raw is not None:  # 0.1 us instead of 2
+                return raw(self.device.index)
             stream = self.torch.cuda.current_stream(self.device)
         return int(stream.cuda_stream) if hasattr(stream, "cuda_stream") else int(stream)
 

@@ -248,7 +248,9 @@ bool overlap(const void* a, size_t na, const void* b, size_t nb) {
 }
 
 // Is [p, p + bytes) inside one device allocation of the current device?
-ags_status check_device_range(const void* p, size_t bytes, const char* name, std::string& why) {
+// lo, hi: the allocation's bounds, if it is.
+ags_status check_device_range(const void* p, size_t bytes, const char* name, std::string& why,
+                              uintptr_t* lo = nullptr, uintptr_t* hi = nullptr) {
     hipPointerAttribute_t attr;
     std::memset(&attr, 0, sizeof attr);
     hipError_t e = hipPointerGetAttributes(&attr, p);
@@ -280,6 +282,8 @@ ags_status check_device_range(const void* p, size_t bytes, const char* name, std
         why = std::string(name) + " is smaller than the layout needs";
         return AGS_E_ARG;
     }
+    if (lo) *lo = b;
+    if (hi) *hi = b + size;
     return AGS_OK;
 }
 

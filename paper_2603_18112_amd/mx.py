@@ -8,7 +8,7 @@ import ctypes
 
 from . import ags
 
-AGS_MX_BLOCK, AGS_MX_PAD = 32, 256
+AGS_MX_BLOCK, AGS_MX_PAD, AGS_MX_ROWS = 32, 256, 16
 EXPORTS = ("ags_mx_bytes", "ags_mx_quantize", "ags_mx_dequantize", "ags_mx_product_workspace",
            "ags_mx_product", "ags_mx_linear_workspace", "ags_mx_linear")
 
@@ -121,7 +121,13 @@ def _dtype(dtype):
 
 
 def _stream(device):
-    return _t().cuda.current_stream(device).cuda_stream
+    """The current stream of the tensors' device, as an int (the raw query
+    takes 0.1 us, a Stream object 2)."""
+    t = _t()
+    raw = getattr(t._C, "_cuda_getCurrentRawStream", None)
+    if raw is not None and device.index is not None:
+        return raw(device.index)
+    return t.cuda.current_stream(device).cuda_stream
 
 
 def _matrix(x, what):
@@ -141,26 +147,34 @@ def _matrix(x, what):
     return x, rows, cols, stride
 
 
-def _device_guard(device):
-    t = _t()
-    if device.index is not None and device.index != t.cuda.current_device():
-        raise ValueError("the tensors are not on the current device")
+def _up(x, unit):
+    return -(-x // unit) * unit
 
 
 class MX4:
-    """A [rows, cols] tensor held in 4 bits, blocked along its columns."""
+    """A [rows, cols] tensor held in 4 bits, blocked along its columns: one
+    buffer with the codes, then the scales (the sizes ags_mx_bytes gives)."""
 
-    __slots__ = ("codes", "scales", "rows", "cols", "c")
+    __slots__ = ("data", "rows", "cols", "c")
 
     def __init__(self, rows, cols, device=None):
         t = _t()
-        nc, ns = ags_mx_bytes(rows, cols)
+        padded = _up(cols, AGS_MX_PAD)
+        codes, scales = rows * padded // 2, _up(rows, AGS_MX_ROWS) * padded // AGS_MX_BLOCK
         dev = t.device("cuda", t.cuda.current_device()) if device is None else device
-        self.codes = t.empty(nc, dtype=t.uint8, device=dev)
-        self.scales = t.empty(ns, dtype=t.uint8, device=dev)
+        self.data = t.empty(codes + scales, dtype=t.uint8, device=dev)
         self.rows, self.cols = int(rows), int(cols)
-        self.c = ags_mx_tensor(self.codes.data_ptr() or None, self.scales.data_ptr() or None, self.rows,
-                               self.cols)
+        p = self.data.data_ptr() or None
+        # a row of codes is a multiple of 128 bytes, so the scales are aligned too
+        self.c = ags_mx_tensor(p, p and p + codes, self.rows, self.cols)
+
+    @property
+    def codes(self):
+        return self.data[:self.rows * _up(self.cols, AGS_MX_PAD) // 2]
+
+    @property
+    def scales(self):
+        return self.data[self.rows * _up(self.cols, AGS_MX_PAD) // 2:]
 
     @property
     def shape(self):
@@ -173,7 +187,6 @@ def _quantize(x, noise, q, qt):
         qt, q = _quantize(x.t(), None if noise is None else noise.t().contiguous(), qt, q)
         return q, qt
     x, rows, cols, stride = _matrix(x, "x")
-    _device_guard(x.device)
     dt = _dtype(x.dtype)[0]
     n_ptr, n_stride = None, 0
     if noise is not None:
@@ -211,8 +224,7 @@ def dequantize(q, dtype="f32"):
     """The values q stands for, [rows, cols]."""
     t = _t()
     code, dt = _dtype(dtype)
-    out = t.empty((q.rows, q.cols), dtype=dt, device=q.codes.device)
-    _device_guard(out.device)
+    out = t.empty((q.rows, q.cols), dtype=dt, device=q.data.device)
     ags_mx_dequantize(q.c, out.data_ptr() or None, code, max(q.cols, 1), _stream(out.device))
     return out
 
@@ -226,8 +238,7 @@ def product(a, b, dtype="bf16", out=None, accumulate=False):
     written to `out` (2-D, unit column stride), added to it with
     `accumulate`."""
     t = _t()
-    dev = a.codes.device
-    _device_guard(dev)
+    dev = a.data.device
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs out")
@@ -278,7 +289,6 @@ def linear(x, w, dtype=None, save=False):
     if x.shape[-1] != w.k:
         raise ValueError(f"x must have {w.k} columns")
     x2, rows, _, stride = _matrix(x, "x")
-    _device_guard(x2.device)
     out_code, out_dt = _dtype(x.dtype if dtype is None else dtype)
     shape = (*x.shape[:-1], w.n)
     if save:
