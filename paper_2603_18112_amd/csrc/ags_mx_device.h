@@ -49,33 +49,43 @@ __device__ __forceinline__ unsigned codes_nearest(const float* x, unsigned byte)
     return r;
 }
 
-// |x| 2^-e taken to a neighbour on the grid by a random byte r, with x's sign.
-// y = |x| 2^-e is exact and below 8.  From 1 up the grid has one bit after the
-// leading one, so adding (r + 1/2) / 256 of that bit to the fp32 pattern
-// carries into it, and over the binade's end, as the rule asks; what is below
-// the bit is then cut off.  Below 1 the grid is 1/2, that of the binade of
-// 1 + y.  That sum may round: y keeps 11 significant bits first (no threshold,
-// all multiples of 2^-10, lies between y and what is left of it), so the sum is
-// exact down to y = 2^-13, below which no byte rounds up.  bf16 values have 8.
-template <bool BF16>
-__device__ __forceinline__ float round_stochastic(float x, float inv, unsigned r) {
-    unsigned u = __float_as_uint(fabsf(x) * inv);
-    if (!BF16) u &= 0xffffe000u;
-    const float y = __uint_as_float(u), one = y < 1.0f ? 1.0f : 0.0f;
-    const unsigned up = (__float_as_uint(y + one) + ((r << 14) | 0x2000u)) & 0xffc00000u;
-    return copysignf(__uint_as_float(up) - one, x);
-}
+typedef float v2f __attribute__((ext_vector_type(2)));
+typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
 
-// Codes of 8 elements and their random bytes; the converter has nothing left
-// to round, 8 becomes 6.
-template <bool BF16>
-__device__ __forceinline__ unsigned codes_stochastic(const float* x, unsigned byte, const unsigned* r) {
-    const float inv = scale_inverse(byte);
-    float v[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = round_stochastic<BF16>(x[i], inv, r[i]);
-    return codes_nearest(v, 127u);
-}
+// Codes of 8 elements with random bytes.  The stochastic converter takes its
+// first element, on whichever step of the grid it lies, to the upper neighbour
+// where the fraction f of the step has f + seed / 2^32 >= 1; a byte r becomes
+// the seed of (r + 1/2) / 256.  The second element's seed is another, and the
+// converter writes one byte of its register, which the compiler takes to be
+// written whole: so each element is converted into a register of its own, of
+// which the low four bits count.
+struct Stochastic {
+    unsigned c[8];
+    float scale;
+
+    __device__ __forceinline__ explicit Stochastic(unsigned byte) : scale(scale_value(byte)) {}
+
+    // The seed of byte J of r.
+    template <int J>
+    static __device__ __forceinline__ unsigned seed(unsigned r) {
+        return __builtin_amdgcn_perm(r, 0x00800000u, ((4u + J) << 24) | 0x00020000u);
+    }
+    // (The bf16 form of the converter rounds otherwise in some cases.)
+    __device__ __forceinline__ void put(int i, float x, unsigned seed) {
+        float any;  // the second element's result is not used
+        any = __builtin_nondeterministic_value(any);
+        c[i] = __builtin_amdgcn_cvt_scalef32_sr_pk_fp4_f32(0u, v2f{x, any}, seed, scale, 0);
+    }
+    // Bytes 0 of four registers.
+    static __device__ __forceinline__ unsigned bytes(unsigned a, unsigned b, unsigned d, unsigned e) {
+        const unsigned lo = __builtin_amdgcn_perm(b, a, 0x0c0c0400u), hi = __builtin_amdgcn_perm(e, d, 0x0c0c0400u);
+        return lo | (hi << 16);
+    }
+    __device__ __forceinline__ unsigned codes() const {
+        const unsigned even = bytes(c[0], c[2], c[4], c[6]), odd = bytes(c[1], c[3], c[5], c[7]);
+        return (even & 0x0f0f0f0fu) | ((odd & 0x0f0f0f0fu) << 4);
+    }
+};
 
 __device__ __forceinline__ unsigned magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 

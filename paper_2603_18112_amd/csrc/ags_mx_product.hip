@@ -31,8 +31,8 @@ __device__ __forceinline__ v8i operand(uint4 v) {
     return v8i{(int)v.x, (int)v.y, (int)v.z, (int)v.w, 0, 0, 0, 0};
 }
 
-typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
-typedef float v2f __attribute__((ext_vector_type(2)));
+using mx::v2bf;
+using mx::v2f;
 
 // To nearest even, by the hardware's converter.
 __device__ __forceinline__ unsigned pack_bf16(float x, float y) {

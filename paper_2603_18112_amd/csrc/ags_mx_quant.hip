@@ -31,17 +31,20 @@ __device__ __forceinline__ void load_noise8(const uint8_t* p, int64_t left, unsi
         if (i < left) r[i >> 2] |= (unsigned)p[i] << (8 * (i & 3));
 }
 
-// r: the elements' random bytes.
-template <typename T, bool STOCHASTIC>
-__device__ __forceinline__ unsigned codes8(const float* x, unsigned byte, const unsigned* r) {
-    const unsigned c = STOCHASTIC ? mx::codes_stochastic<sizeof(T) == 2>(x, byte, r) : mx::codes_nearest(x, byte);
-    return byte == 255u ? 0u : c;
+// Codes of 8 elements and, stochastic, their random bytes in two dwords.
+__device__ __forceinline__ unsigned stochastic8(const float* x, unsigned byte, const unsigned* r) {
+    typedef mx::Stochastic S;
+    S c(byte);
+    c.put(0, x[0], S::seed<0>(r[0])), c.put(1, x[1], S::seed<1>(r[0]));
+    c.put(2, x[2], S::seed<2>(r[0])), c.put(3, x[3], S::seed<3>(r[0]));
+    c.put(4, x[4], S::seed<0>(r[1])), c.put(5, x[5], S::seed<1>(r[1]));
+    c.put(6, x[6], S::seed<2>(r[1])), c.put(7, x[7], S::seed<3>(r[1]));
+    return c.codes();
 }
-
-// The 8 bytes of two dwords.
-__device__ __forceinline__ void bytes8(const unsigned* w, unsigned* r) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) r[i] = (w[i >> 2] >> (8 * (i & 3))) & 255u;
+template <bool STOCHASTIC>
+__device__ __forceinline__ unsigned codes8(const float* x, unsigned byte, const unsigned* r) {
+    const unsigned c = STOCHASTIC ? stochastic8(x, byte, r) : mx::codes_nearest(x, byte);
+    return byte == 255u ? 0u : c;
 }
 
 // The scale byte of 4 neighbouring lanes' 32 elements.
@@ -64,14 +67,11 @@ __global__ __launch_bounds__(kQBlock) void mx_rows_kernel(MxQuantArgs a, unsigne
     const int64_t c = (int64_t)chunk * 256 + lane * 8;
     float x[8];
     mx::load8(static_cast<const T*>(a.x) + row * a.stride + c, a.cols - c, x);
-    unsigned w[2], r[8];
-    if (STOCHASTIC) {
-        load_noise8(a.noise + row * a.noise_stride + c, a.cols - c, w);
-        bytes8(w, r);
-    }
+    unsigned r[2] = {0, 0};
+    if (STOCHASTIC) load_noise8(a.noise + row * a.noise_stride + c, a.cols - c, r);
     const unsigned b = scale_of_quad<STOCHASTIC>(x);
     const int64_t kp = (int64_t)per_row * 256;
-    *reinterpret_cast<unsigned*>(a.codes + row * (kp / 2) + c / 2) = codes8<T, STOCHASTIC>(x, b, r);
+    *reinterpret_cast<unsigned*>(a.codes + row * (kp / 2) + c / 2) = codes8<STOCHASTIC>(x, b, r);
     if ((lane & 3) == 0) a.scales[mx::scale_at(a.rows, row, c)] = (uint8_t)b;
 }
 
@@ -151,7 +151,7 @@ __global__ __launch_bounds__(kQBlock) void mx_transpose_kernel(MxQuantArgs a, un
     const int64_t left = a.cols - c0 - c;
     const T* px = static_cast<const T*>(a.x) + c0 + c;
     const uint8_t* pn = a.noise + c0 + c;
-    constexpr int kAhead = 4;  // rows of a thread in flight
+    constexpr int kAhead = sizeof(T) == 4 ? 8 : 4;  // rows of a thread in flight
 #pragma unroll
     for (int i0 = 0; i0 < kTile / 16; i0 += kAhead) {
         float x[kAhead][8];
@@ -180,9 +180,7 @@ __global__ __launch_bounds__(kQBlock) void mx_transpose_kernel(MxQuantArgs a, un
             if (STOCHASTIC) *reinterpret_cast<uint2*>(&noise[lr * kTile + c]) = make_uint2(r[i][0], r[i][1]);
             if (ROWS) {
                 const unsigned b = scale_of_quad<STOCHASTIC>(x[i]);
-                unsigned bytes[8];
-                if (STOCHASTIC) bytes8(r[i], bytes);
-                const unsigned v = codes8<T, STOCHASTIC>(x[i], b, bytes);
+                const unsigned v = codes8<STOCHASTIC>(x[i], b, r[i]);
                 // the row's four scales as one dword
                 unsigned all = b << (2 * (tid & 12));
                 all |= (unsigned)__shfl_xor((int)all, 4, 64);
@@ -215,14 +213,20 @@ __global__ __launch_bounds__(kQBlock) void mx_transpose_kernel(MxQuantArgs a, un
         sc[k] = (uint8_t)b;
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-            float x[8];
-            unsigned r[8];
+            if constexpr (STOCHASTIC) {
+                mx::Stochastic c(b);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                x[i] = v.value(k, 8 * g + i);
-                if (STOCHASTIC) r[i] = (nz[8 * g + i] >> (8 * k)) & 255u;
+                for (int i = 0; i < 8; ++i) {
+                    const unsigned r = nz[8 * g + i];
+                    c.put(i, v.value(k, 8 * g + i), k == 0 ? mx::Stochastic::seed<0>(r) : mx::Stochastic::seed<1>(r));
+                }
+                cs[k][g] = b == 255u ? 0u : c.codes();
+            } else {
+                float x[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = v.value(k, 8 * g + i);
+                cs[k][g] = codes8<false>(x, b, nullptr);
             }
-            cs[k][g] = codes8<T, STOCHASTIC>(x, b, r);
         }
     }
     __syncthreads();
@@ -249,8 +253,6 @@ __global__ __launch_bounds__(kQBlock) void mx_transpose_kernel(MxQuantArgs a, un
 
 // ---------------------------------------------------------------- reading --
 
-typedef float v2f __attribute__((ext_vector_type(2)));
-
 template <typename T>
 __global__ __launch_bounds__(kQBlock) void mx_dequant_kernel(MxDequantArgs a, unsigned units, unsigned per_row) {
     const unsigned u = blockIdx.x * (kQBlock / 32) + threadIdx.x / 32;
@@ -265,7 +267,7 @@ __global__ __launch_bounds__(kQBlock) void mx_dequant_kernel(MxDequantArgs a, un
     float x[8];
 #define MX_PAIR(I)                                                                  \
     {                                                                               \
-        const v2f v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, s, I);        \
+        const mx::v2f v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, s, I);        \
         x[2 * I] = v[0], x[2 * I + 1] = v[1];                                       \
     }
     MX_PAIR(0) MX_PAIR(1) MX_PAIR(2) MX_PAIR(3)
