@@ -5,7 +5,7 @@
 //                    elements, 8 each; 4 lanes share a block's scale.
 // mx_transpose_kernel     blocks along the columns (the transposed form), and those
 //                    along the rows in the same pass: a tile of 128 x 128 goes
-//                    through LDS, a thread takes 32 rows of two columns.
+//                    through LDS, a thread takes 32 rows of a column.
 // mx_dequant_kernel  8 codes a thread.
 //
 // All stream from HBM and use no matrix cores.  Rows may start anywhere: the
@@ -78,60 +78,52 @@ __global__ __launch_bounds__(kQBlock) void mx_rows_kernel(MxQuantArgs a, unsigne
 // ------------------------------------------------------------ tile kernel --
 
 constexpr int kTile = 128;
-// Bytes between the columns' codes in LDS: 16-byte writes of 8 neighbouring
-// column pairs fall on different banks.
+// Eight waves to a tile: with four, two columns to a lane, LDS left fewer waves
+// on a CU to cover the loads (8192 x 8192 bf16 both forms 42.6 -> 40.7 us, with
+// random bytes 75.6 -> 71.5; 5001 x 2047, rows that start anywhere, 16.9 -> 12.0).
+constexpr int kTBlock = 512;
+// Bytes between the columns' codes in LDS: 16-byte writes of neighbouring
+// columns fall on different banks.
 constexpr int kCodePitch = kTile / 2 + 16;
 
-// The larger of two pairs of 16-bit magnitudes.
-__device__ __forceinline__ unsigned max_pairs(unsigned a, unsigned b) {
-    typedef unsigned short u2 __attribute__((ext_vector_type(2)));
-    const u2 m = __builtin_elementwise_max(__builtin_bit_cast(u2, a), __builtin_bit_cast(u2, b));
-    return __builtin_bit_cast(unsigned, m);
-}
-
-// Two neighbouring columns' 32 values from LDS, and their magnitudes' maxima
-// (as fp32 bits).
+// A column's 32 values from LDS, and their largest magnitude (as fp32 bits).
 template <typename T>
-struct ColumnPair;
+struct Column;
 template <>
-struct ColumnPair<unsigned short> {
-    unsigned w[32];  // both columns of a row
+struct Column<unsigned short> {
+    unsigned w[32];
     __device__ __forceinline__ void load(const unsigned short* p) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) w[i] = *reinterpret_cast<const unsigned*>(p + i * kTile);
+        for (int i = 0; i < 32; ++i) w[i] = p[i * kTile];
     }
-    __device__ __forceinline__ void maxima(unsigned* m) const {
-        unsigned t = 0;
+    __device__ __forceinline__ unsigned largest() const {
+        unsigned m = 0;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) t = max_pairs(t, w[i] & 0x7fff7fffu);
-        m[0] = t << 16, m[1] = t & 0xffff0000u;
+        for (int i = 0; i < 32; ++i) m = max(m, w[i] & 0x7fffu);
+        return m << 16;
     }
-    __device__ __forceinline__ float value(int c, int i) const {
-        return __uint_as_float(c ? w[i] & 0xffff0000u : w[i] << 16);
-    }
+    __device__ __forceinline__ float value(int i) const { return __uint_as_float(w[i] << 16); }
 };
 template <>
-struct ColumnPair<float> {
-    float2 w[32];
+struct Column<float> {
+    float w[32];
     __device__ __forceinline__ void load(const float* p) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) w[i] = *reinterpret_cast<const float2*>(p + i * kTile);
+        for (int i = 0; i < 32; ++i) w[i] = p[i * kTile];
     }
-    __device__ __forceinline__ void maxima(unsigned* m) const {
-        m[0] = m[1] = 0;
+    __device__ __forceinline__ unsigned largest() const {
+        unsigned m = 0;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            m[0] = max(m[0], mx::magnitude(w[i].x));
-            m[1] = max(m[1], mx::magnitude(w[i].y));
-        }
+        for (int i = 0; i < 32; ++i) m = max(m, mx::magnitude(w[i]));
+        return m;
     }
-    __device__ __forceinline__ float value(int c, int i) const { return c ? w[i].y : w[i].x; }
+    __device__ __forceinline__ float value(int i) const { return w[i]; }
 };
 
 // One tile.  ROWS: the form along the rows is wanted too.  The grid covers
 // the padded rows and columns, since padding is stored as zeros.
 template <typename T, bool STOCHASTIC, bool ROWS>
-__global__ __launch_bounds__(kQBlock) void mx_transpose_kernel(MxQuantArgs a, unsigned tiles_c, unsigned tiles) {
+__global__ __launch_bounds__(kTBlock) void mx_transpose_kernel(MxQuantArgs a, unsigned tiles_c, unsigned tiles) {
     __shared__ alignas(16) T tile[kTile * kTile];
     __shared__ alignas(16) uint8_t noise[STOCHASTIC ? kTile * kTile : 8];
     // The codes and scales of the columns take the tile's place once it has
@@ -143,29 +135,29 @@ __global__ __launch_bounds__(kQBlock) void mx_transpose_kernel(MxQuantArgs a, un
     const unsigned xcd = blockIdx.x % kXcds, base = tiles / kXcds, rest = tiles % kXcds;
     const unsigned t = xcd * base + min(xcd, rest) + blockIdx.x / kXcds;
     const int64_t r0 = (int64_t)(t / tiles_c) * kTile, c0 = (int64_t)(t % tiles_c) * kTile;
-    const int tid = threadIdx.x, lane = tid & 63;
+    const int tid = threadIdx.x;
     const int64_t kp = (int64_t)tiles_c * kTile;
 
-    // 16 threads take a row, 8 elements each; 16 rows at a time.
+    // 16 threads take a row, 8 elements each; 32 rows at a time.
     const int c = (tid & 15) * 8;
     const int64_t left = a.cols - c0 - c;
     const T* px = static_cast<const T*>(a.x) + c0 + c;
     const uint8_t* pn = a.noise + c0 + c;
-    constexpr int kAhead = sizeof(T) == 4 ? 8 : 4;  // rows of a thread in flight
+    constexpr int kAhead = 4;  // rows of a thread, all in flight
 #pragma unroll
-    for (int i0 = 0; i0 < kTile / 16; i0 += kAhead) {
+    for (int i0 = 0; i0 < kTile / (kTBlock / 16); i0 += kAhead) {
         float x[kAhead][8];
         unsigned r[kAhead][2];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            const int64_t row = r0 + (i0 + i) * 16 + (tid >> 4);
+            const int64_t row = r0 + (i0 + i) * (kTBlock / 16) + (tid >> 4);
             const int64_t l = row < a.rows ? left : 0;
             mx::load8(px + row * a.stride, l, x[i]);
             if (STOCHASTIC) load_noise8(pn + row * a.noise_stride, l, r[i]);
         }
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            const int lr = (i0 + i) * 16 + (tid >> 4);
+            const int lr = (i0 + i) * (kTBlock / 16) + (tid >> 4);
             if constexpr (sizeof(T) == 2) {
                 unsigned w[4];
 #pragma unroll
@@ -194,58 +186,37 @@ __global__ __launch_bounds__(kQBlock) void mx_transpose_kernel(MxQuantArgs a, un
     }
     __syncthreads();
 
-    // A wave takes 32 rows, a lane two columns.
-    const int rb = tid >> 6, cc = lane * 2;
-    ColumnPair<T> v;
+    // Two waves take 32 rows, a lane one column.
+    const int rb = tid >> 7, cc = tid & 127;
+    Column<T> v;
     v.load(&tile[rb * 32 * kTile + cc]);
-    unsigned m[2], cs[2][4];
-    uint8_t sc[2];
-    v.maxima(m);
-    unsigned nz[32];
-    if (STOCHASTIC) {
+    const unsigned b = mx::scale_byte<STOCHASTIC>(v.largest());
+    unsigned cs[4];
 #pragma unroll
-        for (int i = 0; i < 32; ++i)
-            nz[i] = *reinterpret_cast<const unsigned short*>(&noise[(rb * 32 + i) * kTile + cc]);
-    }
+    for (int g = 0; g < 4; ++g) {
+        if constexpr (STOCHASTIC) {
+            mx::Stochastic s(b);
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const unsigned b = mx::scale_byte<STOCHASTIC>(m[k]);
-        sc[k] = (uint8_t)b;
+            for (int i = 0; i < 8; ++i)
+                s.put(i, v.value(8 * g + i), mx::Stochastic::seed<0>(noise[(rb * 32 + 8 * g + i) * kTile + cc]));
+            cs[g] = b == 255u ? 0u : s.codes();
+        } else {
+            float x[8];
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            if constexpr (STOCHASTIC) {
-                mx::Stochastic c(b);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const unsigned r = nz[8 * g + i];
-                    c.put(i, v.value(k, 8 * g + i), k == 0 ? mx::Stochastic::seed<0>(r) : mx::Stochastic::seed<1>(r));
-                }
-                cs[k][g] = b == 255u ? 0u : c.codes();
-            } else {
-                float x[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = v.value(k, 8 * g + i);
-                cs[k][g] = codes8<false>(x, b, nullptr);
-            }
+            for (int i = 0; i < 8; ++i) x[i] = v.value(8 * g + i);
+            cs[g] = codes8<false>(x, b, nullptr);
         }
     }
     __syncthreads();
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        *reinterpret_cast<uint4*>(codes + (cc + k) * kCodePitch + rb * 16) =
-            make_uint4(cs[k][0], cs[k][1], cs[k][2], cs[k][3]);
-        col_scale[(cc + k) * 4 + rb] = sc[k];
-    }
+    *reinterpret_cast<uint4*>(codes + cc * kCodePitch + rb * 16) = make_uint4(cs[0], cs[1], cs[2], cs[3]);
+    col_scale[cc * 4 + rb] = (uint8_t)b;
     __syncthreads();
     // Whole columns of the tile: 64 bytes each, four threads to a column.
     const int64_t kpt = mx_padded(a.rows);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int col = i * 64 + (tid >> 2), part = (tid & 3) * 16;
-        if (c0 + col < a.cols)
-            *reinterpret_cast<uint4*>(a.codes_t + (c0 + col) * (kpt / 2) + r0 / 2 + part) =
-                *reinterpret_cast<const uint4*>(codes + col * kCodePitch + part);
-    }
+    const int col = tid >> 2, part = (tid & 3) * 16;
+    if (c0 + col < a.cols)
+        *reinterpret_cast<uint4*>(a.codes_t + (c0 + col) * (kpt / 2) + r0 / 2 + part) =
+            *reinterpret_cast<const uint4*>(codes + col * kCodePitch + part);
     if (tid < kTile && c0 + tid < a.cols)
         *reinterpret_cast<unsigned*>(&a.scales_t[mx::scale_at(a.cols, c0 + tid, r0)]) =
             *reinterpret_cast<const unsigned*>(&col_scale[tid * 4]);
@@ -314,9 +285,9 @@ hipError_t launch_quantize(const MxQuantArgs& a, hipStream_t s) {
     const unsigned tiles_c = (unsigned)(mx_padded(a.cols) / kTile);
     const unsigned tiles = tiles_c * (unsigned)(mx_padded(a.rows) / kTile);
     if (a.codes)
-        hipLaunchKernelGGL((mx_transpose_kernel<T, STOCHASTIC, true>), dim3(tiles), dim3(kQBlock), 0, s, a, tiles_c, tiles);
+        hipLaunchKernelGGL((mx_transpose_kernel<T, STOCHASTIC, true>), dim3(tiles), dim3(kTBlock), 0, s, a, tiles_c, tiles);
     else
-        hipLaunchKernelGGL((mx_transpose_kernel<T, STOCHASTIC, false>), dim3(tiles), dim3(kQBlock), 0, s, a, tiles_c, tiles);
+        hipLaunchKernelGGL((mx_transpose_kernel<T, STOCHASTIC, false>), dim3(tiles), dim3(kTBlock), 0, s, a, tiles_c, tiles);
     return hipGetLastError();
 }
 
