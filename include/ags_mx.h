@@ -45,7 +45,8 @@
  * allocations; the text of the last failed call on this thread from
  * ags_last_error(NULL); work goes on hip_stream and the call returns without
  * waiting.  There is no handle: the caller owns every buffer, workspaces
- * included, and orders calls that share one.
+ * included, and orders calls that share one.  A dtype argument is an
+ * ags_dtype.
  */
 #ifndef AGS_MX_H
 #define AGS_MX_H
@@ -73,22 +74,22 @@ typedef struct {
 } ags_mx_tensor;
 
 /* Bytes of a tensor's codes and scales (host only).  AGS_E_LAYOUT where
- * cols exceeds 2^24 or the element count 2^40. */
+ * cols exceeds 2^24 or the elements, padding included, 2^34. */
 ags_status ags_mx_bytes(int64_t rows, int64_t cols, size_t *codes, size_t *scales);
 
 /* Store x [rows, cols] (fp32 or bf16, row i at element i * row_stride,
  * row_stride >= cols) as q [rows, cols], as qt [cols, rows] (x transposed,
  * blocked along its columns), or as both in one pass; the other may be NULL.
  * d_noise: NULL for rounding to nearest, or random bytes [rows][noise_stride]
- * (both forms use an element's one byte).  x needs its element's alignment
- * only; 16-byte aligned rows are read faster. */
-ags_status ags_mx_quantize(const void *d_x, ags_dtype dtype, int64_t rows, int64_t cols,
+ * (both forms use an element's one byte).  Rows need their element's alignment
+ * only. */
+ags_status ags_mx_quantize(const void *d_x, int32_t dtype, int64_t rows, int64_t cols,
                            int64_t row_stride, const uint8_t *d_noise, int64_t noise_stride,
                            const ags_mx_tensor *q, const ags_mx_tensor *qt, void *hip_stream);
 
 /* Read q back to out [q.rows][row_stride] (fp32 or bf16: both hold every
  * value exactly). */
-ags_status ags_mx_dequantize(const ags_mx_tensor *q, void *d_out, ags_dtype dtype,
+ags_status ags_mx_dequantize(const ags_mx_tensor *q, void *d_out, int32_t dtype,
                              int64_t row_stride, void *hip_stream);
 
 /* out [a.rows][row_stride], row_stride >= b.rows, a.cols == b.cols: the
@@ -98,7 +99,7 @@ ags_status ags_mx_dequantize(const ags_mx_tensor *q, void *d_out, ags_dtype dtyp
  * anything but the operands: sums are added in a fixed order. */
 ags_status ags_mx_product_workspace(int64_t m, int64_t n, int64_t k, size_t *out_bytes);
 ags_status ags_mx_product(const ags_mx_tensor *a, const ags_mx_tensor *b, void *d_out,
-                          ags_dtype dtype, int64_t row_stride, int32_t accumulate,
+                          int32_t dtype, int64_t row_stride, int32_t accumulate,
                           void *d_workspace, size_t workspace_bytes, void *hip_stream);
 
 /* y [rows][y_stride] = x w' for x [rows, w.cols] (as in ags_mx_quantize):
@@ -106,8 +107,8 @@ ags_status ags_mx_product(const ags_mx_tensor *a, const ags_mx_tensor *b, void *
  * tokens) take one kernel that does both.  The values are those of
  * ags_mx_quantize and ags_mx_product up to the order of fp32 sums. */
 ags_status ags_mx_linear_workspace(int64_t rows, int64_t n, int64_t k, size_t *out_bytes);
-ags_status ags_mx_linear(const void *d_x, ags_dtype dtype, int64_t rows, int64_t row_stride,
-                         const ags_mx_tensor *w, void *d_y, ags_dtype y_dtype, int64_t y_stride,
+ags_status ags_mx_linear(const void *d_x, int32_t dtype, int64_t rows, int64_t row_stride,
+                         const ags_mx_tensor *w, void *d_y, int32_t y_dtype, int64_t y_stride,
                          void *d_workspace, size_t workspace_bytes, void *hip_stream);
 
 #ifdef __cplusplus

@@ -45,7 +45,7 @@ struct WsLayout {
     size_t state_bytes = 0;  // gradscale .. state end
 };
 
-size_t elem_bytes(ags_dtype dt) { return dt == AGS_BF16 ? 2 : 4; }
+size_t elem_bytes(int32_t dt) { return dt == AGS_BF16 ? 2 : 4; }
 
 bool materialize_gbar(const ags_config& c) {
     // Only a LARS step has a second pass over the replica mean.

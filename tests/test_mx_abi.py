@@ -145,3 +145,13 @@ def test_reference_stochastic_is_unbiased():
         mean += v / 256
     step = np.where(np.abs(x) < 2 * 2.0 ** e[0, 0], 0.5, np.where(np.abs(x) < 4 * 2.0 ** e[0, 0], 1.0, 2.0))
     assert np.all(np.abs(mean - x) <= step * 2.0 ** e[0, 0] / 512 + 1e-12)
+
+
+@pytest.mark.parametrize("rows,stride", [((1 << 26), 1 << 40), (1 << 24, (1 << 62) // (1 << 24)), (3, 1 << 62)])
+def test_strides_past_any_address_space(rows, stride):
+    # (rows - 1) * stride elements of 4 bytes pass 2^64, or come near it: the
+    # size of the buffer must not wrap to a small one.
+    for row_stride, noise in ((stride, None), (64, V)):
+        with pytest.raises(ags.AGSError) as e:
+            mx.ags_mx_quantize(X, ags.AGS_F32, rows, 64, row_stride, noise, stride, _t(rows, 64), None)
+        assert e.value.status == ags.AGS_E_ARG and "stride" in str(e.value)
