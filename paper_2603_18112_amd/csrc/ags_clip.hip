@@ -5,8 +5,15 @@
 //                    each group in index order and writes N_g and c_g.
 // clip_scale_kernel  one block per piece: out = x c_g.  In place, blocks of a
 //                    group with c_g = 1 exit at once.
+// clip_small_kernel  both of them in one block, for few elements.
 //
-// Both stream from HBM (about one flop per byte) and use no matrix cores.
+// All stream from HBM (about one flop per byte; fp64 sums cost nothing: with
+// fp32 sums the norm takes as long) and use no matrix cores.  c_g is known only
+// when all has been read, so a set larger than the caches is read twice.
+// MI355X: norm of 138M fp32 88 us (6.3 TB/s; a kernel that only reads reaches
+// 7.1), of 138M bf16 48 us; scaling passes 8 x 25.5M fp32 to bf16 some 225 us
+// (5.4 TB/s read and written; a copy reaches 4.7); 25.5M bf16 into a row 32 us in
+// all; 2000 to 65536 elements 7, which is the host's time for the call.
 #include <math.h>
 
 #include "ags_clip_internal.h"
@@ -48,40 +55,43 @@ __device__ __forceinline__ double wave_reduce(double v) {
     return v;
 }
 
-template <typename T>
-struct Load8;  // 8 consecutive elements at a 16-byte boundary, as fp32
-template <>
-struct Load8<float> {
-    static __device__ __forceinline__ void get(const float* p, float* x) {
-        const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-        x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
-    }
-    static __device__ __forceinline__ float one(const float* p) { return *p; }
-    static __device__ __forceinline__ void put(float* p, const float* x) {
-        reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
-        reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
-    }
-    static __device__ __forceinline__ void put_one(float* p, float x) { *p = x; }
-};
-template <>
-struct Load8<unsigned short> {
-    static __device__ __forceinline__ void get(const unsigned short* p, float* x) {
-        const uint4 v = *reinterpret_cast<const uint4*>(p);
-        const unsigned w[4] = {v.x, v.y, v.z, v.w};
+__device__ __forceinline__ float load1(const float* p) { return *p; }
+__device__ __forceinline__ float load1(const unsigned short* p) { return bf16_value(*p); }
+__device__ __forceinline__ void store1(float* p, float x) { *p = x; }
+__device__ __forceinline__ void store1(unsigned short* p, float x) { *p = bf16_round(x); }
+
+// N elements of T side by side, as fp32.  An access is of at most 16 bytes a
+// lane and side by side over the lanes (8 fp32 elements a lane, in two accesses
+// half a line apart, read 138M elements with streaming at 5.1 TB/s; 4 do at
+// 6.0).  Any alignment of the element will do.
+template <typename T, int N>
+struct Access {
+    static_assert(N * sizeof(T) <= 16, "one access");
+    typedef unsigned V __attribute__((ext_vector_type(N * sizeof(T) / 4), aligned(sizeof(T))));
+
+    // STREAM: past the caches.
+    template <bool STREAM>
+    static __device__ __forceinline__ void load(const T* p, float* x) {
+        const V* q = reinterpret_cast<const V*>(p);
+        const V v = STREAM ? __builtin_nontemporal_load(q) : *q;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[2 * i] = __uint_as_float(w[i] << 16);
-            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        for (int i = 0; i < N; ++i) {
+            if constexpr (sizeof(T) == 4) x[i] = __uint_as_float(v[i]);
+            else x[i] = __uint_as_float(i & 1 ? v[i / 2] & 0xffff0000u : v[i / 2] << 16);
         }
     }
-    static __device__ __forceinline__ float one(const unsigned short* p) { return bf16_value(*p); }
-    static __device__ __forceinline__ void put(unsigned short* p, const float* x) {
-        unsigned w[4];
+    template <bool STREAM>
+    static __device__ __forceinline__ void store(T* p, const float* x) {
+        V v;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = bf16_round(x[2 * i]) | ((unsigned)bf16_round(x[2 * i + 1]) << 16);
-        *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+        for (unsigned i = 0; i < N * sizeof(T) / 4; ++i) {
+            if constexpr (sizeof(T) == 4) v[i] = __float_as_uint(x[i]);
+            else v[i] = bf16_round(x[2 * i]) | ((unsigned)bf16_round(x[2 * i + 1]) << 16);
+        }
+        V* q = reinterpret_cast<V*>(p);
+        if (STREAM) __builtin_nontemporal_store(v, q);
+        else *q = v;
     }
-    static __device__ __forceinline__ void put_one(unsigned short* p, float x) { *p = bf16_round(x); }
 };
 
 // Elements before p's next 16-byte boundary, at most n.
@@ -96,44 +106,46 @@ __device__ __forceinline__ const void* base_of(const ClipArgs& a, int i) {
 }
 
 // The sum over n elements by NT threads, this one's share.
-template <int KIND, int NT, typename T>
+template <int KIND, int NT, bool STREAM, typename T>
 __device__ __forceinline__ double piece_sum(const T* p, int n, int tid) {
+    constexpr int N = 16 / sizeof(T), U = 32 / N;  // an access, and those in flight
+    typedef Access<T, N> A;
     const int head = head_elems(p, n);
     double acc = 0.0, acc2 = 0.0;
-    if (tid < head) acc = accumulate<KIND>(acc, Load8<T>::one(p + tid));
+    if (tid < head) acc = accumulate<KIND>(acc, load1(p + tid));
     p += head;
     n -= head;
-    const int groups = n / 8;
+    const int groups = n / N;
     int i = tid;
-    for (; i + 3 * NT < groups; i += 4 * NT) {
-        float x[4][8];
+    for (; i + (U - 1) * NT < groups; i += U * NT) {
+        float x[U][N];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) Load8<T>::get(p + (size_t)(i + u * NT) * 8, x[u]);
+        for (int u = 0; u < U; ++u) A::template load<STREAM>(p + (size_t)(i + u * NT) * N, x[u]);
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int j = 0; j < 8; j += 2) {
+            for (int j = 0; j < N; j += 2) {
                 acc = accumulate<KIND>(acc, x[u][j]);
                 acc2 = accumulate<KIND>(acc2, x[u][j + 1]);
             }
     }
     for (; i < groups; i += NT) {
-        float x[8];
-        Load8<T>::get(p + (size_t)i * 8, x);
+        float x[N];
+        A::template load<STREAM>(p + (size_t)i * N, x);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc = accumulate<KIND>(acc, x[j]);
+        for (int j = 0; j < N; ++j) acc = accumulate<KIND>(acc, x[j]);
     }
-    const int tail = groups * 8 + tid;
-    if (tail < n) acc = accumulate<KIND>(acc, Load8<T>::one(p + tail));
+    const int tail = groups * N + tid;
+    if (tail < n) acc = accumulate<KIND>(acc, load1(p + tail));
     return combine<KIND>(acc, acc2);
 }
 
-template <int KIND, int NT>
+template <int KIND, int NT, bool STREAM>
 __device__ __forceinline__ double sum_of(const ClipArgs& a, const ClipPiece& pc, int tid) {
     const void* base = base_of(a, pc.in_base);
     return pc.in_dt == AGS_F32
-               ? piece_sum<KIND, NT>(static_cast<const float*>(base) + pc.in_off, pc.count, tid)
-               : piece_sum<KIND, NT>(static_cast<const unsigned short*>(base) + pc.in_off, pc.count, tid);
+               ? piece_sum<KIND, NT, STREAM>(static_cast<const float*>(base) + pc.in_off, pc.count, tid)
+               : piece_sum<KIND, NT, STREAM>(static_cast<const unsigned short*>(base) + pc.in_off, pc.count, tid);
 }
 
 template <int KIND>
@@ -170,7 +182,9 @@ __global__ __launch_bounds__(kClipBlock) void clip_norm_kernel(ClipArgs a) {
     __shared__ int sh_last;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const ClipPiece pc = a.pieces[blockIdx.x];
-    double v = wave_reduce<KIND>(sum_of<KIND, kClipBlock>(a, pc, tid));
+    double v = (int)blockIdx.x < a.streamed ? sum_of<KIND, kClipBlock, true>(a, pc, tid)
+                                            : sum_of<KIND, kClipBlock, false>(a, pc, tid);
+    v = wave_reduce<KIND>(v);
     if (lane == 0) sh[wave] = v;
     __syncthreads();
     if (tid == 0) {
@@ -210,43 +224,40 @@ __global__ __launch_bounds__(kClipBlock) void clip_norm_kernel(ClipArgs a) {
     if (tid <= kClipCounters) a.done[tid * kClipCounterStride] = 0u;
 }
 
-template <int NT, typename TI, typename TO>
+// IN, OUT: past the caches.
+template <int NT, bool IN, bool OUT, typename TI, typename TO>
 __device__ __forceinline__ void piece_scale(const TI* in, TO* out, int n, float2 c, int tid) {
+    constexpr int N = sizeof(TI) + sizeof(TO) == 4 ? 8 : 4, U = 32 / N;
     const int head = head_elems(in, n);
-    if ((reinterpret_cast<uintptr_t>(out + head) & 15u) != 0) {
-        // the two sides' boundaries differ: element by element
-        for (int i = tid; i < n; i += NT) Load8<TO>::put_one(out + i, Load8<TI>::one(in + i) * c.x * c.y);
-        return;
-    }
-    if (tid < head) Load8<TO>::put_one(out + tid, Load8<TI>::one(in + tid) * c.x * c.y);
+    if (tid < head) store1(out + tid, load1(in + tid) * c.x * c.y);
     in += head;
     out += head;
     n -= head;
-    const int groups = n / 8;
+    const int groups = n / N;
     int i = tid;
-    for (; i + NT < groups; i += 2 * NT) {
-        float x[2][8];
+    for (; i + (U - 1) * NT < groups; i += U * NT) {
+        float x[U][N];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) Load8<TI>::get(in + (size_t)(i + u * NT) * 8, x[u]);
+        for (int u = 0; u < U; ++u) Access<TI, N>::template load<IN>(in + (size_t)(i + u * NT) * N, x[u]);
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
+        for (int u = 0; u < U; ++u) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[u][j] = x[u][j] * c.x * c.y;
-            Load8<TO>::put(out + (size_t)(i + u * NT) * 8, x[u]);
+            for (int j = 0; j < N; ++j) x[u][j] = x[u][j] * c.x * c.y;
+            Access<TO, N>::template store<OUT>(out + (size_t)(i + u * NT) * N, x[u]);
         }
     }
     for (; i < groups; i += NT) {
-        float x[8];
-        Load8<TI>::get(in + (size_t)i * 8, x);
+        float x[N];
+        Access<TI, N>::template load<IN>(in + (size_t)i * N, x);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = x[j] * c.x * c.y;
-        Load8<TO>::put(out + (size_t)i * 8, x);
+        for (int j = 0; j < N; ++j) x[j] = x[j] * c.x * c.y;
+        Access<TO, N>::template store<OUT>(out + (size_t)i * N, x);
     }
-    const int tail = groups * 8 + tid;
-    if (tail < n) Load8<TO>::put_one(out + tail, Load8<TI>::one(in + tail) * c.x * c.y);
+    const int tail = groups * N + tid;
+    if (tail < n) store1(out + tail, load1(in + tail) * c.x * c.y);
 }
 
-template <int NT>
+template <int NT, bool IN, bool OUT>
 __device__ __forceinline__ void scale_piece(const ClipArgs& a, const ClipPiece& pc, float2 c, int tid) {
     if (a.in_place && c.x == 1.0f && c.y == 1.0f) return;
     const void* in = base_of(a, pc.in_base);
@@ -255,29 +266,32 @@ __device__ __forceinline__ void scale_piece(const ClipArgs& a, const ClipPiece& 
     const int odt = a.in_place ? pc.in_dt : pc.out_dt;
     if (pc.in_dt == AGS_F32) {
         const float* p = static_cast<const float*>(in) + pc.in_off;
-        if (odt == AGS_F32) piece_scale<NT>(p, static_cast<float*>(out) + oo, pc.count, c, tid);
-        else piece_scale<NT>(p, static_cast<unsigned short*>(out) + oo, pc.count, c, tid);
+        if (odt == AGS_F32) piece_scale<NT, IN, OUT>(p, static_cast<float*>(out) + oo, pc.count, c, tid);
+        else piece_scale<NT, IN, OUT>(p, static_cast<unsigned short*>(out) + oo, pc.count, c, tid);
     } else {
         const unsigned short* p = static_cast<const unsigned short*>(in) + pc.in_off;
-        if (odt == AGS_F32) piece_scale<NT>(p, static_cast<float*>(out) + oo, pc.count, c, tid);
-        else piece_scale<NT>(p, static_cast<unsigned short*>(out) + oo, pc.count, c, tid);
+        if (odt == AGS_F32) piece_scale<NT, IN, OUT>(p, static_cast<float*>(out) + oo, pc.count, c, tid);
+        else piece_scale<NT, IN, OUT>(p, static_cast<unsigned short*>(out) + oo, pc.count, c, tid);
     }
 }
 
 __global__ __launch_bounds__(kClipBlock) void clip_scale_kernel(ClipArgs a) {
     // Backwards: the norm's pass left its last pieces in the caches.
-    const ClipPiece pc = a.pieces[a.n_pieces - 1 - blockIdx.x];
-    scale_piece<kClipBlock>(a, pc, a.coef[pc.group], threadIdx.x);
+    const int i = a.n_pieces - 1 - (int)blockIdx.x;
+    const ClipPiece pc = a.pieces[i];
+    const float2 c = a.coef[pc.group];
+    if (i < a.streamed) scale_piece<kClipBlock, true, true>(a, pc, c, threadIdx.x);
+    else scale_piece<kClipBlock, false, true>(a, pc, c, threadIdx.x);
 }
 
 // Both passes over a small set in one block, a wave to a piece.
 template <int KIND>
-__global__ __launch_bounds__(1024) void clip_small_kernel(ClipArgs a, int scale) {
+__global__ __launch_bounds__(kClipSmallWaves * 64) void clip_small_kernel(ClipArgs a, int scale) {
     __shared__ double sums[kClipSmallPieces];
-    constexpr int kW = 16;
+    constexpr int kW = kClipSmallWaves;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     for (int i = wave; i < a.n_pieces; i += kW) {
-        const double v = wave_reduce<KIND>(sum_of<KIND, 64>(a, a.pieces[i], lane));
+        const double v = wave_reduce<KIND>(sum_of<KIND, 64, false>(a, a.pieces[i], lane));
         if (lane == 0) sums[i] = v;
     }
     __syncthreads();
@@ -291,7 +305,7 @@ __global__ __launch_bounds__(1024) void clip_small_kernel(ClipArgs a, int scale)
     __syncthreads();
     for (int i = wave; i < a.n_pieces; i += kW) {
         const ClipPiece pc = a.pieces[i];
-        scale_piece<64>(a, pc, a.coef[pc.group], lane);
+        scale_piece<64, false, false>(a, pc, a.coef[pc.group], lane);
     }
 }
 
@@ -317,7 +331,7 @@ hipError_t launch_clip_norm(const ClipArgs& a, int kind, hipStream_t s) {
 }
 
 hipError_t launch_clip_small(const ClipArgs& a, int kind, bool scale, hipStream_t s) {
-    const dim3 grid(1), block(1024);
+    const dim3 grid(1), block(kClipSmallWaves * 64);
     const int sc = scale ? 1 : 0;
     switch (kind) {
         case AGS_CLIP_L2: hipLaunchKernelGGL(clip_small_kernel<AGS_CLIP_L2>, grid, block, 0, s, a, sc); break;

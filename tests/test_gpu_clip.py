@@ -348,3 +348,36 @@ def test_host_memory_and_short_allocations_are_refused():
         clip.ags_clip_norm(h, (ctypes.c_void_p * 1)(small.data_ptr() + 2), norms.data_ptr())
     assert e.value.status == ags.AGS_E_ALIGN
     clip.ags_clip_destroy(h)
+
+
+@pytest.mark.parametrize("sizes,src,dst,shift", [
+    ([45_000_001], "f32", "bf16", 1), ([80_000_003], "bf16", "bf16", 3), ([40_000_007], "f32", None, 0),
+    ([1_500_001] * 31, "f32", "f32", 2), ([8191, 8193, 70_000_001, 77], "bf16", "f32", 1)],
+    ids=["one", "one-bf16", "in-place", "many", "uneven"])
+def test_sets_larger_than_the_caches(sizes, src, dst, shift):
+    # past 128 MiB the front is read and written past the caches; the sums of
+    # the check are fp64 on the device
+    xs = [rand(n, src, seed=i) for i, n in enumerate(sizes)]
+    norm = math.sqrt(math.fsum(float((x.double() ** 2).sum()) for x in xs))
+    offsets = np.cumsum([shift] + sizes[:-1])
+    kept = [x.clone() for x in xs]
+    if dst is None:
+        h = clip.GradClip.for_tensors(xs)
+        got = h.clip(xs, 3.0)
+        outs = xs
+    else:
+        total = shift + sum(sizes)
+        row = torch.full((total,), 7.0, device="cuda", dtype=DT[dst])
+        h = clip.GradClip([(n, i, 0, 0, 0, int(o)) for i, (n, o) in enumerate(zip(sizes, offsets))], sizes,
+                          [src] * len(sizes), [total], [dst])
+        got = h.clip(xs, 3.0, [row])
+        outs = [row[o:o + n] for n, o in zip(sizes, offsets)]
+        assert bool((row[:shift] == 7.0).all())
+    check_norms(got, [norm])
+    c = min(1.0, 3.0 / (norm + 1e-6))
+    for x, y in zip(kept, outs):
+        want = x.double() * c
+        err = (y.double() - want).abs()
+        kind = dst or src
+        assert bool((err <= (ROUND[kind] + 2.0 ** -24 + 2.0 ** -40) * want.abs() + LEAST[kind]).all())
+    h.close()
