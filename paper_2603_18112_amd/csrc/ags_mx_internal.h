@@ -51,10 +51,11 @@ struct MxShape {
 };
 
 // The kernel for few rows reads x's codes from the caches once for each 16 rows
-// of w, so beyond 16 rows it is for small products only: 32 rows 4096 x 4096
-// 9.8 us against 14.3 in tiles of 64 x 64 (which need a second launch to join
-// the parts), 24 rows 4096 x 25088 19.5 against 16.6, 32 rows 16384 x 16384
-// 50.7 against some 38.
+// of w, so beyond 16 rows it is for small products only.  Against tiles of 64 x
+// 64 in parts with the launch that joins them, kernels' times in us: 32 rows
+// 4096 x 4096 9.8 against 14.3, 24 rows 4096 x 25088 20.3 against 21.8 (from the
+// caches 19.3 against 17.6), 20 rows 16384 x 16384 45 against 42, 32 rows 51
+// against 38.
 inline bool mx_few(int64_t m, int64_t n, int64_t kp) { return m <= 16 || (m <= 32 && n * kp <= ((int64_t)1 << 26)); }
 
 // Does ags_mx_linear take x to 4 bits in the product's kernel?  Every block

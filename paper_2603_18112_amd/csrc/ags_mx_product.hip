@@ -4,8 +4,8 @@
 //                   256 elements of the contracted axis go from memory straight
 //                   into LDS while the matrix cores work on the stage before.
 // mx_join_kernel    adds the partial sums of a contracted axis cut in parts.
-// mx_few_kernel     few rows (tokens): a block of sixteen waves takes 16 rows
-//                   of the weights, the waves share the contracted axis.
+// mx_few_kernel     few rows (tokens): a block of eight waves takes 16 rows of
+//                   the weights, the waves share the contracted axis.
 #include <algorithm>
 #include <type_traits>
 
@@ -404,11 +404,26 @@ __global__ __launch_bounds__(256) void mx_join_kernel(MxProductArgs a) {
 
 // Up to 16 * MT rows of x against all of w: every weight is read once, straight
 // into registers, so the kernel is bound by the weights' bytes.  A block takes
-// 16 rows of w; of each 16 chunks of 256 columns a wave takes one; the waves'
-// sums meet in LDS, in a fixed order.  T: x's type where the block takes up to
-// 16 rows of x to 4 bits itself (each block anew: one launch instead of two,
-// for few elements of x), or void where x is stored already.
-constexpr int kFewWaves = 16;
+// 16 rows of w; of each kFewWaves chunks of 256 columns a wave takes one; the
+// waves' sums meet in LDS, in a fixed order.  A wave's loads are of whole lines,
+// 8 rows of 128 bytes: as an operand the 16 lanes r then hold rows r / 2, the
+// even ones the first half of a chunk and the odd ones the second.  Products
+// with both halves of x are taken, and of their results the rows that met their
+// own half: twice the matrix instructions, which wait for memory anyway.  (With
+// 16 rows of 64 bytes a load, each line was asked for twice.)  T: x's type where
+// the block takes up to 16 rows of x to 4 bits itself (each block anew: one
+// launch instead of two, for few elements of x), or void where x is stored
+// already.
+//
+// MI355X, weights not in the caches: 1 row 4096 x 4096 5.4 us, 16384 x 16384 28.7
+// (5.0 TB/s; 31.1 with half lines and 16 waves), 1 row 4096 x 25088 14.5, 16 rows
+// 17.7; from the caches 4.4, 26.4, 10.3, 14.5.  Tried: 16 waves a block (5.3,
+// 28.8, 14.0, 18.3; from the caches slower), 8 or 32 rows of w a block (15.3 and
+// 17.8 for 1 x 4096 x 25088), 2 to 4 chunks of a wave under way, blocks that stay
+// for several groups of rows (29 for 16384 x 16384, 16 and 21 for 4096 x 25088),
+// loads past the caches (26.8 for 16384 x 16384, but 12.4 against 10.3 for 4096 x
+// 25088 once the weights are cached).
+constexpr int kFewWaves = 8;
 
 struct FewX {
     const void* x;  // x, or its codes
@@ -435,8 +450,6 @@ __device__ __forceinline__ unsigned store32(const T* p, int64_t left, uint4* cod
     return b;
 }
 
-// One chunk of a wave is in flight at a time: with four, for which one block
-// fits a CU instead of two, 1 row took 30 us instead of 26 (16384 x 16384).
 template <int MT, typename T>
 __device__ __forceinline__ void few_rows(const MxProductArgs& a, const FewX& fx) {
     constexpr bool kStore = !std::is_void<T>::value;
@@ -459,59 +472,78 @@ __device__ __forceinline__ void few_rows(const MxProductArgs& a, const FewX& fx)
         }
         __syncthreads();
     }
-    // Lane l holds row r = l % 16 of both operands; it takes the pieces 2 q and
-    // 2 q + 1 of a chunk, q = l / 16, so that their scales are neighbours.
-    const int64_t n0 = (int64_t)blockIdx.x * 16, row = min(n0 + r, a.n - 1), pitch = a.kp / 2;
-    const uint8_t* pw = a.b + row * pitch + q * 32;
+    const int64_t n0 = (int64_t)blockIdx.x * 16, pitch = a.kp / 2;
     const int64_t pb = mx_scale_rows(a.n) * 8, pa = mx_scale_rows(a.m) * 8;
-    const uint8_t* pe = a.sb + row * 8 + q * 2;
-    v4f acc[MT];
+    const uint8_t *pw[2], *pe[2];  // of rows 0 .. 7 and 8 .. 15
 #pragma unroll
-    for (int t = 0; t < MT; ++t) acc[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int i = 0; i < 2; ++i) {
+        const int64_t row = min(n0 + i * 8 + (r >> 1), a.n - 1);
+        const int piece = (r & 1) * 4 + q;
+        pw[i] = a.b + row * pitch + piece * 16;
+        pe[i] = a.sb + row * 8 + piece;
+    }
+    v4f acc[MT][2][2];  // [rows of w][half of x]
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) acc[t][i][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     for (int c = w; c < chunks; c += kFewWaves) {
-        const uint4 w0 = *reinterpret_cast<const uint4*>(pw + (int64_t)c * 128);
-        const uint4 w1 = *reinterpret_cast<const uint4*>(pw + (int64_t)c * 128 + 16);
-        const int we = *reinterpret_cast<const uint16_t*>(pe + c * pb);
+        uint4 wv[2];
+        int we[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            wv[i] = *reinterpret_cast<const uint4*>(pw[i] + (int64_t)c * 128);
+            we[i] = pe[i][c * pb];
+        }
         uint4 xv[MT][2] = {};
-        int xw[MT] = {};
+        int xw[MT][2] = {};
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
             const int xr = t * 16 + r;
             if (xr >= m) continue;  // rows past the end multiply zeros
-            if constexpr (kStore) {
-                const int at = c * m + xr;
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    xv[t][j] = *reinterpret_cast<const uint4*>(&xs[at * 128 + (((q * 2 + j) ^ ((xr >> 1) & 7)) << 4)]);
-                xw[t] = *reinterpret_cast<const uint16_t*>(&xe[at * 8 + q * 2]);
-            } else {
-                const uint8_t* p = static_cast<const uint8_t*>(fx.x) + xr * pitch + (int64_t)c * 128 + q * 32;
-                xv[t][0] = *reinterpret_cast<const uint4*>(p);
-                xv[t][1] = *reinterpret_cast<const uint4*>(p + 16);
-                xw[t] = *reinterpret_cast<const uint16_t*>(fx.scales + c * pa + xr * 8 + q * 2);
+            for (int j = 0; j < 2; ++j) {
+                const int piece = j * 4 + q;
+                if constexpr (kStore) {
+                    const int at = c * m + xr;
+                    xv[t][j] = *reinterpret_cast<const uint4*>(&xs[at * 128 + ((piece ^ ((xr >> 1) & 7)) << 4)]);
+                    xw[t][j] = xe[at * 8 + piece];
+                } else {
+                    xv[t][j] = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(fx.x) + xr * pitch +
+                                                               (int64_t)c * 128 + piece * 16);
+                    xw[t][j] = fx.scales[c * pa + xr * 8 + piece];
+                }
             }
         }
 #pragma unroll
-        for (int t = 0; t < MT; ++t) {
-            acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(w0), operand(xv[t][0]), acc[t], kFp4, kFp4, 0,
-                                                                      we, 0, xw[t]);
-            acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(w1), operand(xv[t][1]), acc[t], kFp4, kFp4, 1,
-                                                                      we, 1, xw[t]);
-        }
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    acc[t][i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+                        operand(wv[i]), operand(xv[t][j]), acc[t][i][j], kFp4, kFp4, 0, we[i], 0, xw[t][j]);
     }
+    // A lane's four results are of operand rows 4 q .. 4 q + 3: rows 2 q and
+    // 2 q + 1 of w, by halves.
 #pragma unroll
     for (int t = 0; t < MT; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) red[w][t][i][lane] = acc[t][i];
+        for (int i = 0; i < 2; ++i) {
+            red[w][t][2 * i][lane] = acc[t][i][0][0] + acc[t][i][1][1];
+            red[w][t][2 * i + 1][lane] = acc[t][i][0][2] + acc[t][i][1][3];
+        }
     __syncthreads();
-    // Element (t, i, l): row 16 t + l % 16 of x, column 4 (l / 16) + i.
+    // Element (t, i, l): row 16 t + l % 16 of x, column 8 (i / 2) + 2 (l / 16) + i % 2.
     const Out o = output_of(a, 0);
     for (int e = tid; e < MT * 256; e += kFewWaves * 64) {
         const int t = e >> 8, l = (e >> 2) & 63, i = e & 3;
         float v = 0.0f;
 #pragma unroll
         for (int k = 0; k < kFewWaves; ++k) v += red[k][t][i][l];
-        const int64_t xr = t * 16 + (l & 15), col = n0 + (l >> 4) * 4 + i;
+        const int64_t xr = t * 16 + (l & 15), col = n0 + (i >> 1) * 8 + (l >> 4) * 2 + (i & 1);
         if (xr < a.m && col < a.n) store1(o, xr * o.stride + col, v);
     }
 }
