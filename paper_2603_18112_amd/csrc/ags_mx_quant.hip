@@ -8,8 +8,18 @@
 //                    through LDS, a thread takes 32 rows of a column.
 // mx_dequant_kernel  8 codes a thread.
 //
-// All stream from HBM and use no matrix cores.  Rows may start anywhere: the
-// 16-byte accesses below need their element's alignment only.
+// A block's scale is an integer maximum of fp32 bit patterns; codes come from the
+// converter instructions.  All stream from HBM and use no matrix cores.  Rows may
+// start anywhere: the 16-byte accesses below need their element's alignment only.
+//
+// MI355X, 8192 x 8192, data from memory (from the caches as far as they go): along
+// rows bf16 34 us, 5.0 TB/s (29), fp32 53, 5.7 TB/s (49), bf16 with random bytes
+// 50 (42); along columns bf16 39 (31); both forms bf16 50 (40), with random bytes
+// 78 (66), fp32 68 (63) and 86 (85); reading back to bf16 32 (26).  With random
+// bytes both forms are bound by the converter's work as much as by memory: fp32
+// moves half as much again and takes 8 us longer.  Tried: loads past the caches
+// (bf16 both 46, but 45 against 40 from the caches), the columns read 4 at a time
+// from LDS (58.7 against 57.5).
 #include "ags_mx_device.h"
 #include "ags_mx_internal.h"
 
@@ -131,10 +141,16 @@ __global__ __launch_bounds__(kTBlock) void mx_transpose_kernel(MxQuantArgs a, un
     uint8_t *const codes = reinterpret_cast<uint8_t*>(tile), *const col_scale = codes + kTile * kCodePitch;
     static_assert(kTile * (kCodePitch + 4) <= (int)sizeof(tile), "codes and scales fit");
     // Consecutive blocks go to the 8 XCDs in turn; each XCD takes a run of
-    // tiles, so that both halves of a line of codes meet in one L2.
+    // squares of four tiles (padded sizes are multiples of two), so that the
+    // halves of a line of codes, which neighbouring tiles write in either form,
+    // meet in one L2.  Tile after tile along the rows, the halves of the columns'
+    // lines went to memory apart: 8192 x 8192 bf16 from memory 57 against 50 us,
+    // with random bytes 86 against 78, fp32 93 against 86.
     const unsigned xcd = blockIdx.x % kXcds, base = tiles / kXcds, rest = tiles % kXcds;
     const unsigned t = xcd * base + min(xcd, rest) + blockIdx.x / kXcds;
-    const int64_t r0 = (int64_t)(t / tiles_c) * kTile, c0 = (int64_t)(t % tiles_c) * kTile;
+    const unsigned square = t / 4, squares_c = tiles_c / 2;
+    const int64_t r0 = (int64_t)(square / squares_c * 2 + (t >> 1 & 1)) * kTile;
+    const int64_t c0 = (int64_t)(square % squares_c * 2 + (t & 1)) * kTile;
     const int tid = threadIdx.x;
     const int64_t kp = (int64_t)tiles_c * kTile;
 
