@@ -59,9 +59,11 @@ struct MxShape {
 inline bool mx_few(int64_t m, int64_t n, int64_t kp) { return m <= 16 || (m <= 32 && n * kp <= ((int64_t)1 << 26)); }
 
 // Does ags_mx_linear take x to 4 bits in the product's kernel?  Every block
-// does so then; it keeps x in LDS.
-inline bool mx_linear_fused(int64_t rows, int64_t k) { return rows <= 16 && rows * k <= 16384; }
-
+// does so then; it keeps x in LDS.  One launch against two, us a call bound by
+// the host / in a graph: 1 row 4096 x 4096 9.0 / 3.8 against 13.1 / 5.2, 8 rows
+// (32768 elements of x) 9.0 / 5.3 against 13.3 / 5.9, 16 rows (65536) 9.1 / 7.3
+// against 13.4 / 6.4; 1 row 16384 x 16384 in a graph 28.0 against 30.1.
+inline bool mx_linear_fused(int64_t rows, int64_t k) { return rows <= 16 && rows * k <= 32768; }
 
 // The tile and the split with the least estimated time in us.  A stage (256
 // columns) of a tile of 64, 128 or 256 squared takes 0.55, 0.68 or 1.35 on an

@@ -81,8 +81,10 @@ constexpr int kXcds = 8;
 
 // Consecutive blocks go to the 8 XCDs in turn.  Each XCD takes a run of
 // consecutive tiles, and tiles are numbered in bands of kBand rows, so the
-// blocks that share an XCD's L2 read few rows and few columns.
-constexpr unsigned kBand = 8;
+// blocks that share an XCD's L2 read few rows and few columns.  8192^3 bf16 / fp32
+// results, bands of 1, 4, 8, 16, 64: 265 / 311, 252 / 269, 252 / 276, 258 / 285,
+// 271 / 312 us.
+constexpr unsigned kBand = 4;
 
 __device__ __forceinline__ void tile_of_block(unsigned block, unsigned tm, unsigned tn, unsigned& i, unsigned& j) {
     const unsigned total = tm * tn, xcd = block % kXcds, at = block / kXcds;
@@ -116,7 +118,6 @@ __device__ __forceinline__ void block_barrier() {
     asm volatile("" ::: "memory");
 }
 
-// TM x TN: the tile in units of 64; four waves, two by two.
 // 32 rows of BYTES bytes from LDS (PITCH apart) to memory, those of the first
 // `rows` rows and `bytes` bytes.  T: the elements, whose alignment is all that
 // the 16-byte accesses to memory need.
@@ -168,6 +169,20 @@ __device__ __forceinline__ void store_added(const Out& o, const char* strip, int
     }
 }
 
+// TM x TN: the tile in units of 64; four waves, two by two, each with TM x TN
+// fragments of 32 x 32.
+//
+// With 256 x 256 outputs a block does 256 operations for each byte of codes it
+// loads, so the matrix cores are the bound: pure 32 x 32 x 64 instructions on
+// random codes reach 6.36 PFLOP/s here, where the card's power limit holds the
+// clock to 1.5 GHz (9.6 on zeros).  MI355X, long runs: 8192^3 to bf16 252 us, 4.4
+// PFLOP/s, to fp32 269, 4.1; 4096 x 4096 x 16384 125, 4.4; 16384 x 4096 x 4096 147,
+// 3.7; 4096^3 39, 3.5; 2048^3 9.7, 1.8.  Of 8192^3's 252 the loads of codes and
+// scales cost 45 (without those in the loop 204, timed on a copy) and the stores
+// 12 (to fp32 44).  Tried: 16 x 16 x 128 instructions (7.2 PFLOP/s alone, but the
+// accumulators were moved about: 259), eight waves (276), stages of 128 columns
+// four deep (270), stores past the caches (248 against 244), blocks that stay
+// for several tiles (268).
 template <int TM, int TN>
 __device__ __forceinline__ void tile_product(const MxProductArgs& a, unsigned tiles_m, unsigned tiles_n) {
     constexpr int BM = 64 * TM, BN = 64 * TN;

@@ -396,3 +396,21 @@ def test_refusals():
     with pytest.raises(ags.AGSError) as e:
         mx.ags_mx_quantize(host.data_ptr(), ags.AGS_F32, 4, 64, 64, None, 0, q.c, None)
     assert e.value.status == ags.AGS_E_ARG
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,n,k", [(16, 40, 2048), (16, 40, 2049), (17, 40, 1900), (1, 33, 32768), (1, 33, 32769),
+                                   (3, 7, 10922), (3, 9, 10923), (15, 23, 31), (16, 8, 1)])
+def test_few_rows_either_side_of_one_launch(m, n, k, dtype):
+    # and a NaN and an infinity, which reach the results of their blocks alone
+    x, w = rand(m, k, dtype, 4), rand(n, k, "f32", 5)
+    x[m // 2, k // 3] = float("nan")
+    w[n - 1, k - 1] = float("inf")
+    y = mx.linear(x, mx.Weight(w, backward=False))
+    vx, vw = ref.store_rows(f64(x))[0], ref.store_rows(f64(w))[0]
+    bad = np.zeros((m, n), bool)
+    bad[m // 2], bad[:, n - 1] = True, True
+    got = f64(y)
+    assert np.array_equal(np.isnan(got), bad)
+    vx[m // 2], vw[n - 1] = 0.0, 0.0
+    check_close(torch.from_numpy(np.where(bad, 0.0, got)), vx, vw, dtype, k)
