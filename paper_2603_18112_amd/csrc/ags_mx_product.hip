@@ -81,10 +81,13 @@ constexpr int kXcds = 8;
 
 // Consecutive blocks go to the 8 XCDs in turn.  Each XCD takes a run of
 // consecutive tiles, and tiles are numbered in bands of kBand rows, so the
-// blocks that share an XCD's L2 read few rows and few columns.  8192^3 bf16 / fp32
-// results, bands of 1, 4, 8, 16, 64: 265 / 311, 252 / 269, 252 / 276, 258 / 285,
-// 271 / 312 us.
-constexpr unsigned kBand = 4;
+// blocks that share an XCD's L2 read few rows and few columns.  8192^3 to bf16 /
+// fp32, bands of 1, 4, 6, 8, 16, 64: 265 / 311, 252 / 269, 252 / 268, 252 / 276,
+// 258 / 285, 271 / 312 us; a linear layer's step of that size, three products
+// after the storing kernels, bands of 3, 4, 5, 6, 7, 8, 10: 920, 951, 924, 926,
+// 913, 957, 934 (and 4096 x 4096 x 16384's backward 364, 361, 360, 359, 364, 373,
+// 366): where bands divide the rows evenly the XCDs keep step with each other.
+constexpr unsigned kBand = 6;
 
 __device__ __forceinline__ void tile_of_block(unsigned block, unsigned tm, unsigned tn, unsigned& i, unsigned& j) {
     const unsigned total = tm * tn, xcd = block % kXcds, at = block / kXcds;
@@ -176,7 +179,7 @@ __device__ __forceinline__ void store_added(const Out& o, const char* strip, int
 // loads, so the matrix cores are the bound: pure 32 x 32 x 64 instructions on
 // random codes reach 6.36 PFLOP/s here, where the card's power limit holds the
 // clock to 1.5 GHz (9.6 on zeros).  MI355X, long runs: 8192^3 to bf16 252 us, 4.4
-// PFLOP/s, to fp32 269, 4.1; 4096 x 4096 x 16384 125, 4.4; 16384 x 4096 x 4096 147,
+// PFLOP/s, to fp32 268, 4.1; 4096 x 4096 x 16384 125, 4.4; 16384 x 4096 x 4096 148,
 // 3.7; 4096^3 39, 3.5; 2048^3 9.7, 1.8.  Of 8192^3's 252 the loads of codes and
 // scales cost 45 (without those in the loop 204, timed on a copy) and the stores
 // 12 (to fp32 44).  Tried: 16 x 16 x 128 instructions (7.2 PFLOP/s alone, but the
