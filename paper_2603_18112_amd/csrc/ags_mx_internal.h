@@ -50,13 +50,19 @@ struct MxShape {
     int32_t tm, tn, splits, few;
 };
 
-// The kernel for few rows reads x's codes from the caches once for each 16 rows
-// of w, so beyond 16 rows it is for small products only.  Against tiles of 64 x
-// 64 in parts with the launch that joins them, kernels' times in us: 32 rows
-// 4096 x 4096 9.8 against 14.3, 24 rows 4096 x 25088 20.3 against 21.8 (from the
-// caches 19.3 against 17.6), 20 rows 16384 x 16384 45 against 42, 32 rows 51
-// against 38.
-inline bool mx_few(int64_t m, int64_t n, int64_t kp) { return m <= 16 || (m <= 32 && n * kp <= ((int64_t)1 << 26)); }
+// The kernel for few rows is one launch with no parts to join, but reads x's
+// codes from the caches once for each 16 rows of w and waits for memory chunk by
+// chunk; the tiles load ahead.  Against tiles of 64 squared, with the launch that
+// joins their parts (in brackets) where those are faster, weights from memory,
+// kernels' times in us: 8 rows 4096 x 4096 4.7 against 7.4, 16 rows 5.2 / 7.3, 32
+// rows 6.5 / 7.4; 16 rows 4096 x 25088 16.0 / 12.8 (+ 4.0), 32 rows 22.3 / 13.0
+// (+ 3.9); 16 rows 1000 x 4096 4.6 / 7.2, 32 rows 5.8 / 7.2; where w's rows make
+// tiles for every CU, 1 row 16384 x 16384 28.5 / 32.6, 8 rows 32.9 / 32.2, 16 rows
+// 35.6 / 31.8, 32 rows 50 / 32.3; 16 rows 16384 x 4096 13.7 / 9.8.
+inline bool mx_few(int64_t m, int64_t n, int64_t kp) {
+    if (n >= 8192) return m <= 8;
+    return m <= 16 || (m <= 32 && n * kp <= ((int64_t)1 << 24));
+}
 
 // Does ags_mx_linear take x to 4 bits in the product's kernel?  Every block
 // does so then; it keeps x in LDS.  One launch against two, us a call bound by
@@ -66,18 +72,20 @@ inline bool mx_few(int64_t m, int64_t n, int64_t kp) { return m <= 16 || (m <= 3
 inline bool mx_linear_fused(int64_t rows, int64_t k) { return rows <= 16 && rows * k <= 32768; }
 
 // The tile and the split with the least estimated time in us.  A stage (256
-// columns) of a tile of 64, 128 or 256 squared takes 0.55, 0.68 or 1.35 on an
-// idle CU (1.9 with all CUs at work, at the clock the power limit leaves);
-// four small tiles on a CU take twice as long as one, two of the middle ones
-// as long as one after the other; prologue and epilogue 2, 3 or 5; a split
-// costs the launch that joins the parts (5) and their bytes at 4 TB/s.
-// Measured against every shape and split (bf16 results, us): 64 x 4096 x 4096
-// small 10.2, middle 12.7, in two parts 14.4; 64 x 16384 x 16384 small 38.2, in
-// two parts 29.3, in three 30.4; 256 x 4096 x 25088 small 53.4, middle in four
-// parts 30.3, large in eight 36.0; 1024 x 4096 x 4096 small 18.4, middle 16.1,
-// large 25.0; 2048 x 4096 x 4096 32.5, 24.7, 28.6; 100 x 500 x 20000 small 26.7,
-// in six parts 14.7.  256 x 128 tiles were not the fastest anywhere by more
-// than a twentieth.
+// columns) of a tile of 64 squared takes 0.26 on a CU, and as much for each
+// further one on it; of 128 squared 0.45 where half the CUs have none, 0.65
+// where all do, 0.68 for each of more; of 256 squared 1.35, or 1.9 with all CUs
+// at work, at the clock the power limit leaves; prologue and epilogue 2.5, 3 or
+// 5; a split costs the launch that joins the parts (5) and their bytes at 4 TB/s.
+// Measured against every shape and split (bf16 results, us, small / middle /
+// large, in their best number of parts if it is not one): 64 x 4096 x 4096 7.8 /
+// 11.1 / 17.7 in four; 64 x 16384 x 16384 23.6 / 31.9 in two / 43.6 in four; 24 x
+// 4096 x 25088 14.9 in four (27.1 in one) / 17.2 in six / 26.7; 256 x 4096 x 25088
+// 29.7 / 28.6 in three / 37.1; 500 x 500 x 20000 13.7 in four (22.6 in one) / 16.1
+// in eight / 27; 512 x 4096 x 8192 18.3 / 20.2 / 32.1; 1024 x 4096 x 4096 18.8 /
+// 14.5 / 27.8; 1500 x 1500 x 6000 19.0 / 17.6 / 31.2; 2048 x 4096 x 4096 33.9 /
+// 25.8 / 31.2; 3000 cubed 32.7 / 29.1 / 26.2; 4096 x 4096 x 1024 25.5 / 21.0 /
+// 18.5.  256 x 128 tiles were not the fastest anywhere by more than a twentieth.
 inline MxShape mx_product_plan(int64_t m, int64_t n, int64_t kp) {
     if (mx_few(m, n, kp)) return MxShape{1, 1, 1, 1};
     MxShape best{1, 1, 1, 0};
@@ -89,8 +97,8 @@ inline MxShape mx_product_plan(int64_t m, int64_t n, int64_t kp) {
             if (s > 1 && stages < 4 * s) break;
             const double load = tiles * s / 256;  // blocks of a CU
             double us = stages / s;
-            if (t == 1) us = us * 0.55 * std::max(1.0, 0.5 * load) + 2 * std::max(1.0, load / 4);
-            else if (t == 2) us = us * 0.68 * std::max(1.0, load) + 3 * std::max(1.0, load / 2);
+            if (t == 1) us = us * 0.26 * std::max(1.0, load) + 2.5 * std::max(1.0, load / 4);
+            else if (t == 2) us = us * (load > 1 ? 0.68 * load : load > 0.5 ? 0.65 : 0.45) + 3 * std::max(1.0, load / 2);
             else us = (us * (load > 0.75 ? 1.9 : 1.35) + 5) * std::max(1.0, std::ceil(load));
             if (s > 1) us += 5 + 8e-6 * (double)m * (double)n / 4 * s;
             if (us < least) {

@@ -2,7 +2,7 @@
 //
 // mx_tile_kernel    a block of four waves takes a tile of the output; stages of
 //                   256 elements of the contracted axis go from memory straight
-//                   into LDS while the matrix cores work on the stage before.
+//                   into LDS while the matrix cores work on those before.
 // mx_join_kernel    adds the partial sums of a contracted axis cut in parts.
 // mx_few_kernel     few rows (tokens): a block of eight waves takes 16 rows of
 //                   the weights, the waves share the contracted axis.
@@ -114,7 +114,11 @@ __device__ __forceinline__ void load_lds4(__amdgpu_buffer_rsrc_t r, unsigned to,
                  : "memory");
 }
 
-__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// Waits until at most N of this wave's loads are under way.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
 __device__ __forceinline__ void block_barrier() {
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
@@ -180,13 +184,14 @@ __device__ __forceinline__ void store_added(const Out& o, const char* strip, int
 // random codes reach 6.36 PFLOP/s here, where the card's power limit holds the
 // clock to 1.5 GHz (9.6 on zeros).  MI355X, long runs: 8192^3 to bf16 252 us, 4.4
 // PFLOP/s, to fp32 268, 4.1; 4096 x 4096 x 16384 125, 4.4; 16384 x 4096 x 4096 148,
-// 3.7; 4096^3 39, 3.5; 2048^3 9.7, 1.8.  Of 8192^3's 252 the loads of codes and
+// 3.7; 4096^3 39, 3.5; 2048^3 9.7, 1.8; in 64 squared 64 x 16384 x 16384 23.5 us, bound
+// by the weights' bytes (6.2 TB/s).  Of 8192^3's 252 the loads of codes and
 // scales cost 45 (without those in the loop 204, timed on a copy) and the stores
 // 12 (to fp32 44).  Tried: 16 x 16 x 128 instructions (7.2 PFLOP/s alone, but the
 // accumulators were moved about: 259), eight waves (276), stages of 128 columns
 // four deep (270), stores past the caches (248 against 244), blocks that stay
 // for several tiles (268).
-template <int TM, int TN>
+template <int TM, int TN, int NB>
 __device__ __forceinline__ void tile_product(const MxProductArgs& a, unsigned tiles_m, unsigned tiles_n) {
     constexpr int BM = 64 * TM, BN = 64 * TN;
     constexpr int kStage = (BM + BN) * 128, kBuf = kStage + (BM + BN) * 8;
@@ -249,10 +254,6 @@ __device__ __forceinline__ void tile_product(const MxProductArgs& a, unsigned ti
             else load_lds4(rs, to, vs[t], off);
         }
     };
-    auto load_stage = [&](int s, int buf) {
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) load_one(i, s, buf);
-    };
 
     // Operands: lane l holds row r = l % 32 of a fragment; its half h = l / 32
     // takes the pieces 4 h + j of a stage in step j of four (the order of the
@@ -303,8 +304,8 @@ __device__ __forceinline__ void tile_product(const MxProductArgs& a, unsigned ti
     __builtin_amdgcn_sched_barrier(0);
 
     // A stage's loads are spread over the steps in which its buffer is free
-    // and time is left for them to arrive: the last step of the stage two
-    // before and the first two of the next.  sched_barrier keeps the order.
+    // and time is left for them to arrive: the last step of the stage NB before
+    // and the first two of the next.  sched_barrier keeps the order.
     constexpr int kSlots = 3 * FM;
 #define MX_LOADS(SLOT, S, BUF)                                                                       \
     _Pragma("unroll") for (int i = (SLOT) * kLoads / kSlots; i < ((SLOT) + 1) * kLoads / kSlots; ++i) \
@@ -322,19 +323,21 @@ __device__ __forceinline__ void tile_product(const MxProductArgs& a, unsigned ti
         if ((SLOT) < 3) { MX_LOADS((SLOT) * FM + x, LOAD_STAGE, LOAD_BUF) }                           \
     }
 
-    // One stage; the operands of its first step are in registers.  Before its
-    // last step the next stage has arrived and the block's reads of this one
-    // are done, so one barrier serves both buffers.  The body has no branches,
-    // over which the compiler would move the products: past the last stage the
-    // loads find a buffer of no bytes, and operands are read that nothing uses.
+    // One stage, in buffer cur; the operands of its first step are in registers.
+    // Before its last step the next stage has arrived (those after it need not
+    // have) and the block's reads of this one are done, so one barrier serves
+    // both buffers.  The body has no branches, over which the compiler would move
+    // the products: past the last stage the loads find a buffer of no bytes, and
+    // operands are read that nothing uses.
     auto stage = [&](int s, int cur) {
-        MX_STEP(0, cur, 1, s + 1, cur ^ 1)
-        MX_STEP(1, cur, 2, s + 1, cur ^ 1)
+        const int next = (cur + 1) % NB, last = (cur + NB - 1) % NB;
+        MX_STEP(0, cur, 1, s + NB - 1, last)
+        MX_STEP(1, cur, 2, s + NB - 1, last)
         MX_STEP(2, cur, 3, 0, 0)
-        wait_loads();
+        wait_loads<(NB - 2) * kLoads>();
         block_barrier();
-        read_scales(cur ^ 1, 1);
-        MX_STEP(3, cur ^ 1, 0, s + 2, cur)
+        read_scales(next, 1);
+        MX_STEP(3, next, 0, s + NB, cur)
 #pragma unroll
         for (int f = 0; f < FM; ++f) ea[0][f] = ea[1][f];
 #pragma unroll
@@ -342,16 +345,19 @@ __device__ __forceinline__ void tile_product(const MxProductArgs& a, unsigned ti
     };
 
     if (s0 < s1) {
-        load_stage(s0, 0);
-        wait_loads();
 #pragma unroll
-        for (int x = 0; x < FM; ++x) { MX_LOADS(x, s0 + 1, 1) }
+        for (int t = 0; t < NB - 1; ++t)
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) load_one(i, s0 + t, t);
+        wait_loads<(NB - 2) * kLoads>();
+#pragma unroll
+        for (int x = 0; x < FM; ++x) { MX_LOADS(x, s0 + NB - 1, NB - 1) }
         block_barrier();
 #pragma unroll
         for (int i = 0; i < FM + FN; ++i) read_one(i, 0, 0, 0);
         read_scales(0, 0);
-        for (int s = s0, cur = 0; s < s1; ++s, cur ^= 1) stage(s, cur);
-        wait_loads();
+        for (int s = s0, cur = 0; s < s1; ++s, cur = (cur + 1) % NB) stage(s, cur);
+        wait_loads<0>();
     }
 #undef MX_STEP
 #undef MX_LOADS
@@ -403,9 +409,13 @@ __device__ __forceinline__ void tile_product(const MxProductArgs& a, unsigned ti
     }
 }
 
-template <int TM, int TN>
+// Bytes of LDS of NB stages.
+template <int TM, int TN, int NB>
+constexpr int kTileLds = NB * (64 * TM + 64 * TN) * 136;
+
+template <int TM, int TN, int NB>
 __global__ __launch_bounds__(256, 1) void mx_tile_kernel(MxProductArgs a, unsigned tiles_m, unsigned tiles_n) {
-    tile_product<TM, TN>(a, tiles_m, tiles_n);
+    tile_product<TM, TN, NB>(a, tiles_m, tiles_n);
 }
 
 __global__ __launch_bounds__(256) void mx_join_kernel(MxProductArgs a) {
@@ -578,17 +588,32 @@ hipError_t launch_few(const MxProductArgs& a, const FewX& x, hipStream_t s) {
     return hipGetLastError();
 }
 
-template <int TM, int TN>
-hipError_t launch_tile(const MxProductArgs& a, hipStream_t s) {
-    constexpr int lds = 2 * (64 * TM + 64 * TN) * 136;
-    const unsigned tm = (unsigned)((a.m + 64 * TM - 1) / (64 * TM)), tn = (unsigned)((a.n + 64 * TN - 1) / (64 * TN));
+template <int TM, int TN, int NB>
+hipError_t launch_tile(const MxProductArgs& a, unsigned tm, unsigned tn, hipStream_t s) {
+    constexpr int lds = kTileLds<TM, TN, NB>;
     if (lds > 65536) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(mx_tile_kernel<TM, TN>),
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(mx_tile_kernel<TM, TN, NB>),
                                                  hipFuncAttributeMaxDynamicSharedMemorySize, lds);
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL((mx_tile_kernel<TM, TN>), dim3(tm * tn * (unsigned)a.splits), dim3(256), lds, s, a, tm, tn);
+    hipLaunchKernelGGL((mx_tile_kernel<TM, TN, NB>), dim3(tm * tn * (unsigned)a.splits), dim3(256), lds, s, a, tm, tn);
     return hipGetLastError();
+}
+
+// Four buffers where all blocks fit the CUs at once even so; more blocks cover
+// each other's loads.  1024 x 4096 x 4096 (256 tiles of 128 squared) 14.4 us
+// against 17.0 with two, 256 x 4096 x 25088 (in four parts) 28 against 31.6,
+// 512 x 4096 x 8192 (512 tiles of 64 squared) 18.2 against 22.7; two: 2048 x 2048 x
+// 500 (1024 tiles) 7.1 against 8.6, 2048 x 4096 x 4096 (512 of 128 squared) 24.6
+// against 27.7.
+template <int T>
+hipError_t launch_tiles(const MxProductArgs& a, hipStream_t s) {
+    const unsigned tm = (unsigned)((a.m + 64 * T - 1) / (64 * T)), tn = (unsigned)((a.n + 64 * T - 1) / (64 * T));
+    if constexpr (T < 4) {
+        constexpr unsigned fit = 256u * (163840u / (unsigned)kTileLds<T, T, 4>);
+        if (tm * tn * (unsigned)a.splits <= fit) return launch_tile<T, T, 4>(a, tm, tn, s);
+    }
+    return launch_tile<T, T, 2>(a, tm, tn, s);
 }
 
 }  // namespace
@@ -598,7 +623,7 @@ hipError_t launch_mx_product(const MxProductArgs& args, hipStream_t s) {
     const MxShape p = mx_product_plan(a.m, a.n, a.kp);
     a.splits = p.splits;
     if (p.few) return launch_few(a, FewX{a.a, a.sa, 0, 0}, s);
-    hipError_t e = p.tm == 4 ? launch_tile<4, 4>(a, s) : p.tm == 2 ? launch_tile<2, 2>(a, s) : launch_tile<1, 1>(a, s);
+    hipError_t e = p.tm == 4 ? launch_tiles<4>(a, s) : p.tm == 2 ? launch_tiles<2>(a, s) : launch_tiles<1>(a, s);
     if (e == hipSuccess && a.splits > 1) {
         const unsigned blocks = (unsigned)std::min<int64_t>((a.m * a.n + 255) / 256, 4096);
         hipLaunchKernelGGL(mx_join_kernel, dim3(blocks), dim3(256), 0, s, a);

@@ -414,3 +414,12 @@ def test_few_rows_either_side_of_one_launch(m, n, k, dtype):
     assert np.array_equal(np.isnan(got), bad)
     vx[m // 2], vw[n - 1] = 0.0, 0.0
     check_close(torch.from_numpy(np.where(bad, 0.0, got)), vx, vw, dtype, k)
+
+
+@pytest.mark.parametrize("m,n,k", [
+    (9, 8200, 700), (16, 8193, 1030),                                     # few rows in tiles
+    (70, 90, 257), (70, 90, 600), (70, 90, 1100), (40, 200, 30000),       # 2, 3 and 5 stages, parts
+    (100, 17000, 300), (520, 4001, 515),                                  # more small tiles than fit at once
+    (600, 5000, 1500), (2100, 2130, 800)])                                # the middle ones, fitting and not
+def test_products_ahead_of_memory(m, n, k):
+    test_products_of_whole_numbers_are_exact(m, n, k)
