@@ -9,7 +9,9 @@ behind the C-ABI library ``libags.so`` (see ``include/ags.h``).
 
 ``paper_2603_18112_amd.ags`` is the Python binding (ctypes marshalling
 only); ``layouts`` and ``synth`` describe flat layouts and draw seeded
-synthetic inputs.
+synthetic inputs.  ``clip`` (gradient clipping, ``include/ags_clip.h``) and
+``mx`` (4-bit linear layers, ``include/ags_mx.h``) bind the operators that
+stand around the step in the same library.
 """
 
-__all__ = ["layouts", "synth", "ags"]
+__all__ = ["layouts", "synth", "ags", "clip", "mx"]
