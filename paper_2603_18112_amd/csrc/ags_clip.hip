@@ -199,26 +199,54 @@ __global__ __launch_bounds__(kClipBlock) void clip_norm_kernel(ClipArgs a) {
     }
     __syncthreads();
     if (!sh_last) return;
-    // The last block: few groups take the whole block each, many a wave each.
-    const bool by_wave = a.n_groups >= kWaves;
-    const int first = by_wave ? wave : 0, stride = by_wave ? kWaves : 1;
-    const int t = by_wave ? lane : tid, nt = by_wave ? 64 : kClipBlock;
-    for (int g = first; g < a.n_groups; g += stride) {
-        const int b = a.group_begin[g], e = a.group_begin[g + 1];
-        double s = 0.0;
-        for (int i = b + t; i < e; i += nt)
-            s = combine<KIND>(s, __hip_atomic_load(&a.partials[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
-        s = wave_reduce<KIND>(s);
-        if (by_wave) {
-            if (lane == 0) write_group<KIND>(a, g, s);
-            continue;
+    // The last block.  Few groups take the whole block one after the other; of
+    // more, those of few pieces take a lane each, those of some more 16 lanes and
+    // the others a wave.  MI355X, norms of 1000 groups of three pieces 191 us with
+    // a wave for each and 20 so, 64 groups of 49 pieces 31.7 and 24.7; one group
+    // of 4000 pieces 25.6 with the block against 36.2 with a wave.
+    auto load = [&](int i) { return __hip_atomic_load(&a.partials[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
+    if (a.n_groups < kWaves) {
+        for (int g = 0; g < a.n_groups; ++g) {
+            double s = 0.0;
+            for (int i = a.group_begin[g] + tid; i < a.group_begin[g + 1]; i += kClipBlock) s = combine<KIND>(s, load(i));
+            s = wave_reduce<KIND>(s);
+            __syncthreads();
+            if (lane == 0) sh[wave] = s;
+            __syncthreads();
+            if (tid == 0) {
+                for (int w = 1; w < kWaves; ++w) s = combine<KIND>(s, sh[w]);
+                write_group<KIND>(a, g, s);
+            }
         }
-        __syncthreads();
-        if (lane == 0) sh[wave] = s;
-        __syncthreads();
-        if (tid == 0) {
-            for (int w = 1; w < kWaves; ++w) s = combine<KIND>(s, sh[w]);
-            write_group<KIND>(a, g, s);
+    } else {
+        // Lane l of wave w looks after group base + l kWaves + w.
+        for (int base = wave; base < a.n_groups; base += 64 * kWaves) {
+            const int g = base + lane * kWaves;
+            const int b = g < a.n_groups ? a.group_begin[g] : 0, e = g < a.n_groups ? a.group_begin[g + 1] : 0;
+            if (g < a.n_groups && e - b <= 8) {
+                double s = 0.0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (b + i < e) s = combine<KIND>(s, load(b + i));
+                write_group<KIND>(a, g, s);
+            }
+            for (int wide = 0; wide < 2; ++wide) {
+                const int width = wide ? 64 : 16;
+                uint64_t todo = __ballot(wide ? e - b > 256 : e - b > 8 && e - b <= 256);
+                while (todo) {
+                    int mine = -1;  // the lane whose group this lane works on
+                    for (int k = 0; k < 64 / width && todo; ++k) {
+                        if (lane / width == k) mine = __ffsll((unsigned long long)todo) - 1;
+                        todo &= todo - 1;
+                    }
+                    const int from = __shfl(b, mine < 0 ? 0 : mine, 64), to = __shfl(e, mine < 0 ? 0 : mine, 64);
+                    double s = 0.0;
+                    if (mine >= 0)
+                        for (int i = from + lane % width; i < to; i += width) s = combine<KIND>(s, load(i));
+                    for (int off = width / 2; off >= 1; off >>= 1) s = combine<KIND>(s, __shfl_xor(s, off, 64));
+                    if (mine >= 0 && lane % width == 0) write_group<KIND>(a, base + mine * kWaves, s);
+                }
+            }
         }
     }
     if (tid <= kClipCounters) a.done[tid * kClipCounterStride] = 0u;

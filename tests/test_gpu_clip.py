@@ -381,3 +381,36 @@ def test_sets_larger_than_the_caches(sizes, src, dst, shift):
         kind = dst or src
         assert bool((err <= (ROUND[kind] + 2.0 ** -24 + 2.0 ** -40) * want.abs() + LEAST[kind]).all())
     h.close()
+
+
+@pytest.mark.parametrize("kind", ["l2", "l1", "max"])
+@pytest.mark.parametrize("n_groups", [4, 5, 70, 300])
+def test_groups_of_few_and_many_pieces(n_groups, kind):
+    # a piece is 8192 elements, or some more for many groups: groups of 0, 1, 8, 9, 256 and 257 pieces, and
+    # of many short segments, in changing order
+    sizes = [0, 5, 8 * 8192, 8 * 8192 + 1, 256 * 8192 - 3, 256 * 8192 + 1, 31, 70_001]
+    gen = np.random.default_rng(n_groups)
+    groups = [gen.choice(len(sizes), p=[.1, .2, .2, .2, .03, .02, .15, .1]) for _ in range(n_groups)]
+    groups[:4] = [5, 4, 0, 3]
+    x = rand(2_300_000, "f32", 9)
+    seg, parts = [], [[] for _ in range(n_groups)]
+    for g, i in enumerate(groups):
+        for _ in range(1 if sizes[i] > 40 else int(gen.integers(1, 12))):
+            o = int(gen.integers(0, x.numel() - sizes[i]))
+            seg.append((sizes[i], 0, o, g))
+            parts[g].append((o, sizes[i]))
+    order = gen.permutation(len(seg))
+    h = clip.GradClip([seg[i] for i in order], [x.numel()], ["f32"], n_groups=n_groups, kind=kind)
+    got = f64(h.norm([x]))
+    d = x.double()
+    for g in range(n_groups):
+        v = [d[o:o + n] for o, n in parts[g] if n]
+        if kind == "max":
+            want = max((float(t.abs().max()) for t in v), default=0.0)
+        elif kind == "l1":
+            want = math.fsum(float(t.abs().sum()) for t in v)
+        else:
+            want = math.sqrt(math.fsum(float((t ** 2).sum()) for t in v))
+        assert abs(got[g] - want) <= 2.0 ** -23 * want, g
+    assert np.array_equal(got, f64(h.norm([x])))
+    h.close()
