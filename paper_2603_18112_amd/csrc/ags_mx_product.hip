@@ -208,10 +208,12 @@ __device__ __forceinline__ void tile_product(const MxProductArgs& a, unsigned ti
     const int s0 = (int)((int64_t)stages * split / a.splits), s1 = (int)((int64_t)stages * (split + 1) / a.splits);
     const int ma = (int)min((int64_t)BM, a.m - i0), nb = (int)min((int64_t)BN, a.n - j0);
 
-    // Buffers of the tile's rows; of no bytes for a stage past the last.
+    // Buffers of the tile's rows; of no bytes for a stage past the last, whose
+    // loads have no scalar offset either (it may be taken off the buffer's size).
     auto buffer = [&](const uint8_t* p, unsigned bytes, int s) {
         return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, s < s1 ? bytes : 0u, 0x00027000);
     };
+    auto scalar_off = [&](int s, unsigned bytes) { return s < s1 ? s * bytes : 0u; };
     const uint8_t *const ca = a.a + i0 * pitch, *const cb = a.b + j0 * pitch;
     const unsigned pa = (unsigned)mx_scale_rows(a.m) * 8, pb = (unsigned)mx_scale_rows(a.n) * 8;
     const unsigned chunks = (unsigned)(a.kp / 256);
@@ -241,14 +243,16 @@ __device__ __forceinline__ void tile_product(const MxProductArgs& a, unsigned ti
     auto load_one = [&](int i, int s, int buf) {  // load i of a stage
         const unsigned p = lds0 + buf * kBuf;
         if (i < BM / 32) {
-            load_lds16(buffer(ca, ma * pitch, s), p + (i * 4 + w) * 1024, min(first + i * 32 * pitch, last_a), s * 128);
+            load_lds16(buffer(ca, ma * pitch, s), p + (i * 4 + w) * 1024, min(first + i * 32 * pitch, last_a),
+                       scalar_off(s, 128));
         } else if (i < BM / 32 + BN / 32) {
             const int t = i - BM / 32;
-            load_lds16(buffer(cb, nb * pitch, s), p + BM * 128 + (t * 4 + w) * 1024, min(first + t * 32 * pitch, last_b), s * 128);
+            load_lds16(buffer(cb, nb * pitch, s), p + BM * 128 + (t * 4 + w) * 1024, min(first + t * 32 * pitch, last_b),
+                       scalar_off(s, 128));
         } else {
             const int t = i - BM / 32 - BN / 32;
             const bool is_a = (t * 4 + w) * 64 * kScale < BM * 8;
-            const unsigned to = p + kStage + (t * 4 + w) * 64 * kScale, off = s * (is_a ? pa : pb);
+            const unsigned to = p + kStage + (t * 4 + w) * 64 * kScale, off = scalar_off(s, is_a ? pa : pb);
             const __amdgpu_buffer_rsrc_t rs = buffer(is_a ? sca : scb, is_a ? sza : szb, s);
             if (kScale == 16) load_lds16(rs, to, vs[t], off);
             else load_lds4(rs, to, vs[t], off);
