@@ -5,6 +5,7 @@ kernels of the library.
 from __future__ import annotations
 
 import ctypes
+import math
 
 from . import ags
 
@@ -137,7 +138,7 @@ def _matrix(x, what):
     if x.dim() != 2:
         if x.dim() == 0:
             raise ValueError(f"{what} needs at least one dimension")
-        x = x.reshape(-1, x.shape[-1])
+        x = x.reshape(math.prod(x.shape[:-1]), x.shape[-1])
     rows, cols = x.shape
     if cols > 1 and x.stride(1) != 1:
         raise ValueError(f"{what} must be contiguous along its last axis")

@@ -423,3 +423,16 @@ def test_few_rows_either_side_of_one_launch(m, n, k, dtype):
     (600, 5000, 1500), (2100, 2130, 800)])                                # the middle ones, fitting and not
 def test_products_ahead_of_memory(m, n, k):
     test_products_of_whole_numbers_are_exact(m, n, k)
+
+
+@pytest.mark.parametrize("shape", [(2, 3, 0), (0,), (0, 3, 0), (0, 2, 64), (64,)])
+def test_inputs_of_one_or_many_axes_with_empty_ones(shape):
+    n, k = 40, shape[-1]
+    W = mx.Weight(torch.ones(n, k, device="cuda"))
+    y, saved = mx.linear(torch.ones(shape, device="cuda"), W, save=True)
+    assert torch.equal(y, mx.linear(torch.ones(shape, device="cuda"), W))
+    assert y.shape == (*shape[:-1], n) and bool((y == k).all())
+    dx, dw = mx.linear_backward(torch.ones_like(y), saved, W)
+    rows = y.numel() // n
+    assert dx.shape == shape and dw.shape == (n, k)
+    assert bool((dx == n).all()) and bool((dw == rows).all())
