@@ -136,6 +136,8 @@ class GradClip:
         self.in_numels, self.out_numels = list(map(int, in_numels)), list(map(int, out_numels))
         self.in_dtypes = [names[d] for d in in_dtypes]
         self.out_dtypes = [names[d] for d in out_dtypes]
+        if kind not in KINDS:
+            raise ValueError(f"kind {kind!r} is not one of {sorted(KINDS)}")
         if len(self.in_numels) != len(self.in_dtypes) or len(self.out_numels) != len(self.out_dtypes):
             raise ValueError("one type for each tensor")
         self.n_groups = int(n_groups)
@@ -243,9 +245,12 @@ class GradClip:
         p = self._pointers("the gradients", tensors, self.in_numels, self.in_dtypes)
         q = None
         if out is not None:
+            if not self.out_numels:
+                raise ValueError("the handle was made without outputs")
             q = self._pointers("the outputs", out, self.out_numels, self.out_dtypes, True)
         norms = self._norms(stream)
-        ags_clip_apply(self.handle, p.buffer_info()[0], q and q.buffer_info()[0], max_norm, norms.data_ptr(), self._stream(stream))
+        ags_clip_apply(self.handle, p.buffer_info()[0], None if q is None else q.buffer_info()[0], max_norm,
+                       norms.data_ptr(), self._stream(stream))
         return norms
 
     def close(self):

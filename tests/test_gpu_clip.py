@@ -414,3 +414,15 @@ def test_groups_of_few_and_many_pieces(n_groups, kind):
         assert abs(got[g] - want) <= 2.0 ** -23 * want, g
     assert np.array_equal(got, f64(h.norm([x])))
     h.close()
+
+
+def test_arguments_that_name_nothing_are_value_errors():
+    g = [rand(100)]
+    h = clip.GradClip.for_tensors(g)
+    old = g[0].clone()
+    with pytest.raises(ValueError):
+        h.clip(g, 0.1, out=[])                       # made without outputs; no clipping in place either
+    assert torch.equal(g[0], old)
+    h.close()
+    with pytest.raises(ValueError):
+        clip.GradClip.for_tensors(g, kind="l3")
