@@ -111,6 +111,31 @@ ags_status ags_mx_linear(const void *d_x, int32_t dtype, int64_t rows, int64_t r
                          const ags_mx_tensor *w, void *d_y, int32_t y_dtype, int64_t y_stride,
                          void *d_workspace, size_t workspace_bytes, void *hip_stream);
 
+/* The same product for a training step: x is stored along its rows in the
+ * workspace and, in the same pass, transposed as `saved` [w.cols, rows], what
+ * ags_mx_linear_backward takes.  The results are bit for bit those of
+ * ags_mx_quantize and ags_mx_product. */
+ags_status ags_mx_linear_save_workspace(int64_t rows, int64_t n, int64_t k, size_t *out_bytes);
+ags_status ags_mx_linear_save(const void *d_x, int32_t dtype, int64_t rows, int64_t row_stride,
+                              const ags_mx_tensor *w, void *d_y, int32_t y_dtype, int64_t y_stride,
+                              const ags_mx_tensor *saved, void *d_workspace,
+                              size_t workspace_bytes, void *hip_stream);
+
+/* Gradients of y = x w' for dy [rows, n] (with d_noise as in
+ * ags_mx_quantize): dx [rows][dx_stride] = dy w of dy's type and
+ * dw [n][dw_stride] (+)= dy' x.  saved: x transposed, [k, rows]; wt: w
+ * transposed, [k, n], or NULL where dx is not wanted (need_dx = 0 for the
+ * workspace).  dy is stored in the workspace in both forms in one pass; the
+ * results are bit for bit those of ags_mx_quantize and ags_mx_product. */
+ags_status ags_mx_linear_backward_workspace(int64_t rows, int64_t n, int64_t k, int32_t need_dx,
+                                            size_t *out_bytes);
+ags_status ags_mx_linear_backward(const void *d_dy, int32_t dtype, int64_t rows, int64_t n,
+                                  int64_t row_stride, const uint8_t *d_noise, int64_t noise_stride,
+                                  const ags_mx_tensor *saved, const ags_mx_tensor *wt, void *d_dx,
+                                  int64_t dx_stride, void *d_dw, int32_t dw_dtype,
+                                  int64_t dw_stride, int32_t accumulate, void *d_workspace,
+                                  size_t workspace_bytes, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -11,7 +11,8 @@ from . import ags
 
 AGS_MX_BLOCK, AGS_MX_PAD, AGS_MX_ROWS = 32, 256, 16
 EXPORTS = ("ags_mx_bytes", "ags_mx_quantize", "ags_mx_dequantize", "ags_mx_product_workspace",
-           "ags_mx_product", "ags_mx_linear_workspace", "ags_mx_linear")
+           "ags_mx_product", "ags_mx_linear_workspace", "ags_mx_linear", "ags_mx_linear_save_workspace",
+           "ags_mx_linear_save", "ags_mx_linear_backward_workspace", "ags_mx_linear_backward")
 
 
 class ags_mx_tensor(ctypes.Structure):
@@ -37,6 +38,11 @@ def _lib():
             "ags_mx_product": [T, T, vp, c_int, i64, i32, vp, sz, vp],
             "ags_mx_linear_workspace": [i64, i64, i64, P(sz)],
             "ags_mx_linear": [vp, c_int, i64, i64, T, vp, c_int, i64, vp, sz, vp],
+            "ags_mx_linear_save_workspace": [i64, i64, i64, P(sz)],
+            "ags_mx_linear_save": [vp, c_int, i64, i64, T, vp, c_int, i64, T, vp, sz, vp],
+            "ags_mx_linear_backward_workspace": [i64, i64, i64, i32, P(sz)],
+            "ags_mx_linear_backward": [vp, c_int, i64, i64, i64, vp, i64, T, T, vp, i64, vp, c_int, i64, i32,
+                                       vp, sz, vp],
         }
         for name, args in sig.items():
             f = getattr(lib, name)
@@ -94,6 +100,33 @@ def ags_mx_linear(d_x, dtype, rows, row_stride, w, d_y, y_dtype, y_stride, d_wor
                   workspace_bytes=0, stream=0):
     _check(_lib().ags_mx_linear(d_x, dtype, rows, row_stride, ctypes.byref(w), d_y, y_dtype, y_stride,
                                 d_workspace, workspace_bytes, stream))
+
+
+def ags_mx_linear_save_workspace(rows: int, n: int, k: int) -> int:
+    b = ctypes.c_size_t(0)
+    _check(_lib().ags_mx_linear_save_workspace(rows, n, k, ctypes.byref(b)))
+    return b.value
+
+
+def ags_mx_linear_save(d_x, dtype, rows, row_stride, w, d_y, y_dtype, y_stride, saved, d_workspace=None,
+                       workspace_bytes=0, stream=0):
+    _check(_lib().ags_mx_linear_save(d_x, dtype, rows, row_stride, ctypes.byref(w), d_y, y_dtype, y_stride,
+                                     ctypes.byref(saved), d_workspace, workspace_bytes, stream))
+
+
+def ags_mx_linear_backward_workspace(rows: int, n: int, k: int, need_dx: int) -> int:
+    b = ctypes.c_size_t(0)
+    _check(_lib().ags_mx_linear_backward_workspace(rows, n, k, need_dx, ctypes.byref(b)))
+    return b.value
+
+
+def ags_mx_linear_backward(d_dy, dtype, rows, n, row_stride, d_noise, noise_stride, saved, wt, d_dx, dx_stride,
+                           d_dw, dw_dtype, dw_stride, accumulate=0, d_workspace=None, workspace_bytes=0,
+                           stream=0):
+    _check(_lib().ags_mx_linear_backward(d_dy, dtype, rows, n, row_stride, d_noise, noise_stride,
+                                         ctypes.byref(saved), None if wt is None else ctypes.byref(wt), d_dx,
+                                         dx_stride, d_dw, dw_dtype, dw_stride, accumulate, d_workspace,
+                                         workspace_bytes, stream))
 
 
 # ------------------------------------------------------- torch convenience --
@@ -182,6 +215,16 @@ class MX4:
         return self.rows, self.cols
 
 
+def _noise(noise, rows, cols, what):
+    """(random bytes [rows, cols] or None, their address, row stride)."""
+    if noise is None:
+        return None, None, 0
+    noise, r, c, stride = _matrix(noise, "noise")
+    if noise.dtype is not _t().uint8 or (r, c) != (rows, cols):
+        raise ValueError(f"noise must hold one uint8 for each element of {what}")
+    return noise, noise.data_ptr() or None, stride
+
+
 def _quantize(x, noise, q, qt):
     if x.dim() == 2 and x.stride(1) != 1 and x.stride(0) == 1 and x.shape[1] > 1:
         # a transposed view: the two forms change places
@@ -189,12 +232,7 @@ def _quantize(x, noise, q, qt):
         return q, qt
     x, rows, cols, stride = _matrix(x, "x")
     dt = _dtype(x.dtype)[0]
-    n_ptr, n_stride = None, 0
-    if noise is not None:
-        noise, r, c, n_stride = _matrix(noise, "noise")
-        if noise.dtype is not _t().uint8 or (r, c) != (rows, cols):
-            raise ValueError("noise must hold one uint8 for each element of x")
-        n_ptr = noise.data_ptr()
+    noise, n_ptr, n_stride = _noise(noise, rows, cols, "x")
     if q is True:
         q = MX4(rows, cols, x.device)
     if qt is True:
@@ -234,26 +272,29 @@ def _workspace(nbytes, device):
     return _t().empty(nbytes, dtype=_t().uint8, device=device) if nbytes else None
 
 
+def _output(out, rows, cols, dtype, accumulate, what, device):
+    """(tensor [rows, cols], its type's code, row stride): `out`, or a new one
+    of `dtype`."""
+    if out is None:
+        if accumulate:
+            raise ValueError(f"accumulate needs {what}")
+        code, dt = _dtype(dtype)
+        return _t().empty((rows, cols), dtype=dt, device=device), code, max(cols, 1)
+    code = _dtype(out.dtype)[0]
+    if tuple(out.shape) != (rows, cols):
+        raise ValueError(f"{what} must be [{rows}, {cols}]")
+    return out, code, max(_matrix(out, what)[3], 1)
+
+
 def product(a, b, dtype="bf16", out=None, accumulate=False):
     """a [m, k] times b' [k, n] (MX4s blocked along k): [m, n] of `dtype`, or
     written to `out` (2-D, unit column stride), added to it with
     `accumulate`."""
-    t = _t()
     dev = a.data.device
-    if out is None:
-        if accumulate:
-            raise ValueError("accumulate needs out")
-        code, dt = _dtype(dtype)
-        out = t.empty((a.rows, b.rows), dtype=dt, device=dev)
-        stride = b.rows
-    else:
-        code = _dtype(out.dtype)[0]
-        if tuple(out.shape) != (a.rows, b.rows):
-            raise ValueError(f"out must be [{a.rows}, {b.rows}]")
-        _, _, _, stride = _matrix(out, "out")
+    out, code, stride = _output(out, a.rows, b.rows, dtype, accumulate, "out", dev)
     nbytes = ags_mx_product_workspace(a.rows, b.rows, a.cols)
     ws = _workspace(nbytes, dev)
-    ags_mx_product(a.c, b.c, out.data_ptr() or None, code, max(stride, 1), int(accumulate),
+    ags_mx_product(a.c, b.c, out.data_ptr() or None, code, stride, int(accumulate),
                    None if ws is None else ws.data_ptr(), nbytes, _stream(dev))
     return out
 
@@ -292,10 +333,16 @@ def linear(x, w, dtype=None, save=False):
     x2, rows, _, stride = _matrix(x, "x")
     out_code, out_dt = _dtype(x.dtype if dtype is None else dtype)
     shape = (*x.shape[:-1], w.n)
+    dev = x.device
+    y = t.empty(shape, dtype=out_dt, device=dev)
     if save:
-        q, saved = _quantize(x2, None, True, True)
-        return product(q, w.rows, out_dt).view(shape), saved
-    y = t.empty(shape, dtype=out_dt, device=x.device)
+        saved = MX4(w.k, rows, dev)
+        nbytes = ags_mx_linear_save_workspace(rows, w.n, w.k)
+        ws = _workspace(nbytes, dev)
+        ags_mx_linear_save(x2.data_ptr() or None, _dtype(x.dtype)[0], rows, max(stride, 1), w.rows.c,
+                           y.data_ptr() or None, out_code, max(w.n, 1), saved.c,
+                           None if ws is None else ws.data_ptr(), nbytes, _stream(dev))
+        return y, saved
     nbytes = ags_mx_linear_workspace(rows, w.n, w.k)
     ws = _workspace(nbytes, x.device)
     ags_mx_linear(x2.data_ptr() or None, _dtype(x.dtype)[0], rows, max(stride, 1), w.rows.c,
@@ -314,10 +361,18 @@ def linear_backward(dy, x, w, noise=None, dw=None, dw_dtype="f32", accumulate=Fa
         raise ValueError(f"dy must have {w.n} columns")
     if need_dx and w.cols is None:
         raise ValueError("the weight has no backward form")
-    dy2, rows, _, _ = _matrix(dy, "dy")
+    dy2, rows, n, stride = _matrix(dy, "dy")
+    code, dev, k = _dtype(dy.dtype)[0], dy.device, w.k
+    noise, n_ptr, n_stride = _noise(noise, rows, n, "dy")
+    dw, dw_code, dw_stride = _output(dw, n, k, dw_dtype, accumulate, "dw", dev)
     xt = x if isinstance(x, MX4) else quantize_t(x)
-    if xt.shape != (w.k, rows):
-        raise ValueError(f"x and dy differ in rows, or x has not {w.k} columns")
-    q, qt = _quantize(dy2, noise, True if need_dx else None, True)
-    dx = product(q, w.cols, dy.dtype).view(*dy.shape[:-1], w.k) if need_dx else None
-    return dx, product(qt, xt, dw_dtype, dw, accumulate)
+    if xt.shape != (k, rows):
+        raise ValueError(f"x and dy differ in rows, or x has not {k} columns")
+    dx = _t().empty((*dy.shape[:-1], k), dtype=dy.dtype, device=dev) if need_dx else None
+    nbytes = ags_mx_linear_backward_workspace(rows, n, k, 1 if need_dx else 0)
+    ws = _workspace(nbytes, dev)
+    ags_mx_linear_backward(dy2.data_ptr() or None, code, rows, n, max(stride, 1), n_ptr, n_stride, xt.c,
+                           w.cols.c if need_dx else None, dx.data_ptr() or None if need_dx else None, max(k, 1),
+                           dw.data_ptr() or None, dw_code, dw_stride, int(accumulate),
+                           None if ws is None else ws.data_ptr(), nbytes, _stream(dev))
+    return dx, dw

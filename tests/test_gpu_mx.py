@@ -436,3 +436,47 @@ def test_inputs_of_one_or_many_axes_with_empty_ones(shape):
     rows = y.numel() // n
     assert dx.shape == shape and dw.shape == (n, k)
     assert bool((dx == n).all()) and bool((dw == rows).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,n,k", [(1, 1, 1), (5, 33, 700), (20, 640, 5000), (130, 64, 9000), (300, 700, 20), (17, 257, 4100)])
+def test_training_calls_are_the_separate_ones(m, n, k, dtype):
+    x, dy, r = rand(m, k, dtype, 1), rand(m, n, dtype, 2), noise_of(m, n)
+    W = mx.Weight(rand(n, k, "f32", 3))
+    q, qt = mx.quantize_both(x)
+    y, saved = mx.linear(x, W, save=True)
+    assert saved.shape == (k, m) and torch.equal(saved.codes, qt.codes)
+    assert torch.equal(mx.dequantize(saved), mx.dequantize(qt))
+    assert torch.equal(y, mx.product(q, W.rows, dtype))
+    for noise in (None, r):
+        d, dt = mx.quantize_both(dy, noise=noise)
+        dx, dw = mx.linear_backward(dy, saved, W, noise=noise)
+        assert dx.dtype is DT[dtype] and torch.equal(dx, mx.product(d, W.cols, dtype))
+        assert torch.equal(dw, mx.product(dt, qt, "f32"))
+        row = torch.full((2 * n * k + 7,), 2.0, device="cuda", dtype=DT[dtype])
+        none, view = mx.linear_backward(dy, saved, W, noise=noise, dw=row[5:5 + n * k].view(n, k), need_dx=False,
+                                        accumulate=True)
+        want = torch.full((n, k), 2.0, device="cuda", dtype=DT[dtype])
+        assert none is None and torch.equal(view, mx.product(dt, qt, out=want, accumulate=True))
+        assert bool((row[:5] == 2.0).all()) and bool((row[5 + n * k:] == 2.0).all())
+
+
+@pytest.mark.parametrize("m,n,k", [(40, 200, 30000), (70, 90, 1100), (3, 65, 300)])
+def test_training_calls_stay_inside_their_workspaces(m, n, k):
+    x, dy, W = rand(m, k), rand(m, n, seed=1), mx.Weight(rand(n, k, seed=2))
+    y, saved = torch.empty(m, n, device="cuda"), mx.MX4(k, m)
+    dx, dw = torch.empty(m, k, device="cuda"), torch.empty(n, k, device="cuda")
+    s = torch.cuda.current_stream().cuda_stream
+    for need, call in (
+            (mx.ags_mx_linear_save_workspace(m, n, k),
+             lambda p, b: mx.ags_mx_linear_save(x.data_ptr(), ags.AGS_F32, m, k, W.rows.c, y.data_ptr(), ags.AGS_F32, n,
+                                                saved.c, p, b, s)),
+            (mx.ags_mx_linear_backward_workspace(m, n, k, 1),
+             lambda p, b: mx.ags_mx_linear_backward(dy.data_ptr(), ags.AGS_F32, m, n, n, None, 0, saved.c, W.cols.c,
+                                                    dx.data_ptr(), k, dw.data_ptr(), ags.AGS_F32, k, 0, p, b, s))):
+        ws = torch.full((need + 8192,), 0xA5, device="cuda", dtype=torch.uint8)
+        call(ws.data_ptr() + 4096, need)
+        assert bool((ws[:4096] == 0xA5).all()) and bool((ws[4096 + need:] == 0xA5).all())
+    y2, saved2 = mx.linear(x, W, save=True)
+    dx2, dw2 = mx.linear_backward(dy, saved2, W)
+    assert torch.equal(y, y2) and torch.equal(dx, dx2) and torch.equal(dw, dw2)

@@ -155,3 +155,45 @@ def test_strides_past_any_address_space(rows, stride):
         with pytest.raises(ags.AGSError) as e:
             mx.ags_mx_quantize(X, ags.AGS_F32, rows, 64, row_stride, noise, stride, _t(rows, 64), None)
         assert e.value.status == ags.AGS_E_ARG and "stride" in str(e.value)
+
+
+def test_training_calls_refuse(lib):
+    bf, U = ags.AGS_BF16, 0x9000000000
+    save, back = mx.ags_mx_linear_save, mx.ags_mx_linear_backward
+    w, saved = _t(8, 64, V, W), _t(64, 40, U, U + (1 << 24))
+    need = mx.ags_mx_linear_save_workspace(40, 8, 64)
+    assert need >= sum(mx.ags_mx_bytes(40, 64))
+    _raises(ags.AGS_E_ARG, save, X, bf, 40, 64, w, Y, bf, 8, saved, None, 0)                  # no workspace
+    _raises(ags.AGS_E_ARG, save, X, bf, 40, 64, w, Y, bf, 8, saved, Z, need - 1)
+    _raises(ags.AGS_E_ALIGN, save, X, bf, 40, 64, w, Y, bf, 8, saved, Z + 8, need)
+    _raises(ags.AGS_E_ARG, save, X, bf, 40, 64, w, Y, bf, 8, _t(40, 64, U, U + (1 << 24)), Z, need)
+    _raises(ags.AGS_E_ARG, save, X, bf, 40, 64, w, Y, bf, 8, _t(64, 40, X, U), Z, need)       # saved over x
+    _raises(ags.AGS_E_ARG, save, X, bf, 40, 64, w, Y, bf, 8, _t(64, 40, None, U), Z, need)
+    _raises(ags.AGS_E_ARG, save, X, bf, 40, 63, w, Y, bf, 8, saved, Z, need)                  # strides
+    _raises(ags.AGS_E_ARG, save, X, bf, 40, 64, w, Y, bf, 7, saved, Z, need)
+    _raises(ags.AGS_E_ARG, save, X, 2, 40, 64, w, Y, bf, 8, saved, Z, need)
+    _raises(ags.AGS_E_ARG, save, X, bf, 40, 64, w, Y, 2, 8, saved, Z, need)
+    _raises(ags.AGS_E_ALIGN, save, X + 1, bf, 40, 64, w, Y, bf, 8, saved, Z, need)
+    _raises(ags.AGS_E_ARG, save, X, bf, 40, 64, w, Z, bf, 8, saved, Z, need)                  # y over the workspace
+    save(X, bf, 0, 64, w, Y, bf, 8, _t(64, 0))                                                 # nothing to do
+    wt = _t(64, 8, V, W)
+    need = mx.ags_mx_linear_backward_workspace(40, 8, 64, 1)
+    assert need > mx.ags_mx_linear_backward_workspace(40, 8, 64, 0) > 0
+    good = dict(d_dy=X, dtype=bf, rows=40, n=8, row_stride=8, d_noise=None, noise_stride=0, saved=saved, wt=wt,
+                d_dx=Y, dx_stride=64, d_dw=Z, dw_dtype=ags.AGS_F32, dw_stride=64, accumulate=0,
+                d_workspace=0x20000000000, workspace_bytes=need)
+    for status, change in (
+            (ags.AGS_E_ARG, dict(d_workspace=None)), (ags.AGS_E_ARG, dict(workspace_bytes=need - 1)),
+            (ags.AGS_E_ALIGN, dict(d_workspace=0x20000000004)), (ags.AGS_E_ARG, dict(dtype=2)),
+            (ags.AGS_E_ARG, dict(dw_dtype=2)), (ags.AGS_E_ARG, dict(accumulate=2)), (ags.AGS_E_ARG, dict(d_dy=None)),
+            (ags.AGS_E_ARG, dict(row_stride=7)), (ags.AGS_E_ARG, dict(d_noise=X + (1 << 24), noise_stride=7)),
+            (ags.AGS_E_ARG, dict(rows=41)), (ags.AGS_E_ARG, dict(wt=_t(8, 64, V, W))), (ags.AGS_E_ARG, dict(d_dx=None)),
+            (ags.AGS_E_ARG, dict(dx_stride=63)), (ags.AGS_E_ARG, dict(d_dw=None)), (ags.AGS_E_ARG, dict(dw_stride=63)),
+            (ags.AGS_E_ALIGN, dict(d_dw=Z + 2)), (ags.AGS_E_ARG, dict(d_dw=Y)), (ags.AGS_E_ARG, dict(d_dx=X)),
+            (ags.AGS_E_ARG, dict(rows=-1)), (ags.AGS_E_LAYOUT, dict(n=1 << 25, row_stride=1 << 25)),
+            (ags.AGS_E_ARG, dict(d_dw=U))):
+        _raises(status, back, **{**good, **change})
+    assert lib.ags_mx_linear_save_workspace(40, 8, 64, None) == ags.AGS_E_ARG
+    assert lib.ags_mx_linear_backward_workspace(40, 8, 64, 1, None) == ags.AGS_E_ARG
+    _raises(ags.AGS_E_LAYOUT, mx.ags_mx_linear_save_workspace, 1 << 20, 1 << 20, 64)
+    _raises(ags.AGS_E_ARG, mx.ags_mx_linear_backward_workspace, 4, -1, 64, 0)
