@@ -328,9 +328,9 @@ def linear(x, w, dtype=None, save=False):
     t = _t()
     if w.rows is None:
         raise ValueError("the weight has no forward form")
-    if x.shape[-1] != w.k:
+    x2, rows, cols, stride = _matrix(x, "x")
+    if cols != w.k:
         raise ValueError(f"x must have {w.k} columns")
-    x2, rows, _, stride = _matrix(x, "x")
     out_code, out_dt = _dtype(x.dtype if dtype is None else dtype)
     shape = (*x.shape[:-1], w.n)
     dev = x.device
@@ -357,11 +357,11 @@ def linear_backward(dy, x, w, noise=None, dw=None, dw_dtype="f32", accumulate=Fa
     noise: random bytes for dy's rounding (uint8, dy's shape).  dw: written
     there (a view of a replica's row, say), added with `accumulate`; else a
     new tensor of `dw_dtype`.  need_dx=False returns None for dx."""
-    if dy.shape[-1] != w.n:
-        raise ValueError(f"dy must have {w.n} columns")
     if need_dx and w.cols is None:
         raise ValueError("the weight has no backward form")
     dy2, rows, n, stride = _matrix(dy, "dy")
+    if n != w.n:
+        raise ValueError(f"dy must have {w.n} columns")
     code, dev, k = _dtype(dy.dtype)[0], dy.device, w.k
     noise, n_ptr, n_stride = _noise(noise, rows, n, "dy")
     dw, dw_code, dw_stride = _output(dw, n, k, dw_dtype, accumulate, "dw", dev)

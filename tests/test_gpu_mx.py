@@ -480,3 +480,14 @@ def test_training_calls_stay_inside_their_workspaces(m, n, k):
     y2, saved2 = mx.linear(x, W, save=True)
     dx2, dw2 = mx.linear_backward(dy, saved2, W)
     assert torch.equal(y, y2) and torch.equal(dx, dx2) and torch.equal(dw, dw2)
+
+
+def test_inputs_without_axes_are_refused():
+    w, one = mx.Weight(rand(8, 64)), torch.ones((), device="cuda")
+    for bad in (lambda: mx.linear(one, w), lambda: mx.linear_backward(one, rand(1, 64), w),
+                lambda: mx.linear(rand(4, 64).cpu(), w), lambda: mx.quantize(one),
+                lambda: mx.linear_backward(rand(4, 8), rand(4, 64), w, accumulate=True),
+                lambda: mx.linear_backward(rand(4, 8), rand(4, 64), w, dw=torch.zeros(8, 63, device="cuda")),
+                lambda: mx.linear_backward(rand(4, 8), rand(4, 64), w, noise=noise_of(4, 7))):
+        with pytest.raises(ValueError):
+            bad()
