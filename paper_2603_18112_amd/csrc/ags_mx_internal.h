@@ -58,10 +58,12 @@ struct MxShape {
 // rows 6.5 / 7.4; 16 rows 4096 x 25088 16.0 / 12.8 (+ 4.0), 32 rows 22.3 / 13.0
 // (+ 3.9); 16 rows 1000 x 4096 4.6 / 7.2, 32 rows 5.8 / 7.2; where w's rows make
 // tiles for every CU, 1 row 16384 x 16384 28.5 / 32.6, 8 rows 32.9 / 32.2, 16 rows
-// 35.6 / 31.8, 32 rows 50 / 32.3; 16 rows 16384 x 4096 13.7 / 9.8.
+// 35.6 / 31.8, 32 rows 50 / 32.3; 16 rows 16384 x 4096 13.7 / 9.8.  More than 16
+// rows of few, long rows of w, the launch that joins included: 23 x 692 x 14723
+// 11.6 / 8.5, 20 x 1970 x 9049 8.1 / 8.8, 32 x 1780 x 4959 6.5 / 7.5.
 inline bool mx_few(int64_t m, int64_t n, int64_t kp) {
     if (n >= 8192) return m <= 8;
-    return m <= 16 || (m <= 32 && n * kp <= ((int64_t)1 << 24));
+    return m <= 16 || (m <= 32 && kp <= 12288 && n * kp <= ((int64_t)1 << 24));
 }
 
 // Does ags_mx_linear take x to 4 bits in the product's kernel?  Every block
@@ -72,35 +74,43 @@ inline bool mx_few(int64_t m, int64_t n, int64_t kp) {
 inline bool mx_linear_fused(int64_t rows, int64_t k) { return rows <= 16 && rows * k <= 32768; }
 
 // The tile and the split with the least estimated time in us.  A stage (256
-// columns) of a tile of 64 squared takes 0.26 on a CU, and as much for each
-// further one on it; of 128 squared 0.45 where half the CUs have none, 0.65
-// where all do, 0.68 for each of more; of 256 squared 1.35, or 1.9 with all CUs
-// at work, at the clock the power limit leaves; prologue and epilogue 2.5, 3 or
-// 5; a split costs the launch that joins the parts (5) and their bytes at 4 TB/s.
-// Measured against every shape and split (bf16 results, us, small / middle /
-// large, in their best number of parts if it is not one): 64 x 4096 x 4096 7.8 /
-// 11.1 / 17.7 in four; 64 x 16384 x 16384 23.6 / 31.9 in two / 43.6 in four; 24 x
-// 4096 x 25088 14.9 in four (27.1 in one) / 17.2 in six / 26.7; 256 x 4096 x 25088
-// 29.7 / 28.6 in three / 37.1; 500 x 500 x 20000 13.7 in four (22.6 in one) / 16.1
-// in eight / 27; 512 x 4096 x 8192 18.3 / 20.2 / 32.1; 1024 x 4096 x 4096 18.8 /
-// 14.5 / 27.8; 1500 x 1500 x 6000 19.0 / 17.6 / 31.2; 2048 x 4096 x 4096 33.9 /
-// 25.8 / 31.2; 3000 cubed 32.7 / 29.1 / 26.2; 4096 x 4096 x 1024 25.5 / 21.0 /
-// 18.5.  256 x 128 tiles were not the fastest anywhere by more than a twentieth.
+// columns) of a tile of 64 squared takes 0.26 on a CU, its prologue and epilogue
+// 1.4, and as much again for each further one on the CU; a stage of 128 squared
+// 0.34, or 0.68 for each of more than one; of 256 squared 1.3, or 1.7 with all
+// CUs at work, at the clock the power limit leaves; their prologues and epilogues
+// 4 and 5; a split costs the launch that joins the parts (3.2) and their bytes, 8
+// a result, at 6 TB/s.  Fitted to the times of every shape and split for 320
+// products, most of them drawn over 5 to 25000 a side, bf16 and fp32, aligned and
+// odd; the shape this picks is 1% slower than the best one on average, 22% at
+// worst. What takes under 9 in one launch stays so: two take the host that long
+// (443 x 288 x 5178 of a forward pass 14.2 us a call against 16.0 in four parts).
+// Some of them (us in a graph, from memory, small / middle / large, in their best
+// number of parts if it is not one): 64 x 4096 x 4096 7.3 / 11.2 / 17.9 in four;
+// 64 x 16384 x 16384 35.2 / 41.4 in four / 49.9 in four; 24 x 4096 x 25088 16.3
+// in four / 18.5 in eight / 27.7 in sixteen; 256 x 4096 x 25088 33.6 / 32.3 in
+// four / 40.5 in twelve; 500 x 500 x 20000 13.1 in four / 15.1 in eight / 24.9 in
+// sixteen; 496 x 3840 x 21760 49.6 / 39.3 in two / 45.6 in eight; 512 x 4096 x
+// 8192 21.6 / 22.7 / 32.9 in four; 1024 x 4096 x 4096 19.6 / 14.3 / 29.6; 1500 x
+// 1500 x 6000 18.8 / 16.6 / 28.1 in four; 2048 x 4096 x 4096 39.5 / 25.7 / 35.8;
+// 3000 cubed 36.2 / 33.6 / 29.2; 4096 x 4096 x 1024 28.3 / 22.5 / 19.6; 14208 x
+// 15616 x 100 168.1 / 117.5 / 125.2. 256 x 128 tiles were not the fastest
+// anywhere by more than a twentieth.
 inline MxShape mx_product_plan(int64_t m, int64_t n, int64_t kp) {
     if (mx_few(m, n, kp)) return MxShape{1, 1, 1, 1};
     MxShape best{1, 1, 1, 0};
     double least = 1e30;
     const double stages = (double)(kp / 256);
-    for (int t = 1; t <= 4; t *= 2) {
-        const double tiles = (double)((m + 64 * t - 1) / (64 * t)) * (double)((n + 64 * t - 1) / (64 * t));
-        for (int s : {1, 2, 3, 4, 6, 8, 12, 16}) {
-            if (s > 1 && stages < 4 * s) break;
+    for (int s : {1, 2, 3, 4, 6, 8, 12, 16}) {
+        if (s > 1 && (stages < 4 * s || m * n >= (int64_t)1 << 31)) break;  // (mx_join_kernel)
+        if (s == 2 && least < 9) break;
+        for (int t = 1; t <= 4; t *= 2) {
+            const double tiles = (double)((m + 64 * t - 1) / (64 * t)) * (double)((n + 64 * t - 1) / (64 * t));
             const double load = tiles * s / 256;  // blocks of a CU
             double us = stages / s;
-            if (t == 1) us = us * 0.26 * std::max(1.0, load) + 2.5 * std::max(1.0, load / 4);
-            else if (t == 2) us = us * (load > 1 ? 0.68 * load : load > 0.5 ? 0.65 : 0.45) + 3 * std::max(1.0, load / 2);
-            else us = (us * (load > 0.75 ? 1.9 : 1.35) + 5) * std::max(1.0, std::ceil(load));
-            if (s > 1) us += 5 + 8e-6 * (double)m * (double)n / 4 * s;
+            if (t == 1) us = (us * 0.26 + 1.4) * std::max(1.0, load);
+            else if (t == 2) us = us * (load > 1 ? 0.68 * load : 0.34) + 4 * std::max(1.0, load / 10);
+            else us = (us * (load > 0.75 ? 1.7 : 1.3) + 5) * std::max(1.0, std::ceil(load));
+            if (s > 1) us += 3.2 + 1.3e-6 * (double)m * (double)n * s;
             if (us < least) {
                 least = us;
                 best = MxShape{t, t, s, 0};

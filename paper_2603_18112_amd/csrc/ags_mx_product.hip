@@ -422,13 +422,50 @@ __global__ __launch_bounds__(256, 1) void mx_tile_kernel(MxProductArgs a, unsign
     tile_product<TM, TN, NB>(a, tiles_m, tiles_n);
 }
 
+// A thread takes four elements of the output, one after the other in its rows,
+// and has the loads of four parts under way.  The rule for parts keeps m n below
+// 2^31, so 32 bits hold an element's number.
 __global__ __launch_bounds__(256) void mx_join_kernel(MxProductArgs a) {
-    const int64_t total = a.m * a.n;
+    typedef mx::Unaligned<float, 4, 4> Four;
+    const unsigned total = (unsigned)(a.m * a.n), n = (unsigned)a.n;
     const Out o{static_cast<char*>(a.out), a.stride, a.bf16 != 0, a.accumulate != 0};
-    for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < total; t += (int64_t)gridDim.x * 256) {
-        float v = 0.0f;
-        for (int s = 0; s < a.splits; ++s) v += a.partials[s * total + t];
-        store1(o, t / a.n * a.stride + t % a.n, v);
+    for (unsigned t = (blockIdx.x * 256 + threadIdx.x) * 4; t < total; t += gridDim.x * 1024) {
+        const unsigned i = t / n, j = t - i * n, count = min(total - t, 4u);
+        Four v = {};
+        for (int s = 0; s < a.splits; s += 4) {
+            Four p[4] = {};
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const float* from = a.partials + (int64_t)min(s + u, a.splits - 1) * total + t;
+                if (count == 4) {
+                    p[u] = *reinterpret_cast<const Four*>(from);
+                } else {
+#pragma unroll
+                    for (unsigned e = 0; e < 3; ++e)
+                        if (e < count) p[u].v[e] = from[e];
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v.v[e] += s + u < a.splits ? p[u].v[e] : 0.0f;
+        }
+        if (count == 4 && j + 4 <= n && !o.add) {
+            const int64_t at = i * o.stride + j;
+            if (o.bf16) {
+                mx::Unaligned<unsigned, 2, 2> w;
+                w.v[0] = pack_bf16(v.v[0], v.v[1]), w.v[1] = pack_bf16(v.v[2], v.v[3]);
+                *reinterpret_cast<mx::Unaligned<unsigned, 2, 2>*>(reinterpret_cast<unsigned short*>(o.p) + at) = w;
+            } else {
+                *reinterpret_cast<Four*>(reinterpret_cast<float*>(o.p) + at) = v;
+            }
+            continue;
+        }
+#pragma unroll
+        for (unsigned e = 0; e < 4; ++e) {  // added to what is there, over the end of a row, or the last few
+            const unsigned r = (t + e) / n;
+            if (e < count) store1(o, r * o.stride + (t + e - r * n), v.v[e]);
+        }
     }
 }
 
@@ -629,7 +666,7 @@ hipError_t launch_mx_product(const MxProductArgs& args, hipStream_t s) {
     if (p.few) return launch_few(a, FewX{a.a, a.sa, 0, 0}, s);
     hipError_t e = p.tm == 4 ? launch_tiles<4>(a, s) : p.tm == 2 ? launch_tiles<2>(a, s) : launch_tiles<1>(a, s);
     if (e == hipSuccess && a.splits > 1) {
-        const unsigned blocks = (unsigned)std::min<int64_t>((a.m * a.n + 255) / 256, 4096);
+        const unsigned blocks = (unsigned)std::min<int64_t>((a.m * a.n + 1023) / 1024, 4096);
         hipLaunchKernelGGL(mx_join_kernel, dim3(blocks), dim3(256), 0, s, a);
         e = hipGetLastError();
     }

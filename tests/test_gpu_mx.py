@@ -491,3 +491,11 @@ def test_inputs_without_axes_are_refused():
                 lambda: mx.linear_backward(rand(4, 8), rand(4, 64), w, noise=noise_of(4, 7))):
         with pytest.raises(ValueError):
             bad()
+
+
+@pytest.mark.parametrize("m,n,k", [(203, 153, 19645), (45, 7, 9001), (17, 1, 20000), (37, 3, 12345), (35, 66, 9000),
+                                   (496, 385, 9000), (33, 2, 8300), (130, 131, 9100), (23, 692, 13000)])
+def test_parts_joined_over_rows_of_any_length(m, n, k):
+    if (m, n) != (496, 385):
+        assert mx.ags_mx_product_workspace(m, n, k) > 0            # in parts
+    test_products_of_whole_numbers_are_exact(m, n, k)
