@@ -55,8 +55,8 @@ struct MxShape {
 // chunk; the tiles load ahead.  Against tiles of 64 squared, with the launch that
 // joins their parts (in brackets) where those are faster, weights from memory,
 // kernels' times in us: 8 rows 4096 x 4096 4.7 against 7.4, 16 rows 5.2 / 7.3, 32
-// rows 6.5 / 7.4; 16 rows 4096 x 25088 16.0 / 12.8 (+ 4.0), 32 rows 22.3 / 13.0
-// (+ 3.9); 16 rows 1000 x 4096 4.6 / 7.2, 32 rows 5.8 / 7.2; where w's rows make
+// rows 6.5 / 7.4; 16 rows 4096 x 25088 16.0 / 12.8 (+ 2.9), 32 rows 22.3 / 13.0
+// (+ 2.9); 16 rows 1000 x 4096 4.6 / 7.2, 32 rows 5.8 / 7.2; where w's rows make
 // tiles for every CU, 1 row 16384 x 16384 28.5 / 32.6, 8 rows 32.9 / 32.2, 16 rows
 // 35.6 / 31.8, 32 rows 50 / 32.3; 16 rows 16384 x 4096 13.7 / 9.8.  More than 16
 // rows of few, long rows of w, the launch that joins included: 23 x 692 x 14723
