@@ -14,8 +14,9 @@
  *
  * One group is the global norm; a group for each replica clips each
  * worker's gradient by itself; a group for each layer clips layer by layer.
- * Sums are kept in fp64 and added in a fixed order: a call is bitwise
- * reproducible, and no fp32 value over- or underflows its square.  c_g is
+ * Sums are kept in fp64 and added in an order that the configuration alone
+ * fixes, not the tensors' addresses: equal gradients give equal norms bit for
+ * bit, and no fp32 value over- or underflows its square.  c_g is
  * rounded to fp32, the product x c_g once to the output's type.
  *
  * A NaN among a group's elements makes N_g and c_g NaN (so every output of

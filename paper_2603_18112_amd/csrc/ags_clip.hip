@@ -94,27 +94,20 @@ struct Access {
     }
 };
 
-// Elements before p's next 16-byte boundary, at most n.
-template <typename T>
-__device__ __forceinline__ int head_elems(const T* p, int n) {
-    const int h = (int)((16u - ((unsigned)reinterpret_cast<uintptr_t>(p) & 15u)) & 15u) / (int)sizeof(T);
-    return min(h, n);
-}
-
 __device__ __forceinline__ const void* base_of(const ClipArgs& a, int i) {
     return a.table ? a.table[i] : a.ptr[i];
 }
 
-// The sum over n elements by NT threads, this one's share.
+// The sum over n elements by NT threads, this one's share.  Which elements a
+// thread takes depends on n alone, not on the address, so that equal gradients
+// have equal norms wherever they lie.  Against a share that starts at the first
+// 16-byte boundary, 138M elements one element past it: fp32 85.7 us against 86.9,
+// bf16, whose accesses then start inside a dword, 52.9 against 44.7.
 template <int KIND, int NT, bool STREAM, typename T>
 __device__ __forceinline__ double piece_sum(const T* p, int n, int tid) {
     constexpr int N = 16 / sizeof(T), U = 32 / N;  // an access, and those in flight
     typedef Access<T, N> A;
-    const int head = head_elems(p, n);
     double acc = 0.0, acc2 = 0.0;
-    if (tid < head) acc = accumulate<KIND>(acc, load1(p + tid));
-    p += head;
-    n -= head;
     const int groups = n / N;
     int i = tid;
     for (; i + (U - 1) * NT < groups; i += U * NT) {
@@ -250,6 +243,13 @@ __global__ __launch_bounds__(kClipBlock) void clip_norm_kernel(ClipArgs a) {
         }
     }
     if (tid <= kClipCounters) a.done[tid * kClipCounterStride] = 0u;
+}
+
+// Elements before p's next 16-byte boundary, at most n.
+template <typename T>
+__device__ __forceinline__ int head_elems(const T* p, int n) {
+    const int h = (int)((16u - ((unsigned)reinterpret_cast<uintptr_t>(p) & 15u)) & 15u) / (int)sizeof(T);
+    return min(h, n);
 }
 
 // IN, OUT: past the caches.

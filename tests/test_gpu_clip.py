@@ -426,3 +426,24 @@ def test_arguments_that_name_nothing_are_value_errors():
     h.close()
     with pytest.raises(ValueError):
         clip.GradClip.for_tensors(g, kind="l3")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_sums_do_not_depend_on_where_a_tensor_starts(dtype):
+    # 2^53 + 2^29 lies between two fp32 values, and a one added to it is lost in
+    # fp64, two together are not: shares of the threads that moved with the
+    # address gave two norms.
+    N = 16 // DT[dtype].itemsize
+    x = torch.zeros(512, device="cuda", dtype=DT[dtype])
+    x[0], x[1], x[2 * N - 1], x[9 * N] = 2.0 ** 53, 1.0, 1.0, 2.0 ** 29
+    for n in (512, 200_000):                          # one launch, and two
+        h = clip.GradClip([(n, 0, 0, 0)], [n], [dtype], kind="l1")
+        base = torch.zeros(n + 16, device="cuda", dtype=DT[dtype])
+        norms = set()
+        for shift in range(N + 1):
+            base.zero_()
+            base[shift:shift + 512] = x
+            norms.add(float(h.norm([base[shift:shift + n]])))
+        assert len(norms) == 1
+        assert abs(norms.pop() - (2.0 ** 53 + 2.0 ** 29 + 2)) <= 2.0 ** -23 * 2.0 ** 53
+        h.close()
