@@ -17,7 +17,9 @@
  * Sums are kept in fp64 and added in an order that the configuration alone
  * fixes, not the tensors' addresses: equal gradients give equal norms bit for
  * bit, and no fp32 value over- or underflows its square.  c_g is
- * rounded to fp32, the product x c_g once to the output's type.
+ * rounded to fp32, the product x c_g to fp32, and that to a bf16 output's
+ * type.  (A c_g below 2^-100 has 24 bits all the same: it multiplies in two
+ * steps, the second by a power of two.)
  *
  * A NaN among a group's elements makes N_g and c_g NaN (so every output of
  * the group); an infinite one makes N_g infinite and c_g zero (finite

@@ -252,6 +252,8 @@ __device__ __forceinline__ int head_elems(const T* p, int n) {
     return min(h, n);
 }
 
+// The product is rounded to fp32 before it is rounded to bf16: the formula in
+// fp32 arithmetic, off by 2^-24 more than one rounding at most.
 // IN, OUT: past the caches.
 template <int NT, bool IN, bool OUT, typename TI, typename TO>
 __device__ __forceinline__ void piece_scale(const TI* in, TO* out, int n, float2 c, int tid) {

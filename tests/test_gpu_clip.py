@@ -447,3 +447,20 @@ def test_sums_do_not_depend_on_where_a_tensor_starts(dtype):
         assert len(norms) == 1
         assert abs(norms.pop() - (2.0 ** 53 + 2.0 ** 29 + 2)) <= 2.0 ** -23 * 2.0 ** 53
         h.close()
+
+
+@pytest.mark.parametrize("src,dst", [("f32", "bf16"), ("bf16", "bf16"), ("bf16", "f32"), ("f32", "f32")])
+def test_outputs_are_fp32_products_rounded_to_their_type(src, dst):
+    # The largest magnitude is 3, so the coefficient is fp32(1/3), and every
+    # rounding that follows is the one the header names.
+    x = rand(300_000, src, 11).clamp(-3, 3)
+    x[7] = 3.0
+    x[8] = 1.505859375        # fp32: the product lies above 0.501953125, midway between two bf16 values
+    h = clip.GradClip([(x.numel(), 0, 0, 0, 0, 0)], [x.numel()], [src], [x.numel()], [dst], kind="max", eps=0.0)
+    out = torch.empty(x.numel(), device="cuda", dtype=DT[dst])
+    assert float(h.clip([x], 1.0, out=[out])) == 3.0
+    c = torch.tensor(np.float32(1.0 / 3.0), device="cuda")
+    assert torch.equal(out, (x.float() * c).to(DT[dst]))
+    if (src, dst) == ("f32", "bf16"):
+        assert float(out[8]) == 0.5                   # one rounding would give 0.50390625
+    h.close()
