@@ -69,7 +69,7 @@ typedef struct {
     const int32_t *in_dtypes;         /* ags_dtype of each (host, copied)    */
     int32_t n_out;                    /* output tensors; 0: in place only    */
     const int32_t *out_dtypes;
-    int32_t n_groups;                 /* >= 1                                */
+    int32_t n_groups;                 /* 1 .. 2^30                           */
     int32_t kind;                     /* ags_clip_kind                       */
     double eps;                       /* >= 0; the usual value is 1e-6       */
 } ags_clip_config;

@@ -99,3 +99,10 @@ def test_workspace_cap_gives_nomem_before_any_device_call(lib, monkeypatch):
     with pytest.raises(ags.AGSError) as e:
         clip.ags_clip_init(cfg)
     assert e.value.status == ags.AGS_E_NOMEM
+
+
+@pytest.mark.parametrize("n_groups", [(1 << 30) + 1, (1 << 31) - 1])
+def test_group_numbers_that_a_kernel_could_not_count_to(lib, n_groups):
+    # the kernels step over the groups in 32-bit numbers, up to 256 at a time
+    st, msg = _status([(10, 0, 0, 0)], n_groups=n_groups)
+    assert st == ags.AGS_E_LAYOUT and "groups" in msg
