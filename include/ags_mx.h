@@ -95,7 +95,8 @@ ags_status ags_mx_dequantize(const ags_mx_tensor *q, void *d_out, int32_t dtype,
 /* out [a.rows][row_stride], row_stride >= b.rows, a.cols == b.cols: the
  * product, added to out's values with accumulate = 1 (in fp32, one rounding
  * to out's type).  d_workspace: ags_mx_product_workspace bytes (16-byte
- * aligned), or NULL where that is 0.  The result does not depend on
+ * aligned), or NULL where that is 0.  out has at most 2^34 elements and 2^26
+ * rows or columns (AGS_E_LAYOUT).  The result does not depend on
  * anything but the operands: sums are added in a fixed order. */
 ags_status ags_mx_product_workspace(int64_t m, int64_t n, int64_t k, size_t *out_bytes);
 ags_status ags_mx_product(const ags_mx_tensor *a, const ags_mx_tensor *b, void *d_out,

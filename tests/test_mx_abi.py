@@ -197,3 +197,15 @@ def test_training_calls_refuse(lib):
     assert lib.ags_mx_linear_backward_workspace(40, 8, 64, 1, None) == ags.AGS_E_ARG
     _raises(ags.AGS_E_LAYOUT, mx.ags_mx_linear_save_workspace, 1 << 20, 1 << 20, 64)
     _raises(ags.AGS_E_ARG, mx.ags_mx_linear_backward_workspace, 4, -1, 64, 0)
+
+
+@pytest.mark.parametrize("m,n", [(1 << 34, 1), (1, 1 << 34), (1 << 31, 2), ((1 << 26) + 1, 1)])
+def test_products_over_an_empty_axis_stay_within_a_launch(lib, m, n):
+    # operands without columns have no elements to limit their rows: the
+    # product of 2^34 by 1 would need 2^36 work-items
+    for query in (mx.ags_mx_product_workspace, mx.ags_mx_linear_workspace, mx.ags_mx_linear_save_workspace):
+        _raises(ags.AGS_E_LAYOUT, query, m, n, 0)
+    _raises(ags.AGS_E_LAYOUT, mx.ags_mx_linear_backward_workspace, 0, m, n, 1)
+    _raises(ags.AGS_E_LAYOUT, mx.ags_mx_product, _t(m, 0, None, None), _t(n, 0, None, None), X, ags.AGS_BF16, n)
+    assert mx.ags_mx_product_workspace(1 << 26, 256, 0) == 0
+    assert mx.ags_mx_product_workspace(m, 0, 0) == 0                                # nothing to do
