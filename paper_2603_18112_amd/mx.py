@@ -324,8 +324,13 @@ class Weight:
 def linear(x, w, dtype=None, save=False):
     """y = x w' for x [..., k] and a Weight w [n, k]: [..., n] of `dtype` (x's
     unless given).  save=True returns (y, saved): what linear_backward takes
-    in place of x, stored in the same pass over it."""
+    in place of x, stored in the same pass over it.  Autograd does not see the
+    call (linear_backward is its backward pass), so an x that requires a
+    gradient is refused where gradients are recorded."""
     t = _t()
+    if x.requires_grad and t.is_grad_enabled():
+        raise ValueError("x requires a gradient, which linear does not record: detach it, or call under "
+                         "torch.no_grad() and linear_backward for the gradients")
     if w.rows is None:
         raise ValueError("the weight has no forward form")
     x2, rows, cols, stride = _matrix(x, "x")

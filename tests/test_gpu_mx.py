@@ -499,3 +499,31 @@ def test_parts_joined_over_rows_of_any_length(m, n, k):
     if (m, n) != (496, 385):
         assert mx.ags_mx_product_workspace(m, n, k) > 0            # in parts
     test_products_of_whole_numbers_are_exact(m, n, k)
+
+
+def test_an_input_that_requires_a_gradient_is_refused():
+    w, x = mx.Weight(rand(8, 64)), rand(4, 64).requires_grad_()
+    for save in (False, True):
+        with pytest.raises(ValueError, match="gradient"):     # y would lose it without a word
+            mx.linear(x, w, save=save)
+    with torch.no_grad():
+        y, saved = mx.linear(x, w, save=True)
+    assert torch.equal(y, mx.linear(x.detach(), w))
+
+    class Linear(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x):
+            y, ctx.saved = mx.linear(x, w, save=True)
+            return y
+
+        @staticmethod
+        def backward(ctx, dy):
+            return mx.linear_backward(dy, ctx.saved, w)[0]
+
+    dy = rand(4, 8, seed=1)
+    Linear.apply(x).backward(dy)
+    assert torch.equal(x.grad, mx.linear_backward(dy, saved, w)[0])
+    # gradients asked for by name, and weights that are parameters
+    assert torch.equal(mx.linear_backward(dy, x, w)[0], x.grad)
+    p = torch.nn.Parameter(rand(8, 64))
+    mx.Weight(p).update(p)
