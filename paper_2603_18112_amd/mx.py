@@ -164,8 +164,9 @@ def _stream(device):
     return t.cuda.current_stream(device).cuda_stream
 
 
-def _matrix(x, what):
-    """x as 2-D with unit column stride: (tensor, rows, cols, row stride)."""
+def _matrix(x, what, copy=False):
+    """x as 2-D with unit column stride: (tensor, rows, cols, row stride).
+    copy: rows that overlap or are not contiguous are copied, not refused."""
     if not x.is_cuda:
         raise ValueError(f"{what} must be a CUDA tensor")
     if x.dim() != 2:
@@ -174,10 +175,14 @@ def _matrix(x, what):
         x = x.reshape(math.prod(x.shape[:-1]), x.shape[-1])
     rows, cols = x.shape
     if cols > 1 and x.stride(1) != 1:
-        raise ValueError(f"{what} must be contiguous along its last axis")
+        if not copy:
+            raise ValueError(f"{what} must be contiguous along its last axis")
+        x = x.contiguous()
     stride = x.stride(0) if rows > 1 else cols
     if stride < cols:
-        raise ValueError(f"{what}'s rows overlap")
+        if not copy:
+            raise ValueError(f"{what}'s rows overlap")
+        x, stride = x.contiguous(), cols
     return x, rows, cols, stride
 
 
@@ -215,19 +220,23 @@ class MX4:
         return self.rows, self.cols
 
 
-def _noise(noise, rows, cols, what):
+def _noise(noise, rows, cols, what, copy=False):
     """(random bytes [rows, cols] or None, their address, row stride)."""
     if noise is None:
         return None, None, 0
-    noise, r, c, stride = _matrix(noise, "noise")
+    noise, r, c, stride = _matrix(noise, "noise", copy)
     if noise.dtype is not _t().uint8 or (r, c) != (rows, cols):
         raise ValueError(f"noise must hold one uint8 for each element of {what}")
     return noise, noise.data_ptr() or None, stride
 
 
+def _transposed(x):
+    return x.dim() == 2 and x.stride(1) != 1 and x.stride(0) == 1 and x.shape[1] > 1
+
+
 def _quantize(x, noise, q, qt):
-    if x.dim() == 2 and x.stride(1) != 1 and x.stride(0) == 1 and x.shape[1] > 1:
-        # a transposed view: the two forms change places
+    if _transposed(x):
+        # the two forms change places
         qt, q = _quantize(x.t(), None if noise is None else noise.t().contiguous(), qt, q)
         return q, qt
     x, rows, cols, stride = _matrix(x, "x")
@@ -244,8 +253,9 @@ def _quantize(x, noise, q, qt):
 
 def quantize(x, noise=None, out=None):
     """x [..., cols] in 4 bits, blocked along its columns: an MX4 of
-    [rows, cols].  noise: random bytes (uint8, x's shape) for stochastic
-    rounding.  out: an MX4 to write."""
+    [rows, cols].  x is contiguous along its last axis, or a transposed matrix.
+    noise: random bytes (uint8, x's shape) for stochastic rounding.  out: an MX4
+    to write."""
     return _quantize(x, noise, True if out is None else out, None)[0]
 
 
@@ -324,7 +334,8 @@ class Weight:
 def linear(x, w, dtype=None, save=False):
     """y = x w' for x [..., k] and a Weight w [n, k]: [..., n] of `dtype` (x's
     unless given).  save=True returns (y, saved): what linear_backward takes
-    in place of x, stored in the same pass over it.  Autograd does not see the
+    in place of x, stored in the same pass over it.  An x whose rows are not
+    contiguous (transposed, broadcast) is copied first.  Autograd does not see the
     call (linear_backward is its backward pass), so an x that requires a
     gradient is refused where gradients are recorded."""
     t = _t()
@@ -333,7 +344,7 @@ def linear(x, w, dtype=None, save=False):
                          "torch.no_grad() and linear_backward for the gradients")
     if w.rows is None:
         raise ValueError("the weight has no forward form")
-    x2, rows, cols, stride = _matrix(x, "x")
+    x2, rows, cols, stride = _matrix(x, "x", copy=True)
     if cols != w.k:
         raise ValueError(f"x must have {w.k} columns")
     out_code, out_dt = _dtype(x.dtype if dtype is None else dtype)
@@ -361,16 +372,17 @@ def linear_backward(dy, x, w, noise=None, dw=None, dw_dtype="f32", accumulate=Fa
     dw [n, k]).  x: the layer's input, or what linear(save=True) returned.
     noise: random bytes for dy's rounding (uint8, dy's shape).  dw: written
     there (a view of a replica's row, say), added with `accumulate`; else a
-    new tensor of `dw_dtype`.  need_dx=False returns None for dx."""
+    new tensor of `dw_dtype`.  need_dx=False returns None for dx.  Inputs may
+    have any strides, as for linear."""
     if need_dx and w.cols is None:
         raise ValueError("the weight has no backward form")
-    dy2, rows, n, stride = _matrix(dy, "dy")
+    dy2, rows, n, stride = _matrix(dy, "dy", copy=True)
     if n != w.n:
         raise ValueError(f"dy must have {w.n} columns")
     code, dev, k = _dtype(dy.dtype)[0], dy.device, w.k
-    noise, n_ptr, n_stride = _noise(noise, rows, n, "dy")
+    noise, n_ptr, n_stride = _noise(noise, rows, n, "dy", copy=True)
     dw, dw_code, dw_stride = _output(dw, n, k, dw_dtype, accumulate, "dw", dev)
-    xt = x if isinstance(x, MX4) else quantize_t(x)
+    xt = x if isinstance(x, MX4) else quantize_t(x if _transposed(x) else _matrix(x, "x", copy=True)[0])
     if xt.shape != (k, rows):
         raise ValueError(f"x and dy differ in rows, or x has not {k} columns")
     dx = _t().empty((*dy.shape[:-1], k), dtype=dy.dtype, device=dev) if need_dx else None

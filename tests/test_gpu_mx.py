@@ -527,3 +527,31 @@ def test_an_input_that_requires_a_gradient_is_refused():
     assert torch.equal(mx.linear_backward(dy, x, w)[0], x.grad)
     p = torch.nn.Parameter(rand(8, 64))
     mx.Weight(p).update(p)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m", [1, 6, 60])
+def test_layers_take_inputs_of_any_strides(m, dtype):
+    n, k = 40, 96
+    x, dy, r, W = rand(m, k, dtype, 1), rand(m, n, dtype, 2), noise_of(m, n), mx.Weight(rand(n, k, seed=3))
+
+    def check(x, dy, r):
+        y, saved = mx.linear(x.contiguous(), W, save=True)
+        dx, dw = mx.linear_backward(dy.contiguous(), saved, W, noise=None if r is None else r.contiguous())
+        y2, saved2 = mx.linear(x, W, save=True)
+        assert torch.equal(y, y2) and torch.equal(mx.dequantize(saved), mx.dequantize(saved2))
+        assert torch.equal(mx.linear(x, W), mx.linear(x.contiguous(), W))
+        for form in (x, saved2):
+            dx2, dw2 = mx.linear_backward(dy, form, W, noise=r)
+            assert torch.equal(dx, dx2) and torch.equal(dw, dw2)
+
+    for other in (lambda t: t.t().contiguous().t(), lambda t: t.repeat_interleave(2, 1)[:, ::2],
+                  lambda t: torch.cat([t, t], 1)[:, :t.shape[1]]):
+        check(other(x), other(dy), None)
+        check(other(x), other(dy), other(r))
+    one = torch.ones((), device="cuda", dtype=DT[dtype])
+    check(x[:1].expand(m, k), one.expand(m, n), r[:1].expand(m, n))       # a broadcast gradient, as of a sum
+    if m % 6 == 0:
+        a, b, c = (t.view(2, 3, m // 6, -1).transpose(0, 2) for t in (x, dy, r))
+        check(a, b, c)
+        check(a[..., ::2].repeat_interleave(2, -1), b, c)
