@@ -112,6 +112,17 @@ def ags_clip_destroy(handle):
 # ------------------------------------------------------- torch convenience --
 
 
+def _dense(t):
+    """Do t's elements lie side by side, in whatever order of its axes?"""
+    n = 1
+    for stride, size in sorted(zip(t.stride(), t.shape)):
+        if size != 1:
+            if stride != n:
+                return False
+            n *= size
+    return True
+
+
 def _name(dtype):
     return str(dtype).replace("torch.", "").replace("float32", "f32").replace("bfloat16", "bf16")
 
@@ -154,6 +165,9 @@ class GradClip:
                 raise ValueError(f"a segment ends past its tensor ({off})")
         self.device = torch.device("cuda", torch.cuda.current_device())
         self.handle = ags_clip_init(self.cfg, self._stream(stream))
+        # every segment is a whole tensor: the order of its elements is free
+        self.whole = bool(np.all((seg["in_offset"] == 0)
+                                 & (seg["numel"] == np.asarray(self.in_numels, np.int64)[seg["in_base"]])))
 
     @classmethod
     def for_tensors(cls, tensors, *, groups=None, layers=None, out_dtype=None, kind="l2", eps=1e-6,
@@ -161,7 +175,9 @@ class GradClip:
         """For tensors of these sizes and types: one group, or the group of
         each.  With `layers` ((offset, numel, flags) of a flat layout, one per
         tensor) :meth:`clip` can write them into a flat row of `out_dtype`
-        (by default fp32) that reaches at least to the last layer's end."""
+        (by default fp32) that reaches at least to the last layer's end; its
+        tensors are contiguous then.  Norms and scaling in place take dense
+        tensors whose axes lie in any order (channels last) too."""
         numels = [t.numel() for t in tensors]
         dtypes = [_name(t.dtype) for t in tensors]
         groups = [0] * len(numels) if groups is None else [int(g) for g in groups]
@@ -206,9 +222,10 @@ class GradClip:
             stream = self.torch.cuda.current_stream(self.device)
         return int(stream.cuda_stream) if hasattr(stream, "cuda_stream") else int(stream)
 
-    def _pointers(self, what, tensors, numels, dtypes, longer=False):
+    def _pointers(self, what, tensors, numels, dtypes, longer=False, any_order=False):
         """Host array of the tensors' addresses (the library checks that they
-        lie in device memory).  One pass of a C function over the list for each
+        lie in device memory).  any_order: a dense tensor whose axes lie in
+        another order (channels last) will do.  One pass of a C function over the list for each
         property: written as a loop the checks of 161 tensors take longer than
         the kernels."""
         T = self.torch.Tensor
@@ -218,7 +235,7 @@ class GradClip:
             raise ValueError(f"{what} differ in number or size from the handle's")
         if list(map(attrgetter("dtype"), tensors)) != dtypes:
             raise ValueError(f"{what} differ in type from the handle's")
-        if not all(map(T.is_contiguous, tensors)):
+        if not all(map(T.is_contiguous, tensors)) and not (any_order and all(map(_dense, tensors))):
             raise ValueError(f"{what} must be contiguous")
         return array.array("Q", map(T.data_ptr, tensors))
 
@@ -234,7 +251,7 @@ class GradClip:
 
     def norm(self, tensors, stream=None):
         """The norm of each group, fp32 [n_groups] on the device."""
-        p = self._pointers("the gradients", tensors, self.in_numels, self.in_dtypes)
+        p = self._pointers("the gradients", tensors, self.in_numels, self.in_dtypes, any_order=self.whole)
         norms = self._norms(stream)
         ags_clip_norm(self.handle, p.buffer_info()[0], norms.data_ptr(), self._stream(stream))
         return norms
@@ -242,7 +259,8 @@ class GradClip:
     def clip(self, tensors, max_norm, out=None, stream=None):
         """Scale each group by min(1, max_norm / (norm + eps)), in place or
         into the tensors of `out`; returns the norms."""
-        p = self._pointers("the gradients", tensors, self.in_numels, self.in_dtypes)
+        p = self._pointers("the gradients", tensors, self.in_numels, self.in_dtypes,
+                           any_order=self.whole and out is None)
         q = None
         if out is not None:
             if not self.out_numels:

@@ -464,3 +464,40 @@ def test_outputs_are_fp32_products_rounded_to_their_type(src, dst):
     if (src, dst) == ("f32", "bf16"):
         assert float(out[8]) == 0.5                   # one rounding would give 0.50390625
     h.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("big", [1, 30])
+def test_dense_tensors_whose_axes_lie_in_another_order(big, dtype):
+    def make():
+        return [rand(big * 6 * 50 * 9, dtype, 1).view(big * 6, 50, 3, 3).contiguous(memory_format=torch.channels_last),
+                rand(63 * 19, dtype, 2).view(63, 19).t(), rand(17, dtype, 3), rand(5 * 3, dtype, 4).view(5, 1, 3).permute(2, 1, 0)]
+    g, old = make(), make()
+    assert not g[0].is_contiguous() and not g[1].is_contiguous()
+    h = clip.GradClip.for_tensors(g)
+    n = norm64(old)
+    check_norms(h.norm(g), [n])
+    check_norms(h.clip(g, 0.25 * n), [n])
+    for a, b in zip(g, old):
+        assert a.stride() == b.stride()
+        check_out(a, b, n, 0.25 * n, dtype)
+    # elements missing between, or taken twice
+    sizes = [t.numel() for t in old]
+    wide = rand(2 * sizes[1], dtype).view(19, 126)
+    for bad in (wide[:, ::2], wide[:, :63], rand(1, dtype).expand(19, 63), rand(63, dtype).expand(19, 63)):
+        assert bad.numel() == sizes[1]
+        with pytest.raises(ValueError):
+            h.norm([old[0], bad, old[2], old[3]])
+    h.close()
+    # where the order counts: a flat row, a segment of a tensor
+    lay = layouts.custom_layout(sizes, [0] * len(sizes))
+    h = clip.GradClip.for_tensors(old, layers=lay.table(), out_dtype=dtype)
+    with pytest.raises(ValueError):
+        h.clip(old, 1.0, out=[torch.zeros(lay.n_flat, device="cuda", dtype=DT[dtype])])
+    check_norms(h.norm(old), [n])
+    h.close()
+    for seg in ((sizes[1] - 1, 0, 0, 0), (sizes[1] - 1, 0, 1, 0)):
+        h = clip.GradClip([seg], [sizes[1]], [dtype])
+        with pytest.raises(ValueError):
+            h.norm([old[1]])
+        h.close()
