@@ -32,11 +32,6 @@ __device__ __forceinline__ float scale_value(unsigned byte) {
     return __uint_as_float(byte ? byte << 23 : 0x400000u);
 }
 
-// 2^-e, exact: 2^127 .. 2^-125.
-__device__ __forceinline__ float scale_inverse(unsigned byte) {
-    return __uint_as_float((254u - byte) << 23);
-}
-
 // Codes of 8 elements in one dword, to nearest: the converter instruction
 // divides by the scale, rounds ties to even and saturates at 6.
 __device__ __forceinline__ unsigned codes_nearest(const float* x, unsigned byte) {
