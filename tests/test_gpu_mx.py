@@ -555,3 +555,59 @@ def test_layers_take_inputs_of_any_strides(m, dtype):
         a, b, c = (t.view(2, 3, m // 6, -1).transpose(0, 2) for t in (x, dy, r))
         check(a, b, c)
         check(a[..., ::2].repeat_interleave(2, -1), b, c)
+
+
+def test_results_of_rows_past_4_gib():
+    """Output rows whose bytes lie past 2^31 and 2^32, over a filled buffer."""
+    m, n, k = (1 << 17) + 3, 20_000, 300
+    a, b = torch.zeros(m, k, device="cuda"), torch.zeros(n, k, device="cuda")
+    rows, cols = [0, 60_000, m - 130, m - 2, m - 1], [0, 9_999, n - 1]
+    for i, r in enumerate(rows):
+        a[r, 7], a[r, 299] = (1.0, 2.0, 3.0, 4.0, 6.0)[i], 1.0
+    for j, c in enumerate(cols):
+        b[c, 7] = (1.0, -2.0, 4.0)[j]
+    out = torch.full((m, n), 9.0, device="cuda", dtype=torch.bfloat16)
+    for accumulate in (False, True):
+        mx.product(mx.quantize(a), mx.quantize(b), out=out, accumulate=accumulate)
+        want = (2 if accumulate else 1) * a[rows][:, 7:8] * b[cols][:, 7]
+        assert torch.equal(out[rows][:, cols].float(), want)
+        assert int(torch.count_nonzero(out)) == len(rows) * len(cols)
+
+
+@pytest.mark.parametrize("m,n,k,dtype", [(1, 500, 4096, "bf16"), (40, 200, 30000, "f32"), (23, 692, 13000, "bf16"),
+                                         (300, 700, 1000, "f32"), (12, 96, 5000, "f32")])
+def test_graph_replays_of_training_and_tokens(m, n, k, dtype):
+    # one launch for tokens, tiles in parts with the launch that joins them, and
+    # the training calls, replayed between eager calls of the same layer
+    x, dy, r = rand(m, k, dtype), rand(m, n, dtype, 2), noise_of(m, n)
+    W = mx.Weight(rand(n, k, seed=3))
+    acc = torch.zeros(n, k, device="cuda")
+
+    def calls():
+        y0 = mx.linear(x, W)
+        y, saved = mx.linear(x, W, save=True)
+        dx, dw = mx.linear_backward(dy, saved, W, noise=r)
+        mx.linear_backward(dy, saved, W, noise=r, dw=acc, accumulate=True, need_dx=False)
+        return y0, y, dx, dw
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        calls()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        got = calls()
+    for step in range(4):
+        x.copy_(rand(m, k, dtype, 10 + step))
+        dy.copy_(rand(m, n, dtype, 20 + step))
+        r.copy_(noise_of(m, n, step))
+        acc.fill_(step)
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed, there = [t.clone() for t in got], acc.clone()
+        acc.fill_(step)
+        want = calls()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(replayed, want)) and torch.equal(there, acc)
