@@ -501,3 +501,50 @@ def test_dense_tensors_whose_axes_lie_in_another_order(big, dtype):
         with pytest.raises(ValueError):
             h.norm([old[1]])
         h.close()
+
+
+@pytest.mark.parametrize("how", ["in place", "row", "stack", "many"])
+def test_graph_replays_of_two_launches(how):
+    # sets past the one-launch size: the counters of the norm's last block, the
+    # pointer table of many tensors, and scaling in place, replayed between
+    # eager calls of the same handle
+    sizes = {"in place": [700_001, 33, 90_000], "row": [400_000, 70_001], "stack": [100_000, 5, 40_000],
+             "many": [200 + i % 7 for i in range(700)]}[how]
+    lay = layouts.custom_layout(sizes, [0] * len(sizes))
+    out = None
+    if how == "stack":
+        K, stride = 3, layouts.replica_stride(lay)
+        g = [torch.zeros(K, stride, device="cuda")]
+        h = clip.GradClip.for_stack(lay.table(), K, stride)
+    else:
+        g = [rand(n, "f32", i) for i, n in enumerate(sizes)]
+        if how == "row":
+            out = [torch.zeros(lay.n_flat, device="cuda", dtype=torch.bfloat16)]
+        h = clip.GradClip.for_tensors(g, layers=lay.table() if how == "row" else None, out_dtype="bf16")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        h.clip(g, 1.0, out=out)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        norms = h.clip(g, 1.0, out=out)
+    res = g if out is None else out
+    for step in range(4):
+        new = [rand(t.numel(), "f32", 1000 * step + i, 10.0 ** -step).view(t.shape) for i, t in enumerate(g)]
+        for t, x in zip(g, new):
+            t.copy_(x)
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed, there = [t.clone() for t in res], norms.clone()
+        for t, x in zip(g, new):
+            t.copy_(x)
+        if out is not None:
+            out[0].zero_()
+        eager = h.clip(g, 1.0, out=out)
+        torch.cuda.synchronize()
+        assert torch.equal(eager, there) and all(torch.equal(a, b) for a, b in zip(replayed, res))
+        if how != "stack":
+            check_norms(eager, [norm64(new)])
+    h.close()
