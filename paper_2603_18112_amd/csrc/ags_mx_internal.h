@@ -57,10 +57,15 @@ struct MxShape {
 // kernels' times in us: 8 rows 4096 x 4096 4.7 against 7.4, 16 rows 5.2 / 7.3, 32
 // rows 6.5 / 7.4; 16 rows 4096 x 25088 16.0 / 12.8 (+ 2.9), 32 rows 22.3 / 13.0
 // (+ 2.9); 16 rows 1000 x 4096 4.6 / 7.2, 32 rows 5.8 / 7.2; where w's rows make
-// tiles for every CU, 1 row 16384 x 16384 28.5 / 32.6, 8 rows 32.9 / 32.2, 16 rows
-// 35.6 / 31.8, 32 rows 50 / 32.3; 16 rows 16384 x 4096 13.7 / 9.8.  More than 16
-// rows of few, long rows of w, the launch that joins included: 23 x 692 x 14723
-// 11.6 / 8.5, 20 x 1970 x 9049 8.1 / 8.8, 32 x 1780 x 4959 6.5 / 7.5.
+// a tile for every CU, 1 row 16384 x 16384 28.5 / 32.6, 8 rows 32.9 / 32.2, 16 rows
+// 35.6 / 31.8, 32 rows 50 / 32.3; 16 rows 16384 x 4096 13.7 / 9.8, 9 rows 16384 x
+// 2048 7.3 / 6.8; with tiles for half of them, 9 rows 8192 x 4096 7.5 / 8.4, 16 rows
+// 8.0 / 8.4.  More than 16 rows of few, long rows of w, the launch that joins
+// included: 23 x 692 x 14723 11.6 / 8.5, 20 x 1970 x 9049 8.1 / 8.8, 32 x 1780 x
+// 4959 6.5 / 7.5.  For up to 16 rows of few, long rows of w the rule is not the
+// faster one: a block goes through its rows' whole length.  Against 16 parts, 10
+// rows 256 x 25088 11.5 / 8.9, 256 x 65536 25.8 / 11.1, 256 x 2^20 398 / 81 (64 parts:
+// 44); 1 row 256 x 25088 8.4 / 8.4, 512 x 65536 24.6 / 12.2, 282 x 23778 8.2 / 8.7.
 inline bool mx_few(int64_t m, int64_t n, int64_t kp) {
     if (n >= 8192) return m <= 8;
     return m <= 16 || (m <= 32 && kp <= 12288 && n * kp <= ((int64_t)1 << 24));
@@ -70,7 +75,11 @@ inline bool mx_few(int64_t m, int64_t n, int64_t kp) {
 // does so then; it keeps x in LDS.  One launch against two, us a call bound by
 // the host / in a graph: 1 row 4096 x 4096 9.0 / 3.8 against 13.1 / 5.2, 8 rows
 // (32768 elements of x) 9.0 / 5.3 against 13.3 / 5.9, 16 rows (65536) 9.1 / 7.3
-// against 13.4 / 6.4; 1 row 16384 x 16384 in a graph 28.0 against 30.1.
+// against 13.4 / 6.4; in a graph, weights from memory, 1 row 16384 x 16384 30.5
+// against 32.1, 4 rows 16384 x 8192 20.6 / 20.4, 16 rows 8192 x 2048 7.4 / 7.7.  Where
+// the product alone would take tiles (mx_few: more than 8 rows, wide weights) the
+// rule gains on the host what it loses on the card: 9 rows 16384 x 2048 9.3 / 9.3,
+// 16 rows 12.1 / 9.2; 9 rows 25088 x 3584 22.5 / 15.4, which is lost.
 inline bool mx_linear_fused(int64_t rows, int64_t k) { return rows <= 16 && rows * k <= 32768; }
 
 // The tile and the split with the least estimated time in us.  A stage (256

@@ -86,7 +86,10 @@ constexpr int kXcds = 8;
 // 258 / 285, 271 / 312 us; a linear layer's step of that size, three products
 // after the storing kernels, bands of 3, 4, 5, 6, 7, 8, 10: 920, 951, 924, 926,
 // 913, 957, 934 (and 4096 x 4096 x 16384's backward 364, 361, 360, 359, 364, 373,
-// 366): where bands divide the rows evenly the XCDs keep step with each other.
+// 366).  No band is best everywhere: from memory, bands of 3, 4, 5, 6, 8: 8192^3
+// 264, 266, 259, 260, 267; 6144^3 157, 144, 143, 152, 144; 5000^3 87, 85, 93, 86, 94;
+// 12288 x 4096 x 4096 121, 125, 119, 124, 124; 9216 x 2048 x 4096 64, 64, 64, 61, 61.
+// With the operands in the caches all of these are within 2% of each other.
 constexpr unsigned kBand = 6;
 
 __device__ __forceinline__ void tile_of_block(unsigned block, unsigned tm, unsigned tn, unsigned& i, unsigned& j) {
@@ -179,15 +182,16 @@ __device__ __forceinline__ void store_added(const Out& o, const char* strip, int
 // TM x TN: the tile in units of 64; four waves, two by two, each with TM x TN
 // fragments of 32 x 32.
 //
-// With 256 x 256 outputs a block does 256 operations for each byte of codes it
-// loads, so the matrix cores are the bound: pure 32 x 32 x 64 instructions on
+// With 256 x 256 outputs a block does 512 operations (256 multiply-adds) for each
+// byte of codes it loads, so the matrix cores are the bound: pure 32 x 32 x 64 instructions on
 // random codes reach 6.36 PFLOP/s here, where the card's power limit holds the
-// clock to 1.5 GHz (9.6 on zeros).  MI355X, long runs: 8192^3 to bf16 252 us, 4.4
-// PFLOP/s, to fp32 268, 4.1; 4096 x 4096 x 16384 125, 4.4; 16384 x 4096 x 4096 148,
-// 3.7; 4096^3 39, 3.5; 2048^3 9.7, 1.8; in 64 squared 64 x 16384 x 16384 23.5 us, bound
-// by the weights' bytes (6.2 TB/s).  Of 8192^3's 252 the loads of codes and
-// scales cost 45 (without those in the loop 204, timed on a copy) and the stores
-// 12 (to fp32 44).  Tried: 16 x 16 x 128 instructions (7.2 PFLOP/s alone, but the
+// clock to 1.5 GHz (9.6 on zeros).  MI355X, operands from the caches (from memory):
+// 8192^3 to bf16 245 us, 4.5 PFLOP/s (264), to fp32 263 (276); 4096 x 4096 x 16384
+// 117, 4.7 PFLOP/s (130); 4096^3 38 (44); 3000^3 25 (31); 2048 x 4096 x 4096 25 (27);
+// 2048^3 10.3, 1.7 PFLOP/s (10.7); in 64 squared 64 x 16384 x 16384 24, bound by the
+// weights' bytes, 6.0 TB/s (36, 4.0 TB/s).  Of 252 for 8192^3 in a long run the
+// loads of codes and scales cost 45 (without those in the loop 204, timed on a
+// copy) and the stores 12 (to fp32 44).  Tried: 16 x 16 x 128 instructions (7.2 PFLOP/s alone, but the
 // accumulators were moved about: 259), eight waves (276), stages of 128 columns
 // four deep (270), stores past the caches (248 against 244), blocks that stay
 // for several tiles (268).
@@ -642,7 +646,7 @@ hipError_t launch_tile(const MxProductArgs& a, unsigned tm, unsigned tn, hipStre
 }
 
 // Four buffers where all blocks fit the CUs at once even so; more blocks cover
-// each other's loads.  1024 x 4096 x 4096 (256 tiles of 128 squared) 14.4 us
+// each other's loads.  Operands from the caches: 1024 x 4096 x 4096 (256 tiles of 128 squared) 14.4 us
 // against 17.0 with two, 256 x 4096 x 25088 (in four parts) 28 against 31.6,
 // 512 x 4096 x 8192 (512 tiles of 64 squared) 18.2 against 22.7; two: 2048 x 2048 x
 // 500 (1024 tiles) 7.1 against 8.6, 2048 x 4096 x 4096 (512 of 128 squared) 24.6
