@@ -235,7 +235,8 @@ class GradClip:
             raise ValueError(f"{what} differ in number or size from the handle's")
         if list(map(attrgetter("dtype"), tensors)) != dtypes:
             raise ValueError(f"{what} differ in type from the handle's")
-        if not all(map(T.is_contiguous, tensors)) and not (any_order and all(map(_dense, tensors))):
+        if not all(map(T.is_contiguous, tensors)) and not (
+                any_order and all(t.is_contiguous() or _dense(t) for t in tensors)):
             raise ValueError(f"{what} must be contiguous")
         return array.array("Q", map(T.data_ptr, tensors))
 

@@ -548,3 +548,10 @@ def test_graph_replays_of_two_launches(how):
         if how != "stack":
             check_norms(eager, [norm64(new)])
     h.close()
+
+
+def test_empty_tensors_beside_dense_ones():
+    g = [rand(600).view(20, 30).t()] + [torch.zeros(s, device="cuda") for s in ((3, 0), (0, 3), (0,), (2, 0, 3))]
+    h = clip.GradClip.for_tensors(g)
+    check_norms(h.norm(g), [norm64(g[:1])])
+    h.close()
