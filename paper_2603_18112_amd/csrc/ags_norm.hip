@@ -1,0 +1,460 @@
+// gfx950 kernels of the layer norm (include/ags_norm.h).
+//
+// norm_kernel           a wave or a block keeps a row in registers: read once,
+//                       written once.
+// norm_long_kernel      rows that do not fit: read three times, mostly from the
+//                       caches.
+// norm_backward_kernel  the same for dx; every lane also sums the weight's and the
+//                       bias's gradients of its columns over the block's rows.
+// norm_dx_long_kernel, norm_columns_kernel   the two separately, for long rows.
+// norm_join_kernel      adds the blocks' sums.
+#include <type_traits>
+
+#include "ags_mx_device.h"
+#include "ags_norm_internal.h"
+
+namespace ags {
+namespace {
+
+using mx::load8;
+using mx::Unaligned;
+typedef mx::v2f v2f;
+typedef mx::v2bf v2bf;
+
+__device__ __forceinline__ unsigned pack2(float x, float y) {
+    const v2bf v = __builtin_convertvector((v2f{x, y}), v2bf);
+    unsigned u;
+    __builtin_memcpy(&u, &v, 4);
+    return u;
+}
+
+// 8 elements to p, as many as lie in the row.
+__device__ __forceinline__ void store8(unsigned short* p, int64_t left, const float* x) {
+    Unaligned<unsigned, 4, 2> w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w.v[i] = pack2(x[2 * i], x[2 * i + 1]);
+    if (left >= 8) {
+        *reinterpret_cast<Unaligned<unsigned, 4, 2>*>(p) = w;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < left) p[i] = (unsigned short)(w.v[i >> 1] >> (16 * (i & 1)));
+}
+__device__ __forceinline__ void store8(float* p, int64_t left, const float* x) {
+    if (left >= 8) {
+        Unaligned<float, 8, 4> w;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w.v[i] = x[i];
+        *reinterpret_cast<Unaligned<float, 8, 4>*>(p) = w;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < left) p[i] = x[i];
+}
+
+// A tensor of either type, element `at` on.
+__device__ __forceinline__ void load8_any(const void* p, bool bf16, int64_t at, int64_t left, float* x) {
+    if (bf16) load8(static_cast<const unsigned short*>(p) + at, left, x);
+    else load8(static_cast<const float*>(p) + at, left, x);
+}
+__device__ __forceinline__ void store8_any(void* p, bool bf16, int64_t at, int64_t left, const float* x) {
+    if (bf16) store8(static_cast<unsigned short*>(p) + at, left, x);
+    else store8(static_cast<float*>(p) + at, left, x);
+}
+
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    return v;
+}
+
+// Sums of N values over the G lanes of a row, in every lane.  Over a block they
+// meet in LDS, in slot 0 or 1 in turn: one barrier a sum, since the next sum's
+// barrier lies between two uses of a slot.
+template <int G, int N>
+__device__ __forceinline__ void row_sum(float (&v)[N], float (*red)[N][16], int slot) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
+    if constexpr (G > 64) {
+        constexpr int kWaves = G / 64;
+        if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) red[slot][i][threadIdx.x >> 6] = v[i];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            float s = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) s += red[slot][i][w];
+            v[i] = s;
+        }
+    }
+}
+
+// ---------------------------------------------------------------- forward --
+
+// G lanes to a row, NV pieces of 8 elements each; a block of B threads has B / G
+// rows at a time.  T: x's type.
+template <typename T, int G, int NV, int B>
+__global__ __launch_bounds__(B) void norm_kernel(NormArgs a) {
+    __shared__ float red[2][1][16];
+    const int lane = threadIdx.x % G;
+    const int64_t cols = a.cols, step = (int64_t)gridDim.x * (B / G);
+    float w[NV][8], b[NV][8];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int64_t c = ((int64_t)j * G + lane) * 8;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[j][i] = 1.0f, b[j][i] = 0.0f;
+        if (c < cols) {
+            if (a.weight) load8_any(a.weight, a.w_bf16, c, cols - c, w[j]);
+            if (a.bias) load8_any(a.bias, a.w_bf16, c, cols - c, b[j]);
+        }
+    }
+    for (int64_t row = (int64_t)blockIdx.x * (B / G) + threadIdx.x / G; row < a.rows; row += step) {
+        const T* p = static_cast<const T*>(a.x) + row * a.x_stride;
+        float x[NV][8], s[1] = {0.0f};
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int64_t c = ((int64_t)j * G + lane) * 8;
+            load8(p + c, cols - c, x[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[0] += x[j][i];
+        row_sum<G, 1>(s, red, 0);
+        const float mean = s[0] / (float)cols;
+        s[0] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int64_t c = ((int64_t)j * G + lane) * 8;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                x[j][i] -= mean;
+                if (c + i < cols) s[0] = fmaf(x[j][i], x[j][i], s[0]);
+            }
+        }
+        row_sum<G, 1>(s, red, 1);
+        const float rstd = 1.0f / sqrtf(s[0] / (float)cols + a.eps);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int64_t c = ((int64_t)j * G + lane) * 8;
+            if (c >= cols) continue;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[j][i] = fmaf(x[j][i] * rstd, w[j][i], b[j][i]);
+            store8_any(a.y, a.y_bf16, row * a.y_stride + c, cols - c, x[j]);
+        }
+        if (a.saved && lane == 0) {
+            a.saved[row] = mean;
+            a.saved[a.rows + row] = rstd;
+        }
+    }
+}
+
+constexpr int kLong = 1024;  // threads to a long row
+
+template <typename T>
+__global__ __launch_bounds__(kLong) void norm_long_kernel(NormArgs a) {
+    __shared__ float red[2][1][16];
+    const int64_t cols = a.cols;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const T* p = static_cast<const T*>(a.x) + row * a.x_stride;
+        float s[1] = {0.0f}, x[8];
+        for (int64_t c = threadIdx.x * 8; c < cols; c += kLong * 8) {
+            load8(p + c, cols - c, x);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[0] += x[i];
+        }
+        row_sum<kLong, 1>(s, red, 0);
+        const float mean = s[0] / (float)cols;
+        s[0] = 0.0f;
+        for (int64_t c = threadIdx.x * 8; c < cols; c += kLong * 8) {
+            load8(p + c, cols - c, x);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float d = x[i] - mean;
+                if (c + i < cols) s[0] = fmaf(d, d, s[0]);
+            }
+        }
+        row_sum<kLong, 1>(s, red, 1);
+        const float rstd = 1.0f / sqrtf(s[0] / (float)cols + a.eps);
+        for (int64_t c = threadIdx.x * 8; c < cols; c += kLong * 8) {
+            float w[8] = {1, 1, 1, 1, 1, 1, 1, 1}, b[8] = {};
+            if (a.weight) load8_any(a.weight, a.w_bf16, c, cols - c, w);
+            if (a.bias) load8_any(a.bias, a.w_bf16, c, cols - c, b);
+            load8(p + c, cols - c, x);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = fmaf((x[i] - mean) * rstd, w[i], b[i]);
+            store8_any(a.y, a.y_bf16, row * a.y_stride + c, cols - c, x);
+        }
+        if (a.saved && threadIdx.x == 0) {
+            a.saved[row] = mean;
+            a.saved[a.rows + row] = rstd;
+        }
+    }
+}
+
+// --------------------------------------------------------------- backward --
+
+// As norm_kernel; DW: the sums over the block's rows are wanted too.  A part is
+// a block's rows.
+template <typename T, int G, int NV, int B, bool DW>
+__global__ __launch_bounds__(B) void norm_backward_kernel(NormBackwardArgs a) {
+    __shared__ float red[2][2][16];
+    const int lane = threadIdx.x % G;
+    const int64_t cols = a.cols, step = (int64_t)gridDim.x * (B / G);
+    float w[NV][8], dw[NV][8], db[NV][8];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int64_t c = ((int64_t)j * G + lane) * 8;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[j][i] = 1.0f, dw[j][i] = 0.0f, db[j][i] = 0.0f;
+        if (c < cols && a.weight) load8_any(a.weight, a.w_bf16, c, cols - c, w[j]);
+    }
+    int slot = 0;
+    for (int64_t row = (int64_t)blockIdx.x * (B / G) + threadIdx.x / G; row < a.rows; row += step, slot ^= 1) {
+        const T *px = static_cast<const T*>(a.x) + row * a.x_stride, *pd = static_cast<const T*>(a.dy) + row * a.dy_stride;
+        const float mean = a.saved[row], rstd = a.saved[a.rows + row];
+        float z[NV][8], g[NV][8], s[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int64_t c = ((int64_t)j * G + lane) * 8;
+            load8(px + c, cols - c, z[j]);
+            load8(pd + c, cols - c, g[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                z[j][i] = (z[j][i] - mean) * rstd;
+                if constexpr (DW) {
+                    dw[j][i] = fmaf(g[j][i], z[j][i], dw[j][i]);
+                    db[j][i] += g[j][i];
+                }
+                g[j][i] *= w[j][i];
+                s[0] += g[j][i];
+                s[1] = fmaf(g[j][i], z[j][i], s[1]);  // (past the row's end g is zero)
+            }
+        if (!a.dx) continue;
+        row_sum<G, 2>(s, red, slot);
+        const float m0 = s[0] / (float)cols, m1 = s[1] / (float)cols;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int64_t c = ((int64_t)j * G + lane) * 8;
+            if (c >= cols) continue;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z[j][i] = rstd * (g[j][i] - m0 - z[j][i] * m1);
+            store8(static_cast<T*>(a.dx) + row * a.dx_stride + c, cols - c, z[j]);
+        }
+    }
+    if constexpr (DW) {
+        float* out = a.partials + (int64_t)blockIdx.x * 2 * cols;
+        if constexpr (G == B) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                const int64_t c = ((int64_t)j * G + lane) * 8;
+                if (c >= cols) continue;
+                store8(out + c, cols - c, dw[j]);
+                store8(out + cols + c, cols - c, db[j]);
+            }
+        } else {
+            // the block's waves, each with rows of its own, one after the other
+            __shared__ float sum[2][G * NV * 8];
+            for (int k = 0; k < B / G; ++k) {
+                if ((int)threadIdx.x / G == k) {
+#pragma unroll
+                    for (int j = 0; j < NV; ++j)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const int at = (j * 8 + i) * G + lane;
+                            sum[0][at] = k ? sum[0][at] + dw[j][i] : dw[j][i];
+                            sum[1][at] = k ? sum[1][at] + db[j][i] : db[j][i];
+                        }
+                }
+                __syncthreads();
+            }
+            for (int t = threadIdx.x; t < 2 * G * NV; t += B) {
+                const int which = t / (G * NV), j = t / G % NV, l = t % G;
+                const int64_t c = ((int64_t)j * G + l) * 8;
+                if (c >= cols) continue;
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = sum[which][(j * 8 + i) * G + l];
+                store8(out + which * cols + c, cols - c, v);
+            }
+        }
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kLong) void norm_dx_long_kernel(NormBackwardArgs a) {
+    __shared__ float red[2][2][16];
+    const int64_t cols = a.cols;
+    int slot = 0;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, slot ^= 1) {
+        const T *px = static_cast<const T*>(a.x) + row * a.x_stride, *pd = static_cast<const T*>(a.dy) + row * a.dy_stride;
+        const float mean = a.saved[row], rstd = a.saved[a.rows + row];
+        float s[2] = {0.0f, 0.0f};
+        for (int pass = 0; pass < 2; ++pass) {
+            const float m0 = s[0] / (float)cols, m1 = s[1] / (float)cols;
+            for (int64_t c = threadIdx.x * 8; c < cols; c += kLong * 8) {
+                float z[8], g[8], w[8] = {1, 1, 1, 1, 1, 1, 1, 1};
+                load8(px + c, cols - c, z);
+                load8(pd + c, cols - c, g);
+                if (a.weight) load8_any(a.weight, a.w_bf16, c, cols - c, w);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    z[i] = (z[i] - mean) * rstd;
+                    g[i] *= w[i];
+                    if (pass == 0) {
+                        s[0] += g[i];
+                        s[1] = fmaf(g[i], z[i], s[1]);
+                    } else {
+                        z[i] = rstd * (g[i] - m0 - z[i] * m1);
+                    }
+                }
+                if (pass == 1) store8(static_cast<T*>(a.dx) + row * a.dx_stride + c, cols - c, z);
+            }
+            if (pass == 0) row_sum<kLong, 2>(s, red, slot);
+        }
+    }
+}
+
+// A block takes 512 columns of a part's rows, each wave every fourth row.
+template <typename T>
+__global__ __launch_bounds__(256) void norm_columns_kernel(NormBackwardArgs a) {
+    __shared__ float sum[2][4][512];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t cols = a.cols, c = ((int64_t)blockIdx.x * 64 + lane) * 8;
+    const int64_t r0 = a.rows * blockIdx.y / a.parts, r1 = a.rows * (blockIdx.y + 1) / a.parts;
+    float dw[8] = {}, db[8] = {};
+    if (c < cols) {
+        for (int64_t row = r0 + wave; row < r1; row += 4) {
+            float z[8], g[8];
+            load8(static_cast<const T*>(a.x) + row * a.x_stride + c, cols - c, z);
+            load8(static_cast<const T*>(a.dy) + row * a.dy_stride + c, cols - c, g);
+            const float mean = a.saved[row], rstd = a.saved[a.rows + row];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                dw[i] = fmaf(g[i], (z[i] - mean) * rstd, dw[i]);
+                db[i] += g[i];
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        sum[0][wave][i * 64 + lane] = dw[i];
+        sum[1][wave][i * 64 + lane] = db[i];
+    }
+    __syncthreads();
+    if (wave >= 2 || c >= cols) return;
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int at = i * 64 + lane;
+        v[i] = sum[wave][0][at] + sum[wave][1][at] + (sum[wave][2][at] + sum[wave][3][at]);
+    }
+    store8(a.partials + ((int64_t)blockIdx.y * 2 + wave) * cols + c, cols - c, v);
+}
+
+// 64 columns of one of the two gradients to a block; its waves share the parts.
+constexpr int kJoinWaves = 8;
+
+__global__ __launch_bounds__(kJoinWaves * 64) void norm_join_kernel(NormBackwardArgs a) {
+    __shared__ float sum[kJoinWaves][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t tiles = (a.cols + 63) / 64, cols = a.cols;
+    const int which = blockIdx.x >= tiles;
+    void* out = which ? a.dbias : a.dweight;
+    if (!out) return;
+    const int64_t c = (blockIdx.x - which * tiles) * 64 + lane;
+    float v = 0.0f;
+    if (c < cols) {
+        const float* p = a.partials + which * cols + c;
+#pragma unroll 8
+        for (int k = wave; k < a.parts; k += kJoinWaves) v += p[(int64_t)k * 2 * cols];
+    }
+    sum[wave][lane] = v;
+    __syncthreads();
+    if (wave || c >= cols) return;
+    v = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kJoinWaves; ++k) v += sum[k][lane];
+    if (a.dw_bf16) {
+        unsigned short* o = static_cast<unsigned short*>(out) + c;
+        if (a.accumulate) v += __uint_as_float((unsigned)*o << 16);
+        *o = (unsigned short)pack2(v, 0.0f);
+    } else {
+        float* o = static_cast<float*>(out) + c;
+        *o = a.accumulate ? v + *o : v;
+    }
+}
+
+// Blocks that the card holds at once are enough: they go through the rows.
+unsigned norm_blocks(int64_t rows, int64_t at_once, int64_t most) {
+    return (unsigned)std::max<int64_t>(1, std::min<int64_t>((rows + at_once - 1) / at_once, most));
+}
+
+template <typename T>
+hipError_t forward(const NormArgs& a, hipStream_t s) {
+    const int64_t n = a.cols;
+#define NORM_FORWARD(G, NV, B, MOST)                                                                       \
+    hipLaunchKernelGGL((norm_kernel<T, G, NV, B>), dim3(norm_blocks(a.rows, B / G, MOST)), dim3(B), 0, s, a)
+    if (n <= 512) NORM_FORWARD(64, 1, 256, 2048);
+    else if (n <= 1024) NORM_FORWARD(64, 2, 256, 1536);
+    else if (n <= 2048) NORM_FORWARD(256, 1, 256, 2048);
+    else if (n <= 4096) NORM_FORWARD(256, 2, 256, 1536);
+    else if (n <= 8192) NORM_FORWARD(512, 2, 512, 768);
+    else if (n <= 16384) NORM_FORWARD(1024, 2, 1024, 512);
+    else if (n <= kNormForwardCols) NORM_FORWARD(1024, 4, 1024, 256);
+    else
+        hipLaunchKernelGGL((norm_long_kernel<T>), dim3(norm_blocks(a.rows, 1, 512)), dim3(kLong), 0, s, a);
+#undef NORM_FORWARD
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t backward(const NormBackwardArgs& a, hipStream_t s) {
+    const int64_t n = a.cols;
+    const bool dw = a.dweight || a.dbias;
+#define NORM_BACKWARD(G, NV, B)                                                                                   \
+    do {                                                                                                          \
+        if (dw) hipLaunchKernelGGL((norm_backward_kernel<T, G, NV, B, true>), dim3(a.parts), dim3(B), 0, s, a);   \
+        else hipLaunchKernelGGL((norm_backward_kernel<T, G, NV, B, false>),                                       \
+                                dim3(norm_blocks(a.rows, B / G, 1024)), dim3(B), 0, s, a);                        \
+    } while (0)
+    if (a.rows == 0) {}  // empty sums
+    else if (n <= 512) NORM_BACKWARD(64, 1, 512);
+    else if (n <= 1024) NORM_BACKWARD(64, 2, 256);
+    else if (n <= 2048) NORM_BACKWARD(256, 1, 256);
+    else if (n <= 4096) NORM_BACKWARD(256, 2, 256);
+    else if (n <= 8192) NORM_BACKWARD(512, 2, 512);
+    else if (n <= kNormBackwardCols) NORM_BACKWARD(1024, 2, 1024);
+    else {
+        if (a.dx)
+            hipLaunchKernelGGL((norm_dx_long_kernel<T>), dim3(norm_blocks(a.rows, 1, 512)), dim3(kLong), 0, s, a);
+        if (dw)
+            hipLaunchKernelGGL((norm_columns_kernel<T>), dim3((unsigned)((n + 511) / 512), a.parts), dim3(256), 0, s, a);
+    }
+#undef NORM_BACKWARD
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !dw) return e;
+    hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)(2 * ((n + 63) / 64))), dim3(kJoinWaves * 64), 0, s, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_norm(const NormArgs& a, hipStream_t s) {
+    return a.bf16 ? forward<unsigned short>(a, s) : forward<float>(a, s);
+}
+
+hipError_t launch_norm_backward(const NormBackwardArgs& a, hipStream_t s) {
+    return a.bf16 ? backward<unsigned short>(a, s) : backward<float>(a, s);
+}
+
+}  // namespace ags
