@@ -11,8 +11,9 @@ behind the C-ABI library ``libags.so`` (see ``include/ags.h``).
 only); ``layouts`` and ``synth`` describe flat layouts and draw seeded
 synthetic inputs.  ``clip`` (gradient clipping, ``include/ags_clip.h``) and
 ``mx`` (4-bit linear layers, ``include/ags_mx.h``) bind the operators that
-stand around the step in the same library, as does ``norm`` (layer norm,
-``include/ags_norm.h``).
+stand around the step in the same library, as do ``norm`` (layer norm,
+``include/ags_norm.h``) and ``glu`` (gated feed-forward products,
+``include/ags_glu.h``).
 """
 
-__all__ = ["layouts", "synth", "ags", "clip", "mx", "norm"]
+__all__ = ["layouts", "synth", "ags", "clip", "mx", "norm", "glu"]

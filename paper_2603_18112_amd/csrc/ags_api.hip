@@ -1395,3 +1395,4 @@ extern "C" ags_status ags_stats_noalloc(const ags_config* cfg, const float* d_w,
 #include "ags_clip_api.inc"
 #include "ags_mx_api.inc"
 #include "ags_norm_api.inc"
+#include "ags_glu_api.inc"

@@ -11,6 +11,7 @@
 
 #include "ags_mx_device.h"
 #include "ags_mx_internal.h"
+#include "ags_tile_device.h"
 
 #ifndef __gfx950__
 #ifdef __HIP_DEVICE_COMPILE__
@@ -20,6 +21,12 @@
 
 namespace ags {
 namespace {
+
+using tile::block_barrier;
+using tile::load_lds16;
+using tile::load_lds4;
+using tile::tile_of_block;
+using tile::wait_loads;
 
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
@@ -77,11 +84,7 @@ __device__ __forceinline__ void store4(const Out& o, int64_t i, int64_t j, float
 
 // ------------------------------------------------------------ tile kernel --
 
-constexpr int kXcds = 8;
-
-// Consecutive blocks go to the 8 XCDs in turn.  Each XCD takes a run of
-// consecutive tiles, and tiles are numbered in bands of kBand rows, so the
-// blocks that share an XCD's L2 read few rows and few columns.  8192^3 to bf16 /
+// Tiles in bands of kBand rows (tile_of_block): 8192^3 to bf16 /
 // fp32, bands of 1, 4, 6, 8, 16, 64: 265 / 311, 252 / 269, 252 / 268, 252 / 276,
 // 258 / 285, 271 / 312 us; a linear layer's step of that size, three products
 // after the storing kernels, bands of 3, 4, 5, 6, 7, 8, 10: 920, 951, 924, 926,
@@ -91,42 +94,6 @@ constexpr int kXcds = 8;
 // 12288 x 4096 x 4096 121, 125, 119, 124, 124; 9216 x 2048 x 4096 64, 64, 64, 61, 61.
 // With the operands in the caches all of these are within 2% of each other.
 constexpr unsigned kBand = 6;
-
-__device__ __forceinline__ void tile_of_block(unsigned block, unsigned tm, unsigned tn, unsigned& i, unsigned& j) {
-    const unsigned total = tm * tn, xcd = block % kXcds, at = block / kXcds;
-    const unsigned base = total / kXcds, rest = total % kXcds;
-    const unsigned t = xcd * base + min(xcd, rest) + at;
-    const unsigned band = t / (kBand * tn), first = band * kBand, h = min(kBand, tm - first);
-    const unsigned in = t - band * kBand * tn;
-    i = first + in % h;
-    j = in / h;
-}
-
-// Loads from memory straight into LDS: 64 lanes of 16 (or 4) bytes, lane after
-// lane from LDS byte `to`.  Written out because the compiler would wait for
-// all of them before the next LDS read; wait_loads() does so once a stage.
-// (m0 is reserved: the compiler sets it anew where it needs it itself.)
-__device__ __forceinline__ void load_lds16(__amdgpu_buffer_rsrc_t r, unsigned to, unsigned lane_off, unsigned off) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(lane_off),
-                 "s"(r), "s"(off)
-                 : "memory");
-}
-__device__ __forceinline__ void load_lds4(__amdgpu_buffer_rsrc_t r, unsigned to, unsigned lane_off, unsigned off) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(to), "v"(lane_off),
-                 "s"(r), "s"(off)
-                 : "memory");
-}
-
-// Waits until at most N of this wave's loads are under way.
-template <int N>
-__device__ __forceinline__ void wait_loads() {
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-}
-__device__ __forceinline__ void block_barrier() {
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-}
 
 // 32 rows of BYTES bytes from LDS (PITCH apart) to memory, those of the first
 // `rows` rows and `bytes` bytes.  T: the elements, whose alignment is all that
@@ -205,7 +172,7 @@ __device__ __forceinline__ void tile_product(const MxProductArgs& a, unsigned ti
     const unsigned tiles = tiles_m * tiles_n;
     const unsigned split = blockIdx.x / tiles;
     unsigned ti, tj;
-    tile_of_block(blockIdx.x % tiles, tiles_m, tiles_n, ti, tj);
+    tile_of_block<kBand>(blockIdx.x % tiles, tiles_m, tiles_n, ti, tj);
     const int64_t i0 = (int64_t)ti * BM, j0 = (int64_t)tj * BN;
     const unsigned pitch = (unsigned)(a.kp / 2);
     const int stages = (int)(a.kp / 256);
