@@ -12,8 +12,9 @@ only); ``layouts`` and ``synth`` describe flat layouts and draw seeded
 synthetic inputs.  ``clip`` (gradient clipping, ``include/ags_clip.h``) and
 ``mx`` (4-bit linear layers, ``include/ags_mx.h``) bind the operators that
 stand around the step in the same library, as do ``norm`` (layer norm,
-``include/ags_norm.h``) and ``glu`` (gated feed-forward products,
-``include/ags_glu.h``).
+``include/ags_norm.h``), ``glu`` (gated feed-forward products,
+``include/ags_glu.h``) and ``muon`` (orthogonalised updates,
+``include/ags_muon.h``).
 """
 
-__all__ = ["layouts", "synth", "ags", "clip", "mx", "norm", "glu"]
+__all__ = ["layouts", "synth", "ags", "clip", "mx", "norm", "glu", "muon"]

@@ -14,7 +14,8 @@ LIB = os.path.join(LIBDIR, "libags.so")
 SOURCES = [os.path.join(CSRC, "ags_api.hip"), os.path.join(CSRC, "ags_kernels.hip"),
            os.path.join(CSRC, "ags_plan.cpp"), os.path.join(CSRC, "ags_clip.hip"),
            os.path.join(CSRC, "ags_mx_quant.hip"), os.path.join(CSRC, "ags_mx_product.hip"),
-           os.path.join(CSRC, "ags_norm.hip"), os.path.join(CSRC, "ags_glu.hip")]
+           os.path.join(CSRC, "ags_norm.hip"), os.path.join(CSRC, "ags_glu.hip"),
+           os.path.join(CSRC, "ags_muon.hip")]
 HEADERS = [os.path.join(CSRC, "ags_internal.h"), os.path.join(INCLUDE, "ags.h"),
            os.path.join(INCLUDE, "ags_plan.h"), os.path.join(INCLUDE, "ags_clip.h"),
            os.path.join(CSRC, "ags_clip_internal.h"), os.path.join(CSRC, "ags_clip_api.inc"),
@@ -23,7 +24,9 @@ HEADERS = [os.path.join(CSRC, "ags_internal.h"), os.path.join(INCLUDE, "ags.h"),
            os.path.join(INCLUDE, "ags_norm.h"), os.path.join(CSRC, "ags_norm_internal.h"),
            os.path.join(CSRC, "ags_norm_api.inc"), os.path.join(INCLUDE, "ags_glu.h"),
            os.path.join(CSRC, "ags_gemm_internal.h"), os.path.join(CSRC, "ags_gemm_device.h"),
-           os.path.join(CSRC, "ags_glu_internal.h"), os.path.join(CSRC, "ags_glu_api.inc")]
+           os.path.join(CSRC, "ags_glu_internal.h"), os.path.join(CSRC, "ags_glu_api.inc"),
+           os.path.join(INCLUDE, "ags_muon.h"), os.path.join(CSRC, "ags_muon_internal.h"),
+           os.path.join(CSRC, "ags_muon_api.inc")]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

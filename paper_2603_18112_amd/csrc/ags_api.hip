@@ -1396,3 +1396,4 @@ extern "C" ags_status ags_stats_noalloc(const ags_config* cfg, const float* d_w,
 #include "ags_mx_api.inc"
 #include "ags_norm_api.inc"
 #include "ags_glu_api.inc"
+#include "ags_muon_api.inc"

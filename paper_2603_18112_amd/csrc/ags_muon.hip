@@ -1,0 +1,403 @@
+// gfx950 kernels of the orthogonalised updates (include/ags_muon.h).
+//
+// muon_sum_kernel     the replicas' mean, the momentum, U; sums of its squares
+// muon_start_kernel   X = U / (|U| + eps), as fp32 and as operands
+// muon_gram_kernel    A = X X' (or X' X)
+// muon_square_kernel  b A + c A A
+// muon_apply_kernel   X <- a X + (b A + c A A) X; the last one updates the weights
+//
+// Every launch covers all matrices: a block finds its tile in a table, or from
+// its number where all matrices are alike.
+#include "ags_gemm_device.h"
+#include "ags_muon_internal.h"
+
+namespace ags {
+namespace {
+
+using gemm::Side;
+using gemm::store8;
+using mx::load8;
+using mx::Unaligned;
+typedef unsigned short u16;
+typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+
+// Powers of two that bring the operands into fp16's range: X and A have
+// singular values up to 1.38 and 1.9, b A + c A A up to 3.9 (the schedule is
+// checked for these), so no element exceeds 2^16 - 2^5; elements down to 2^-14
+// of the scale keep 11 bits.  (The usual coefficients: 1.20, 1.45, 2.81.)
+constexpr float kScaleX = 32768.0f, kScaleA = 32768.0f, kScaleB = 16384.0f;
+
+__device__ __forceinline__ unsigned pack_half(float x, float y) {
+    const v2h v = __builtin_convertvector((mx::v2f{x, y}), v2h);
+    unsigned u;
+    __builtin_memcpy(&u, &v, 4);
+    return u;
+}
+
+// 8 elements as fp16 to an aligned place, zeros from `left` on.
+__device__ __forceinline__ void store_half8(u16* p, int64_t left, const float* x) {
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = i < left ? x[i] : 0.0f;
+    *reinterpret_cast<uint4*>(p) =
+        make_uint4(pack_half(y[0], y[1]), pack_half(y[2], y[3]), pack_half(y[4], y[5]), pack_half(y[6], y[7]));
+}
+__device__ __forceinline__ void load_half8(const u16* p, float* x) {
+    const gemm::v8h v = *reinterpret_cast<const gemm::v8h*>(p);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = (float)v[i];
+}
+
+// The matrix of this block and its number in it (i, j: its tile; i: its chunk).
+// Blocks of one matrix go to one XCD as far as that balances: blocks b, b + 8,
+// ... share one.
+struct Found {
+    MuonMatrix m;
+    int64_t index;  // in a batch
+    int32_t i, j;
+};
+
+template <bool TILES>
+__device__ __forceinline__ Found find(const MuonWork& w) {
+    Found f;
+    if (w.tiles) {
+        const MuonTile t = w.tiles[blockIdx.x];
+        f.m = w.matrices[t.matrix];
+        f.index = 0;
+        f.i = t.i;
+        f.j = t.j;
+        return f;
+    }
+    const unsigned total = (unsigned)w.blocks, xcd = blockIdx.x % tile::kXcds, at = blockIdx.x / tile::kXcds;
+    const unsigned base = total / tile::kXcds, rest = total % tile::kXcds;
+    const unsigned b = xcd * base + min(xcd, rest) + at;
+    f.m = w.one;
+    f.index = b / (unsigned)w.each;
+    const unsigned t = b % (unsigned)w.each;
+    f.m.ws += f.index * f.m.bytes();
+    if (!TILES) {
+        f.i = (int)t;
+        f.j = 0;
+    } else if (w.tiles_n) {
+        f.i = (int)(t / (unsigned)w.tiles_n);
+        f.j = (int)(t % (unsigned)w.tiles_n);
+    } else {  // t = i (i + 1) / 2 + j, j <= i
+        int i = (int)((sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f);
+        while (i * (i + 1) / 2 > (int)t) --i;
+        while ((i + 1) * (i + 2) / 2 <= (int)t) ++i;
+        f.i = i;
+        f.j = (int)t - i * (i + 1) / 2;
+    }
+    return f;
+}
+
+// ------------------------------------------------------------- elements --
+
+constexpr int kThreads = 256;
+
+__device__ __forceinline__ double block_sum(double v, double* red) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return (red[0] + red[1]) + (red[2] + red[3]);
+}
+
+// Eight elements of the tensor that is orthogonalised.
+__device__ __forceinline__ void load_x(const MuonStepArgs& a, const Found& f, int64_t row, int64_t c, float* x) {
+    const int64_t at = f.index * a.batch_stride + row * a.row_stride + c, left = f.m.cols - c;
+    if (a.bf16) load8(static_cast<const u16*>(a.grads) + at, left, x);
+    else load8(static_cast<const float*>(a.grads) + at, left, x);
+}
+
+template <typename T>
+__device__ __forceinline__ void mean8(const MuonStepArgs& a, int64_t at, int64_t left, float* g) {
+    const T* p = static_cast<const T*>(a.grads) + at;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) g[i] = 0.0f;
+    int k = 0;
+    for (; k + 4 <= a.K; k += 4) {
+        float y[4][8];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) load8(p + (k + u) * a.stride, left, y[u]);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) g[i] += y[u][i];
+    }
+    for (; k < a.K; ++k) {
+        float y[8];
+        load8(p + k * a.stride, left, y);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) g[i] += y[i];
+    }
+    const float n = (float)a.K;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) g[i] /= n;
+}
+
+// A chunk's pieces of 8 elements, thread after thread.
+__global__ __launch_bounds__(kThreads) void muon_sum_kernel(MuonStepArgs a) {
+    __shared__ double red[4];
+    const Found f = find<false>(a.work);
+    const unsigned per_row = (unsigned)(f.m.pitch() / 8), total = (unsigned)f.m.rows * per_row;
+    const unsigned end = min(total, (unsigned)(f.i + 1) * (unsigned)f.m.chunk);
+    double sum = 0.0;
+    for (unsigned p = (unsigned)f.i * (unsigned)f.m.chunk + threadIdx.x; p < end; p += kThreads) {
+        const int64_t row = p / per_row, c = (int64_t)(p - (unsigned)row * per_row) * 8, left = f.m.cols - c;
+        if (left <= 0) continue;
+        float u[8];
+        if (a.from_x) {
+            load_x(a, f, row, c, u);
+        } else {
+            const int64_t at = f.m.offset + row * f.m.cols + c;
+            float m[8];
+            load8(a.m + at, left, m);
+            if (a.bf16) mean8<u16>(a, at, left, u);
+            else mean8<float>(a, at, left, u);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                m[i] = fmaf(a.momentum, m[i], u[i]);
+                u[i] = a.nesterov ? fmaf(a.momentum, m[i], u[i]) : m[i];
+            }
+            store8(a.m + at, left, m);
+            // (past the row's end u is 0)
+            store8(reinterpret_cast<float*>(a.ws + f.m.x_at()) + row * f.m.pitch() + c, 8, u);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum = fma((double)u[i], (double)u[i], sum);
+    }
+    sum = block_sum(sum, red);
+    if (threadIdx.x == 0) reinterpret_cast<double*>(a.ws + f.m.sums_at())[f.i] = sum;
+}
+
+__global__ __launch_bounds__(kThreads) void muon_start_kernel(MuonStepArgs a) {
+    __shared__ double red[4];
+    const Found f = find<false>(a.work);
+    const double* sums = reinterpret_cast<const double*>(a.ws + f.m.sums_at());
+    double sum = 0.0;
+    for (int i = threadIdx.x; i < f.m.chunks; i += kThreads) sum += sums[i];
+    const double inv = 1.0 / (sqrt(block_sum(sum, red)) + a.eps);
+    const int64_t pitch = f.m.pitch();
+    const unsigned per_row = (unsigned)(pitch / 8), total = (unsigned)f.m.rows * per_row;
+    const unsigned end = min(total, (unsigned)(f.i + 1) * (unsigned)f.m.chunk);
+    float* x = reinterpret_cast<float*>(a.ws + f.m.x_at());
+    u16 *h = reinterpret_cast<u16*>(a.ws + f.m.operand_at(0)), *h1 = reinterpret_cast<u16*>(a.ws + f.m.operand_at(1));
+    for (unsigned p = (unsigned)f.i * (unsigned)f.m.chunk + threadIdx.x; p < end; p += kThreads) {
+        const int64_t row = p / per_row, c = (int64_t)(p - (unsigned)row * per_row) * 8, at = row * pitch + c;
+        float u[8] = {};
+        if (c < f.m.cols) {
+            if (a.from_x) load_x(a, f, row, c, u);
+            else load8(x + at, 8, u);
+            // a zero matrix stays zero with eps = 0 too
+#pragma unroll
+            for (int i = 0; i < 8; ++i) u[i] = u[i] == 0.0f ? 0.0f : (float)((double)u[i] * inv);
+        }
+        store8(x + at, 8, u);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u[i] *= kScaleX;
+        store_half8(h + at, 8, u);
+        // the second form's padding, which the products never write
+        if (c + 8 > f.m.cols) {
+            const float zero[8] = {};
+            store_half8(h1 + at, 8, zero);
+        }
+    }
+    // that of A and b A + c A A
+    const int64_t s = f.m.side(), ap = f.m.a_pitch(), from = s / 8 * 8, pads = (ap - from) / 8;
+    if (s == ap) return;
+    for (int64_t p = (int64_t)f.i * kThreads + threadIdx.x; p < s * pads; p += (int64_t)f.m.chunks * kThreads) {
+        const int64_t at = p / pads * ap + from + p % pads * 8;
+        const float zero[8] = {};
+        store_half8(reinterpret_cast<u16*>(a.ws + f.m.a_at()) + at, 8, zero);
+        store_half8(reinterpret_cast<u16*>(a.ws + f.m.b_at()) + at, 8, zero);
+    }
+}
+
+// ------------------------------------------------------------- products --
+
+// Rows of 8 results: f(t, c, x) for the strip's row t and column c.
+template <int WIDE, typename F>
+__device__ __forceinline__ void each8(const char* sm, int pitch, int lane, int64_t rows, int64_t cols, const F& f) {
+    constexpr int kLanes = WIDE / 8, kRows = 64 / kLanes;
+    const int c = lane % kLanes * 8;
+    if (c >= cols) return;
+    const int end = (int)min(rows, (int64_t)32);
+#pragma unroll 2
+    for (int t = lane / kLanes; t < end; t += kRows) {
+        float x[8];
+        gemm::read8(sm + t * pitch + c * 4, x);
+        f(t, c, x);
+    }
+}
+
+// Tiles below the diagonal are stored above it too: four lanes take the strip's
+// 32 rows of a column, 64 bytes of a row.
+struct SymmetricOut {
+    u16* to;             // A, or b A + c A A
+    const u16* from;     // A, where the latter is made
+    int64_t s, pitch;
+    float add, times;    // x times + A add
+    bool mirror;
+
+    template <int WIDE>
+    __device__ __forceinline__ void strip(char* sm, int sm_pitch, int lane, int64_t row0, int64_t col0, int64_t rows,
+                                          int64_t cols) const {
+        each8<WIDE>(sm, sm_pitch, lane, rows, cols, [&](int t, int c, float* x) {
+            const int64_t at = (row0 + t) * pitch + col0 + c;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] *= times;
+            if (from) {
+                float y[8];
+                load_half8(from + at, y);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = fmaf(y[i], add, x[i]);
+            }
+            store_half8(to + at, cols - c, x);
+            if (mirror) {
+                float* p = reinterpret_cast<float*>(sm + t * sm_pitch + c * 4);
+                *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+                *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+            }
+        });
+        if (!mirror) return;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        const int t = (lane & 3) * 8;
+        if (t >= rows) return;
+#pragma unroll 2
+        for (int c = lane >> 2; c < WIDE; c += 16) {
+            if (c >= cols) break;
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const float*>(sm + (t + i) * sm_pitch + c * 4);
+            store_half8(to + (col0 + c) * pitch + row0 + t, rows - t, x);
+        }
+    }
+};
+
+struct ApplyOut {
+    const MuonProductArgs& a;
+    const Found& f;
+
+    template <int WIDE>
+    __device__ __forceinline__ void strip(const char* sm, int sm_pitch, int lane, int64_t row0, int64_t col0,
+                                          int64_t rows, int64_t cols) const {
+        const int64_t pitch = f.m.pitch();
+        float* xs = reinterpret_cast<float*>(a.ws + f.m.x_at());
+        u16* h = reinterpret_cast<u16*>(a.ws + f.m.operand_at(a.turn ^ 1));
+        each8<WIDE>(sm, sm_pitch, lane, rows, cols, [&](int t, int c, float* x) {
+            const int64_t row = row0 + t, at = row * pitch + col0 + c, left = cols - c;
+            float y[8];
+            load8(xs + at, 8, y);  // (zero past the row's end)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = fmaf(a.a, y[i], x[i] * (1.0f / (kScaleB * kScaleX)));
+            if (a.result == kMuonMiddle) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) y[i] = i < left ? x[i] : 0.0f;
+                store8(xs + at, 8, y);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) y[i] *= kScaleX;
+                store_half8(h + at, 8, y);
+            } else if (a.result == kMuonWeights) {
+                float* w = a.w + f.m.offset + row * f.m.cols + col0 + c;
+                const float rate = -a.rates->lr * f.m.scale, decay = a.rates->decay;
+                load8(w, left, y);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) y[i] = fmaf(rate, x[i], y[i] * decay);
+                store8(w, left, y);
+            } else {
+                const int64_t o = f.index * a.out_batch_stride + row * a.out_stride + col0 + c;
+                if (a.out_bf16) store8(static_cast<u16*>(a.out) + o, left, x);
+                else store8(static_cast<float*>(a.out) + o, left, x);
+            }
+        });
+    }
+};
+
+template <int T, int NB>
+__global__ __launch_bounds__(256, 1) void muon_gram_kernel(MuonProductArgs a) {
+    extern __shared__ __attribute__((aligned(16))) char sm[];
+    const Found f = find<true>(a.work);
+    const int64_t s = f.m.side(), pitch = f.m.pitch();
+    const SymmetricOut out{reinterpret_cast<u16*>(a.ws + f.m.a_at()), nullptr, s, f.m.a_pitch(), 0.0f,
+                           kScaleA / (kScaleX * kScaleX), f.i != f.j};
+    const Side x{a.ws + f.m.operand_at(a.turn), pitch * 2, f.m.rows, pitch};
+    const int64_t i0 = (int64_t)f.i * 64 * T, j0 = (int64_t)f.j * 64 * T;
+    if (f.m.tall())
+        gemm::product_tile<gemm::Fp16, T, T, NB, true, true>(x, x, 0, (f.m.rows + 63) / 64, i0, j0, s, s, sm, out);
+    else
+        gemm::product_tile<gemm::Fp16, T, T, NB, false, false>(x, x, 0, (int)(pitch / 64), i0, j0, s, s, sm, out);
+}
+
+template <int T, int NB>
+__global__ __launch_bounds__(256, 1) void muon_square_kernel(MuonProductArgs a) {
+    extern __shared__ __attribute__((aligned(16))) char sm[];
+    const Found f = find<true>(a.work);
+    const int64_t s = f.m.side(), pitch = f.m.a_pitch();
+    const u16* gram = reinterpret_cast<const u16*>(a.ws + f.m.a_at());
+    const SymmetricOut out{reinterpret_cast<u16*>(a.ws + f.m.b_at()), gram, s, pitch, a.b * (kScaleB / kScaleA),
+                           a.c * (kScaleB / (kScaleA * kScaleA)), f.i != f.j};
+    const Side x{gram, pitch * 2, s, 0};
+    gemm::product_tile<gemm::Fp16, T, T, NB, false, false>(x, x, 0, (int)(pitch / 64), (int64_t)f.i * 64 * T,
+                                                           (int64_t)f.j * 64 * T, s, s, sm, out);
+}
+
+template <int T, int NB>
+__global__ __launch_bounds__(256, 1) void muon_apply_kernel(MuonProductArgs a) {
+    extern __shared__ __attribute__((aligned(16))) char sm[];
+    const Found f = find<true>(a.work);
+    const int64_t s = f.m.side(), pitch = f.m.pitch(), ap = f.m.a_pitch();
+    const Side x{a.ws + f.m.operand_at(a.turn), pitch * 2, f.m.rows, pitch}, b{a.ws + f.m.b_at(), ap * 2, s, 0};
+    const int64_t i0 = (int64_t)f.i * 64 * T, j0 = (int64_t)f.j * 64 * T;
+    const ApplyOut out{a, f};
+    if (f.m.tall())
+        gemm::product_tile<gemm::Fp16, T, T, NB, false, false>(x, b, 0, (int)(ap / 64), i0, j0, f.m.rows, f.m.cols, sm,
+                                                               out);
+    else
+        gemm::product_tile<gemm::Fp16, T, T, NB, false, true>(b, x, 0, (int)(ap / 64), i0, j0, f.m.rows, f.m.cols, sm,
+                                                              out);
+}
+
+// The learning rate in force, written by one lane, as that of the AGS step.
+__global__ __launch_bounds__(64) void muon_rates_kernel(MuonRates* p, MuonRates r) {
+    if (threadIdx.x == 0) *p = r;
+}
+
+// ------------------------------------------------------------- launches --
+
+template <typename Kernel>
+hipError_t launch_tiles(Kernel kernel, int t, int nb, const MuonProductArgs& a, hipStream_t s) {
+    const int lds = gemm::lds_bytes(t, t, nb);
+    if (lds > 65536) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                                                 hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(kernel, dim3((unsigned)a.work.blocks), dim3(256), lds, s, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+#define MUON_LAUNCH(KERNEL)                                                                                        \
+    (a.work.t == 4 ? launch_tiles(KERNEL<4, 2>, 4, 2, a, s)                                                        \
+                   : a.work.t == 2 ? (a.work.blocks <= 256 ? launch_tiles(KERNEL<2, 4>, 2, 4, a, s)                \
+                                                           : launch_tiles(KERNEL<2, 2>, 2, 2, a, s))               \
+                                   : launch_tiles(KERNEL<1, 4>, 1, 4, a, s))
+
+hipError_t launch_muon_start(const MuonStepArgs& a, hipStream_t s) {
+    hipLaunchKernelGGL(muon_sum_kernel, dim3((unsigned)a.work.blocks), dim3(kThreads), 0, s, a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(muon_start_kernel, dim3((unsigned)a.work.blocks), dim3(kThreads), 0, s, a);
+    return hipGetLastError();
+}
+hipError_t launch_muon_gram(const MuonProductArgs& a, hipStream_t s) { return MUON_LAUNCH(muon_gram_kernel); }
+hipError_t launch_muon_square(const MuonProductArgs& a, hipStream_t s) { return MUON_LAUNCH(muon_square_kernel); }
+hipError_t launch_muon_apply(const MuonProductArgs& a, hipStream_t s) { return MUON_LAUNCH(muon_apply_kernel); }
+hipError_t launch_muon_rates(MuonRates* p, MuonRates r, hipStream_t s) {
+    hipLaunchKernelGGL(muon_rates_kernel, dim3(1), dim3(64), 0, s, p, r);
+    return hipGetLastError();
+}
+
+}  // namespace ags

@@ -1,0 +1,140 @@
+// Internal declarations of the orthogonalised updates (include/ags_muon.h),
+// shared by their host code and their kernels.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <vector>
+
+#include "ags_gemm_internal.h"
+#include "ags_muon.h"
+
+namespace ags {
+
+// What stands in a matrix's part of the workspace: X in fp32 (before the first
+// step: what is to be orthogonalised), X as operands (two, read and written in
+// turn), A and b A + c A A as operands, partial sums of squares.  Operands' rows
+// are padded with zeros to whole stages of a product.
+struct MuonMatrix {
+    int64_t offset;         // elements, in w, m and the gradients; or 0
+    int64_t ws;             // bytes, in the workspace
+    int32_t rows, cols;
+    int32_t chunks, chunk;  // for passes over the elements: blocks, and pieces of 8 elements of each
+    float scale;
+    int32_t reserved;
+
+    __host__ __device__ int64_t side() const { return rows < cols ? rows : cols; }
+    __host__ __device__ bool tall() const { return rows > cols; }
+    __host__ __device__ int64_t pitch() const { return (cols + 63) / 64 * 64; }       // of X, elements
+    __host__ __device__ int64_t a_pitch() const { return (side() + 63) / 64 * 64; }   // of A
+    __host__ __device__ int64_t x_at() const { return ws; }
+    __host__ __device__ int64_t operand_at(int i) const { return ws + rows * pitch() * (4 + 2 * i); }
+    __host__ __device__ int64_t a_at() const { return ws + rows * pitch() * 8; }
+    __host__ __device__ int64_t b_at() const { return a_at() + side() * a_pitch() * 2; }
+    __host__ __device__ int64_t sums_at() const { return b_at() + side() * a_pitch() * 2; }
+    __host__ __device__ int64_t bytes() const { return sums_at() - ws + (chunks * 8 + 63) / 64 * 64; }
+};
+
+inline MuonMatrix muon_matrix(int64_t offset, int64_t rows, int64_t cols, double scale, int64_t ws) {
+    MuonMatrix m{};
+    m.offset = offset;
+    m.ws = ws;
+    m.rows = (int32_t)rows;
+    m.cols = (int32_t)cols;
+    m.scale = (float)scale;
+    const int64_t pieces = rows * (m.pitch() / 8);
+    m.chunk = (int32_t)std::max<int64_t>(512, gemm_up((pieces + 1023) / 1024, 256));
+    m.chunks = (int32_t)((pieces + m.chunk - 1) / m.chunk);
+    return m;
+}
+
+struct MuonTile {
+    int32_t matrix, i, j, reserved;
+};
+
+// Which blocks do what: tables on the device (a handle's matrices), or one
+// matrix and `batch` like it, one after the other in the workspace.
+struct MuonWork {
+    const MuonMatrix* matrices;  // NULL: `one`
+    const MuonTile* tiles;       // of the launch: tiles of an output, or (matrix, chunk)
+    MuonMatrix one;
+    int32_t blocks;      // in all
+    int32_t each;        // without a table: of a matrix
+    int32_t tiles_n;     // without a table: tiles to a row; 0: those not above the diagonal
+    int32_t t;           // a tile's side is 64 t
+};
+
+struct MuonRates {
+    float lr, decay;     // decay: 1 - lr weight_decay
+};
+
+struct MuonStepArgs {
+    MuonWork work;
+    char* ws;
+    // Where U comes from: replicas and momentum, or a tensor.
+    const void* grads;
+    int64_t stride, batch_stride, row_stride;
+    int32_t K, bf16, nesterov, from_x;
+    float momentum;
+    float* m;
+    double eps;
+};
+
+enum MuonResult : int32_t { kMuonMiddle = 0, kMuonWeights = 1, kMuonOut = 2 };
+
+struct MuonProductArgs {
+    MuonWork work;
+    char* ws;
+    float a, b, c;
+    int32_t turn;        // which operand form of X is read
+    int32_t result;      // what a step's X becomes
+    float* w;
+    const MuonRates* rates;
+    void* out;
+    int64_t out_batch_stride, out_stride;
+    int32_t out_bf16;
+};
+
+// The tile side for a launch of products: the least estimated time, of all the
+// tiles over all CUs, and of the longest.
+struct MuonProduct {
+    int64_t m, n, k, count;
+    bool symmetric;
+};
+
+inline int64_t muon_tiles(const MuonProduct& p, int t) {
+    const int64_t tm = (p.m + 64 * t - 1) / (64 * t), tn = (p.n + 64 * t - 1) / (64 * t);
+    return p.symmetric ? tm * (tm + 1) / 2 : tm * tn;
+}
+
+inline int muon_tile_side(const std::vector<MuonProduct>& v) {
+    int best = 1;
+    double least = 1e30;
+    for (int t : {1, 2, 4}) {
+        const double stage = t == 1 ? 0.09 : t == 2 ? 0.26 : 1.15;   // us on a CU that is full of such tiles
+        const double alone = t == 1 ? 0.26 : t == 2 ? 0.34 : 1.15, ends = t == 1 ? 1.4 : t == 2 ? 3 : 6;
+        double sum = 0, longest = 0;
+        for (const MuonProduct& p : v) {
+            const double stages = (double)((p.k + 63) / 64);
+            sum += (double)muon_tiles(p, t) * (double)p.count * (stages * stage + ends * stage / alone);
+            longest = std::max(longest, stages * alone + ends);
+        }
+        const double us = std::max(sum / 256, longest);
+        if (us < least) {
+            least = us;
+            best = t;
+        }
+    }
+    return best;
+}
+
+// Weak for the same reason as the clipping launchers.
+__attribute__((weak)) hipError_t launch_muon_start(const MuonStepArgs&, hipStream_t);
+__attribute__((weak)) hipError_t launch_muon_gram(const MuonProductArgs&, hipStream_t);
+__attribute__((weak)) hipError_t launch_muon_square(const MuonProductArgs&, hipStream_t);
+__attribute__((weak)) hipError_t launch_muon_apply(const MuonProductArgs&, hipStream_t);
+__attribute__((weak)) hipError_t launch_muon_rates(MuonRates*, MuonRates, hipStream_t);
+
+}  // namespace ags
