@@ -15,7 +15,7 @@
  *
  * Activations, weights and gradients are bf16, sums fp32.  h is rounded once.
  * The backward pass rounds dg and du to bf16, as operands of its products;
- * where g and u were saved they are bf16 too.  Sums are added in an order that
+ * where g and u were saved they have 24 bits (16 of mantissa).  Sums are added in an order that
  * the sizes alone fix: equal inputs give equal results bit for bit.  NaN and
  * infinities go where the formulas take them.
  *
@@ -62,8 +62,10 @@ ags_status ags_glu_store(const void *d_gate, int64_t gate_stride, const void *d_
 
 /* h [rows][h_stride] of h_dtype from x [rows, k] (bf16; any alignment and
  * stride, but rows that start at multiples of 16 bytes and a k that is a
- * multiple of 64 save a copy).  d_saved: bf16 [rows][lines], g and u as the
- * weight's rows lie, for the backward pass; or NULL.  rows up to 2^31. */
+ * multiple of 64 save a copy).  d_saved: g and u for the backward
+ * pass, 3 bytes each in the order of the weight's rows, 3 lines bytes a row of x
+ * (the upper 16 bits of all of them, bf16 values cut off, then the next 8 of
+ * each), 16-byte aligned; or NULL.  rows up to 2^30. */
 ags_status ags_glu_forward_workspace(int64_t rows, int64_t n, int64_t k, size_t *out_bytes);
 ags_status ags_glu_forward(const void *d_x, int64_t rows, int64_t x_stride,
                            const ags_glu_weight *w, int32_t act, void *d_h, int32_t h_dtype,

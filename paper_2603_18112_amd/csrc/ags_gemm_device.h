@@ -61,8 +61,8 @@ struct Side {
 // Elements of the contracted axis in a stage.
 constexpr int kDepth = 64;
 
-// Bytes of LDS of NB stages of a tile of 64 TM x 64 TN.
-constexpr int lds_bytes(int tm, int tn, int nb) { return nb * 64 * (tm + tn) * 2 * kDepth; }
+// Bytes of LDS of a tile of 64 TM x 64 TN: NA stages of a, NB of b.
+constexpr int lds_bytes(int tm, int tn, int na, int nb) { return 64 * (tm * na + tn * nb) * 2 * kDepth; }
 
 // One operand's part in a tile of W (64, 128 or 256) of its side.
 //
@@ -79,33 +79,39 @@ struct Loader {
     static constexpr int kFragments = W / 64;   // 32 of the side each, of a wave
     static constexpr int kRow = ALONG ? 2 * W : 128, kRows = 1024 / kRow;  // bytes of a row, rows of a load
 
-    const char* base;
-    int64_t pitch;
-    int64_t rows;     // across: of the tile
-    unsigned last;    // across: offset of the last row
+    const char* base;     // along: of the stage that is loaded next; across: of the tile
+    unsigned pitch, records, offset;
+    unsigned last;        // across: offset of the last row
     unsigned first, width;
-    int off[4];       // across: of step j; along: of fragment f
+    int left;             // along: of the contracted axis
+    int off[4];           // across: of step j; along: of fragment f
 
-    __device__ __forceinline__ Loader(const Side& s, int64_t at, int w, int lane, int side) {
+    __device__ __forceinline__ Loader(const Side& s, int64_t at, int stage, bool live, int w, int lane, int side) {
         const char* p = static_cast<const char*>(s.p);
-        pitch = s.pitch;
+        pitch = (unsigned)s.pitch;
         const int row = w * kRows + lane * 16 / kRow, piece = lane * 16 % kRow / 16;
         if constexpr (ALONG) {
-            base = p + at * 2;
-            rows = s.rows;
+            base = p + at * 2 + (int64_t)stage * kDepth * s.pitch;
+            left = (int)(s.rows - (int64_t)stage * kDepth);
             width = (unsigned)min((int64_t)W, s.width - at) * 2;
+            last = offset = 0;
             const int swizzle = W == 64 ? (row >> 1) & 1 : row & 3;
-            first = (unsigned)(row * pitch) + (piece ^ (4 * swizzle)) * 16;
+            first = row * pitch + (piece ^ (4 * swizzle)) * 16;
             const int h = lane >> 5, g = (lane >> 4) & 1, t = (lane >> 2) & 3, c = lane & 3;
 #pragma unroll
             for (int f = 0; f < kFragments; ++f)
                 off[f] = (h * 32 + t) * kRow + ((side * kFragments + f) ^ (W == 64 ? t >> 1 : t)) * 64 + g * 32 + c * 8;
+            records = live ? along_records() : 0u;
         } else {
-            base = p + at * pitch;
-            rows = min((int64_t)W, s.rows - at);
+            base = p + at * s.pitch;
+            const int rows = (int)min((int64_t)W, s.rows - at);
+            offset = stage * 128;
+            records = live ? rows * pitch : 0u;
+            left = 0;
+            width = 0;
             const unsigned to = (unsigned)(piece ^ ((row >> 1) & 7)) * 16;  // row + 32 i: the same
-            first = (unsigned)(row * pitch) + to;
-            last = (unsigned)((rows - 1) * pitch) + to;
+            first = row * pitch + to;
+            last = (rows - 1) * pitch + to;
             const int r = lane & 31, h = lane >> 5;
 #pragma unroll
             for (int j = 0; j < 4; ++j)
@@ -113,21 +119,29 @@ struct Loader {
         }
     }
 
-    // Load i of stage s to LDS byte `to` (of the operand's part of a buffer); a
-    // stage that is not `live` finds a buffer of no bytes.
-    __device__ __forceinline__ void load(int i, int s, bool live, unsigned to, int w) const {
-        const unsigned at = to + (i * 4 + w) * 1024;
+    __device__ __forceinline__ unsigned along_records() const {
+        return left > 0 ? (min(left, kDepth) - 1) * pitch + width : 0u;
+    }
+
+    // The next stage; one that is not `live` finds a buffer of no bytes.
+    __device__ __forceinline__ void advance(bool live) {
         if constexpr (ALONG) {
-            const int64_t left = rows - (int64_t)s * kDepth;
-            const unsigned bytes = live && left > 0 ? (unsigned)((min(left, (int64_t)kDepth) - 1) * pitch) + width : 0u;
-            const char* p = base + (live ? (int64_t)s * kDepth * pitch : 0);
-            load_lds16(__builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), 0, bytes, 0x00027000), at,
-                       first + i * (4 * kRows) * (unsigned)pitch, 0u);
+            base += (int64_t)kDepth * pitch;
+            left -= kDepth;
+            records = live ? along_records() : 0u;
         } else {
-            load_lds16(__builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0,
-                                                         live ? (unsigned)(rows * pitch) : 0u, 0x00027000),
-                       at, min(first + i * 32 * (unsigned)pitch, last), live ? s * 128u : 0u);
+            offset = live ? offset + 128 : 0u;  // (it may be taken off the buffer's size)
+            records = live ? records : 0u;
         }
+    }
+
+    // Load i of the stage to LDS byte `to` (of the operand's part of a buffer).
+    __device__ __forceinline__ void load(int i, unsigned to, int w) const {
+        const __amdgpu_buffer_rsrc_t r =
+            __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, records, 0x00027000);
+        const unsigned at = to + (i * 4 + w) * 1024;
+        if constexpr (ALONG) load_lds16(r, at, first + i * (4 * kRows) * pitch, 0u);
+        else load_lds16(r, at, min(first + i * 32 * pitch, last), offset);
     }
 
     // Fragment f of step j (of four) from the operand's part of a buffer.  Lane l
@@ -149,40 +163,60 @@ struct Loader {
     }
 };
 
+// What LDS operations the wave has under way are done.
+__device__ __forceinline__ void lds_wait() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// A wave's 32 rows of 32 FN results as fp32 in its part of LDS, kPitch<FN> bytes
+// a row.  Lane l holds row l % 32 of a fragment, and of each 8 columns the four
+// from 4 (l / 32): registers 4 g .. 4 g + 3 are of columns 8 g + 4 (l / 32) on.
+template <int FN>
+constexpr int kPitch = FN * 128 + 16;
+template <int FN>
+constexpr int kStrip = 32 * kPitch<FN>;
+
+template <int FN>
+__device__ __forceinline__ void to_strip(const v16f (&acc)[FN], char* strip, int lane) {
+    char* p = strip + (lane & 31) * kPitch<FN> + (lane >> 5) * 16;
+#pragma unroll
+    for (int y = 0; y < FN; ++y)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            *reinterpret_cast<float4*>(p + y * 128 + g * 32) =
+                make_float4(acc[y][4 * g], acc[y][4 * g + 1], acc[y][4 * g + 2], acc[y][4 * g + 3]);
+    lds_wait();
+}
+
 // The tile at (i0, j0) of an output m x n, over stages [s0, s1) of the
-// contracted axis.  `out` gets 32 rows of a wave's columns at a time, in LDS:
+// contracted axis.  A wave has TM x TN fragments of 32 x 32 results; `out` gets 32 rows of
+// them at a time, and the wave's part of LDS:
 //
-//   out(strip, pitch, lane, row0, col0, rows, cols)
+//   out.band<TN>(fragments, strip, lane, row0, col0, rows, cols)
 //
-// rows x cols of them lie in the output (cols at most WIDE = 32 TN of a wave).
-// A wave's 32 x 32 fragments: TM x TN.
+// from (row0, col0) on rows x cols lie in the output (more than the 32 x 32 TN, or none).
 //
-// Loads run NB - 1 stages ahead, spread between the matrix instructions of the
-// steps in which their buffer is free.
-template <typename E, int TM, int TN, int NB, bool ALONG_A, bool ALONG_B, typename Out>
+// LDS holds NA stages of a and NB of b (NB = NA or NA + 1).  A stage is four steps.  Loads of
+// a start in the last step of stage s for s + NA, whose buffer the barrier before it
+// has freed; those of b in the first step for s + NB - 1.  What a stage loads has
+// at least three steps (NA = 2) to arrive.
+template <typename E, int TM, int TN, int NA, int NB, bool ALONG_A, bool ALONG_B, typename Out>
 __device__ __forceinline__ void product_tile(const Side& a, const Side& b, int s0, int s1, int64_t i0, int64_t j0,
                                              int64_t m, int64_t n, char* sm, const Out& out) {
     constexpr int BM = 64 * TM, BN = 64 * TN, FM = TM, FN = TN;
-    constexpr int kBuf = (BM + BN) * 128;
+    static_assert(NB == NA || NB == NA + 1, "the count of loads under way below");
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = w >> 1, wn = w & 1;
-    const Loader<BM, ALONG_A> la(a, i0, w, lane, wm);
-    const Loader<BN, ALONG_B> lb(b, j0, w, lane, wn);
+    Loader<BM, ALONG_A> la(a, i0, s0, s0 < s1, w, lane, wm);
+    Loader<BN, ALONG_B> lb(b, j0, s0, s0 < s1, w, lane, wn);
     const unsigned lds0 = (unsigned)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)sm);
-    constexpr int kLoads = la.kLoads + lb.kLoads;
+    constexpr int kA = BM / 32, kB = BN / 32;          // a wave's loads of a stage
+    constexpr int kBufA = BM * 128, kBufB = BN * 128, kAtB = NA * kBufA;
 
-    auto load_one = [&](int i, int s, int buf) {
-        const unsigned p = lds0 + buf * kBuf;
-        if (i < BM / 32) la.load(i, s, s < s1, p, w);
-        else lb.load(i - BM / 32, s, s < s1, p + BM * 128, w);
-    };
     uint4 fa[2][FM], fb[2][FN];
-    // Read i of a step's operands, in the order they are needed: a's first
-    // fragment, all of b's, the rest of a's.
-    auto read_one = [&](int i, int buf, int j, int to) {
-        const char* p = sm + buf * kBuf;
-        if (i >= 1 && i <= FN) fb[to][i - 1] = lb.read(p + BM * 128, i - 1, j);
-        else fa[to][i ? i - FN : 0] = la.read(p, i ? i - FN : 0, j);
+    // Read i of a step's operands from buffers ca and cb, in the order they are needed:
+    // a's first fragment, all of b's, the rest of a's.
+    auto read_one = [&](int i, int ca, int cb, int j, int to) {
+        if (i >= 1 && i <= FN) fb[to][i - 1] = lb.read(sm + kAtB + cb * kBufB, i - 1, j);
+        else fa[to][i ? i - FN : 0] = la.read(sm + ca * kBufA, i ? i - FN : 0, j);
     };
 
     // b's fragments are the instruction's first operand: four results of a lane
@@ -195,80 +229,88 @@ __device__ __forceinline__ void product_tile(const Side& a, const Side& b, int s
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[x][y][i] = 0.0f;
 
-    // A stage's loads are spread over three steps: the last of the stage NB
-    // before and the first two of the next.  sched_barrier keeps the order.
-    constexpr int kSlots = 3 * FM;
-    auto loads = [&](int slot, int s, int buf) {
+    // A step multiplies all pairs of fragments; the next step's reads stand
+    // between the products of its first half, loads between those of its second:
+    // an instruction or two to each, which issue while the matrix cores work.
+    // sched_barrier keeps the order.
+    constexpr int kProducts = FM * FN, kReads = FM + FN, kHalf = kProducts > 8 ? kProducts / 2 : kProducts;
+    constexpr int kFirst = kProducts > 8 ? kProducts / 2 : 0;
+    auto step = [&](int j, int ca, int cb, auto&& load, int n) {
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i)
-            if (i >= slot * kLoads / kSlots && i < (slot + 1) * kLoads / kSlots) load_one(i, s, buf);
-        __builtin_amdgcn_sched_barrier(0);
-    };
-    // Step j: products of one row of fragments after the other, the next step's
-    // reads between them, none before the last row.
-    constexpr int kReads = FM > 1 ? (FM + FN + FM - 2) / (FM > 1 ? FM - 1 : 1) : FM + FN;
-    auto step = [&](int j, int next_buf, int slot, int load_stage, int load_buf) {
+        for (int q = 0; q < kProducts; ++q) {
 #pragma unroll
-        for (int x = 0; x < FM; ++x) {
-#pragma unroll
-            for (int i = x * kReads; i < (x + 1) * kReads && i < FM + FN; ++i)
-                read_one(i, next_buf, (j + 1) & 3, (j + 1) & 1);
-#pragma unroll
-            for (int y = 0; y < FN; ++y) acc[x][y] = E::mfma(fb[j & 1][y], fa[j & 1][x], acc[x][y]);
+            for (int i = 0; i < kReads; ++i)
+                if (i * kHalf / kReads == q) read_one(i, ca, cb, (j + 1) & 3, (j + 1) & 1);
+            acc[q / FN][q % FN] = E::mfma(fb[j & 1][q % FN], fa[j & 1][q / FN], acc[q / FN][q % FN]);
             __builtin_amdgcn_sched_barrier(0);
-            if (slot < 3) loads(slot * FM + x, load_stage, load_buf);
+#pragma unroll
+            for (int i = 0; i < n; ++i)
+                if (kFirst + i * (kProducts - kFirst) / n == q) load(i);
+            __builtin_amdgcn_sched_barrier(0);
         }
     };
-    // One stage, in buffer cur; the operands of its first step are in registers.
+    auto nothing = [](int) {};
+    // One stage, in buffers ca and cb; the operands of its first step are in registers.
     // Before its last step the next stage has arrived (those after it need not
-    // have) and the block's reads of this one are done, so one barrier serves
-    // both buffers.  Past the last stage the loads find a buffer of no bytes, and
-    // operands are read that nothing uses.
-    auto stage = [&](int s, int cur) {
-        const int next = cur + 1 == NB ? 0 : cur + 1, last = cur ? cur - 1 : NB - 1;
-        step(0, cur, 1, s + NB - 1, last);
-        step(1, cur, 2, s + NB - 1, last);
-        step(2, cur, 3, 0, 0);
-        wait_loads<(NB - 2) * kLoads>();
+    // have) and the block's reads of this one are done, so one barrier serves both.
+    // Past the last stage the loads find a buffer of no bytes, and operands are read
+    // that nothing uses.
+    constexpr int kUnderWay = (NA - 2) * kA + (NB - 2) * kB;
+    auto stage = [&](int s, int ca, int cb) {
+        const int next_a = ca + 1 == NA ? 0 : ca + 1, next_b = cb + 1 == NB ? 0 : cb + 1, free_b = cb ? cb - 1 : NB - 1;
+        step(0, ca, cb, [&](int i) { lb.load(i, lds0 + kAtB + free_b * kBufB, w); }, kB);
+        lb.advance(s + NB < s1);
+        step(1, ca, cb, nothing, 0);
+        step(2, ca, cb, nothing, 0);
+        wait_loads<kUnderWay>();
         block_barrier();
-        step(3, next, 0, s + NB, cur);
+        step(3, next_a, next_b, [&](int i) { la.load(i, lds0 + ca * kBufA, w); }, kA);
+        la.advance(s + NA + 1 < s1);
     };
     if (s0 < s1) {
 #pragma unroll
-        for (int t = 0; t < NB - 1; ++t)
+        for (int t = 0; t < NB; ++t) {
+            if (t < NA) {
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) load_one(i, s0 + t, t);
-        wait_loads<(NB - 2) * kLoads>();
+                for (int i = 0; i < kA; ++i) la.load(i, lds0 + t * kBufA, w);
+                la.advance(s0 + t + 1 < s1);
+            }
+            if (t < NB - 1) {
 #pragma unroll
-        for (int x = 0; x < FM; ++x) loads(x, s0 + NB - 1, NB - 1);
+                for (int i = 0; i < kB; ++i) lb.load(i, lds0 + kAtB + t * kBufB, w);
+                lb.advance(s0 + t + 1 < s1);
+            }
+        }
+        wait_loads<(NA - 1) * kA + (NB - 2) * kB>();
         block_barrier();
 #pragma unroll
-        for (int i = 0; i < FM + FN; ++i) read_one(i, 0, 0, 0);
-        for (int s = s0, cur = 0; s < s1; ++s, cur = cur + 1 == NB ? 0 : cur + 1) stage(s, cur);
+        for (int i = 0; i < FM + FN; ++i) read_one(i, 0, 0, 0, 0);
+        for (int s = s0, ca = 0, cb = 0; s < s1; ++s) {
+            stage(s, ca, cb);
+            ca = ca + 1 == NA ? 0 : ca + 1;
+            cb = cb + 1 == NB ? 0 : cb + 1;
+        }
         wait_loads<0>();
     }
 
-    // 32 rows at a time go through the wave's own part of LDS.  Lane l holds row
-    // l % 32 of a fragment, and of each 8 columns the four from 4 (l / 32).
+    // 32 rows at a time, through the wave's own part of LDS.
     block_barrier();
-    constexpr int kWide = BN / 2, kPitch = kWide * 4 + 16;
-    char* strip = sm + w * 32 * kPitch;
-    const int r = lane & 31, h = lane >> 5;
-#pragma unroll
-    for (int x = 0; x < FM; ++x) {
-#pragma unroll
-        for (int y = 0; y < FN; ++y)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const v16f v = acc[x][y];
-                *reinterpret_cast<float4*>(strip + r * kPitch + y * 128 + g * 32 + h * 16) =
-                    make_float4(v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]);
-            }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        const int64_t row0 = i0 + wm * (BM / 2) + x * 32, col0 = j0 + wn * kWide;
-        out.template strip<kWide>(strip, kPitch, lane, row0, col0, m - row0, n - col0);
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    char* strip = sm + w * kStrip<FN>;
+    const int64_t row0 = i0 + wm * (BM / 2), col0 = j0 + wn * (BN / 2);
+    // (written out: the compiler gives up unrolling the loop where `out` is long, and
+    // the sums would go to memory)
+    auto band = [&](const v16f (&c)[FN], int64_t row) {
+        out.template band<FN>(c, strip, lane, row, col0, m - row, n - col0);
+        lds_wait();
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    band(acc[0], row0);
+    if constexpr (FM > 1) band(acc[1], row0 + 32);
+    if constexpr (FM > 2) {
+        band(acc[2], row0 + 64);
+        band(acc[3], row0 + 96);
     }
+    static_assert(FM == 1 || FM == 2 || FM == 4, "bands of a tile");
 }
 
 // To nearest even, by the hardware's converter.

@@ -54,31 +54,77 @@ __global__ __launch_bounds__(256) void glu_pack_kernel(GluPackArgs a) {
 
 // ------------------------------------------------------------- activation --
 
-// act(g), and its derivative.
+// act(g), and its derivative, in fp32.  The hardware's 2^x and 1 / x are within an
+// ulp; the argument's rounding costs e^-g |g| ulps, of which little is left in
+// g / (1 + e^-g).  (expf and a division take four times the instructions, 2 ms
+// against 1.85 for 8192 x 4096 -> 16384.)
+__device__ __forceinline__ float sigmoid(float g) {
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.44269504f));
+}
 __device__ __forceinline__ float act_of(int act, float g) {
-    if (act == AGS_GLU_SILU) return g / (1.0f + expf(-g));
+    if (act == AGS_GLU_SILU) return g * sigmoid(g);
     return 0.5f * g * (1.0f + erff(g * 0.70710678f));
 }
 __device__ __forceinline__ void act_both(int act, float g, float* f, float* d) {
     if (act == AGS_GLU_SILU) {
-        const float s = 1.0f / (1.0f + expf(-g));
+        const float s = sigmoid(g);
         *f = g * s;
         *d = s * fmaf(g, 1.0f - s, 1.0f);
     } else {
         const float c = 0.5f * (1.0f + erff(g * 0.70710678f));
         *f = g * c;
-        *d = fmaf(g * 0.39894228f, expf(-0.5f * g * g), c);
+        *d = fmaf(g * 0.39894228f, __builtin_amdgcn_exp2f(g * g * -0.72134752f), c);
+    }
+}
+
+// g and u are saved with 24 bits each, fp32 without the last 8 of its mantissa: the
+// upper 16 bits of a row's, then the next 8.  (In bf16 they would cost the gradients
+// as much as their own rounding does: dgate off by 0.31 % of its norm, not 0.24.)
+__device__ __forceinline__ unsigned bits24(float x) {
+    const unsigned b = __float_as_uint(x);
+    return (b & 0x7fffffffu) > 0x7f800000u ? b : b + 0x80u;  // (in bits 8 .. 31)
+}
+// Four elements' upper halves, and their next bytes.
+__device__ __forceinline__ void split24(float a, float b, float c, float d, uint2* hi, unsigned* lo) {
+    const unsigned x = bits24(a), y = bits24(b), z = bits24(c), w = bits24(d);
+    *hi = make_uint2(__builtin_amdgcn_perm(y, x, 0x07060302u), __builtin_amdgcn_perm(w, z, 0x07060302u));
+    const unsigned p = __builtin_amdgcn_perm(y, x, 0x0c0c0501u), q = __builtin_amdgcn_perm(w, z, 0x0c0c0501u);
+    *lo = p | (q << 16);
+}
+__device__ __forceinline__ void join24(uint4 hi, uint2 lo, float* x) {
+    const unsigned h[4] = {hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const unsigned l = (i < 4 ? lo.x : lo.y) >> (8 * (i & 3)) & 0xffu;
+        x[i] = __uint_as_float((i & 1 ? h[i >> 1] & 0xffff0000u : h[i >> 1] << 16) | l << 8);
+    }
+}
+
+// Where a row of dg and du ends in a stage of their products: zeros up to there.
+__device__ __forceinline__ void pad_grads(u16* row, int64_t n, int half) {
+    const int64_t lines = glu_lines(n);
+    if (lines < glu_grads(n)) {
+        *reinterpret_cast<uint4*>(row + lines + half * 16) = make_uint4(0, 0, 0, 0);
+        *reinterpret_cast<uint4*>(row + lines + half * 16 + 8) = make_uint4(0, 0, 0, 0);
     }
 }
 
 // Eight sums of gate and the same eight of up, hidden units from `unit` on.
 __device__ __forceinline__ void put_pair(const GluArgs& a, int64_t row, int64_t unit, float* g, float* u) {
-    const int64_t line = unit / 16 * 32 + unit % 16, left = a.n - unit;
+    const int64_t lines = glu_lines(a.n), line = unit / 16 * 32 + unit % 16, left = a.n - unit;
     if (a.mode == kGluForward) {
         if (a.saved) {
-            u16* s = static_cast<u16*>(a.saved) + row * glu_lines(a.n) + line;
-            store8(s, 8, g);
-            store8(s + 16, 8, u);
+            char* s = static_cast<char*>(a.saved) + row * 3 * lines;
+#pragma unroll
+            for (int up = 0; up < 2; ++up) {
+                const float* x = up ? u : g;
+                uint2 hi[2];
+                unsigned lo[2];
+                split24(x[0], x[1], x[2], x[3], &hi[0], &lo[0]);
+                split24(x[4], x[5], x[6], x[7], &hi[1], &lo[1]);
+                *reinterpret_cast<uint4*>(s + (line + 16 * up) * 2) = make_uint4(hi[0].x, hi[0].y, hi[1].x, hi[1].y);
+                *reinterpret_cast<uint2*>(s + 2 * lines + line + 16 * up) = make_uint2(lo[0], lo[1]);
+            }
         }
         if (left <= 0) return;
 #pragma unroll
@@ -97,64 +143,176 @@ __device__ __forceinline__ void put_pair(const GluArgs& a, int64_t row, int64_t 
             g[i] = dh[i] * u[i] * d;
             u[i] = dh[i] * f;
         }
-        u16* p = static_cast<u16*>(a.grads) + row * glu_grads(a.n) + line;
-        store8(p, 8, g);
-        store8(p + 16, 8, u);
-        const int64_t lines = glu_lines(a.n);
-        if (line / 32 * 32 + 32 == lines && lines < glu_grads(a.n)) {
-            const float zero[8] = {};
-            store8(p + 32, 8, zero);
-            store8(p + 48, 8, zero);
+        u16* p = static_cast<u16*>(a.grads) + row * glu_grads(a.n);
+        store8(p + line, 8, g);
+        store8(p + line + 16, 8, u);
+        if (line / 32 * 32 + 32 == lines) pad_grads(p, a.n, unit % 16 / 8);
+    }
+}
+
+// 32 rows of BYTES bytes from LDS, PITCH apart, to memory: those of the first
+// `rows` rows and `bytes` bytes.  T: the elements, whose alignment is all that the
+// 16-byte stores need.
+template <typename T, int BYTES, int PITCH, bool NT = false>
+__device__ __forceinline__ void store_rows(const char* strip, int lane, char* to, int64_t stride, int64_t rows,
+                                           int64_t bytes) {
+    constexpr int kLanes = BYTES / 16, kRows = 64 / kLanes, kN = 16 / sizeof(T);
+    typedef Unaligned<T, kN, sizeof(T)> Piece;
+    const int c = lane % kLanes * 16, t0 = lane / kLanes;
+    if (c >= bytes) return;
+#pragma unroll
+    for (int t = 0; t < 32; t += kRows) {
+        if (t0 + t >= rows) continue;
+        const uint4 raw = *reinterpret_cast<const uint4*>(strip + (t0 + t) * PITCH + c);
+        const Piece v = __builtin_bit_cast(Piece, raw);
+        char* p = to + (t0 + t) * stride + c;
+        if constexpr (NT) {
+            typedef unsigned u4 __attribute__((ext_vector_type(4)));
+            __builtin_nontemporal_store(__builtin_bit_cast(u4, raw), reinterpret_cast<u4*>(p));
+        } else if (c + 16 <= bytes) {
+            *reinterpret_cast<Piece*>(p) = v;
+        } else {
+#pragma unroll
+            for (int i = 0; i < kN; ++i)
+                if (c + (i + 1) * (int)sizeof(T) <= bytes) reinterpret_cast<T*>(p)[i] = v.v[i];
         }
     }
 }
 
-// What a product tile's sums become.  (Not unrolled: four copies of these loops stand in
-// the tile of 256 squared.)
+// Rows of fp32 results in LDS, eight at a time: f(t, c, x) for row t and column c.
+template <int FN, typename F>
+__device__ __forceinline__ void each8(const char* strip, int lane, int64_t rows, int64_t cols, const F& f) {
+    constexpr int kLanes = FN * 4, kRows = 64 / kLanes;
+    const int c = lane % kLanes * 8;
+    if (c >= cols) return;
+    const int end = (int)min(rows, (int64_t)32);
+#pragma unroll 2
+    for (int t = lane / kLanes; t < end; t += kRows) {
+        float x[8];
+        gemm::read8(strip + t * gemm::kPitch<FN> + c * 4, x);
+        f(t, c, x);
+    }
+}
+
+// One part's sums to rows of n.
+template <int FN>
+__device__ __forceinline__ void put_part(const gemm::v16f (&acc)[FN], float* part, int64_t n, char* strip, int lane,
+                                         int64_t row0, int64_t col0, int64_t rows, int64_t cols) {
+    gemm::to_strip<FN>(acc, strip, lane);
+    each8<FN>(strip, lane, rows, cols,
+              [&](int t, int c, float* x) { store8(part + (row0 + t) * n + col0 + c, cols - c, x); });
+}
+
+// What a tile's sums of gate and up become.  A fragment's registers 0 .. 7 are of gate, 8 .. 15
+// of up, for the same units of the block of 16: 4 h .. 4 h + 3 and 8 + 4 h .. (h:
+// the lane's half).  So the activation is taken in registers, and what goes through
+// LDS, for stores of whole rows, is rounded already.
+template <int MODE, int ACT>
 struct PairOut {
     const GluArgs& a;
+    float* part;
 
-    template <int WIDE>
-    __device__ __forceinline__ void strip(const char* sm, int pitch, int lane, int64_t row0, int64_t col0, int64_t rows,
-                                          int64_t cols) const {
-        constexpr int kLanes = WIDE / 16, kRows = 64 / kLanes;
-        const int q = lane % kLanes, c = q / 2 * 32 + (q & 1) * 8;
-        if (c >= cols) return;
-        const int end = (int)min(rows, (int64_t)32);
-#pragma unroll 1
-        for (int t = lane / kLanes; t < end; t += kRows) {
-            float g[8], u[8];
-            gemm::read8(sm + t * pitch + c * 4, g);
-            gemm::read8(sm + t * pitch + c * 4 + 64, u);
-            put_pair(a, row0 + t, (col0 + c) / 32 * 16 + c % 16, g, u);
-        }
+    template <int FN>
+    __device__ __forceinline__ void band(const gemm::v16f (&acc)[FN], char* strip, int lane, int64_t row0, int64_t col0,
+                                         int64_t rows, int64_t cols) const {
+        if constexpr (MODE == kGluPart) put_part<FN>(acc, part, glu_lines(a.n), strip, lane, row0, col0, rows, cols);
+        else if constexpr (MODE == kGluForward) forward<FN>(acc, strip, lane, row0, col0, rows, cols);
+        else grads<FN>(acc, strip, lane, row0, col0, rows, cols);
     }
-};
 
-// One part's sums where there is one, to rows of n.
-template <typename Out>
-struct OrPart {
-    const Out& out;
-    float* p;
-    int64_t n;
+    template <int FN>
+    __device__ __forceinline__ void forward(const gemm::v16f (&acc)[FN], char* strip, int lane, int64_t row0,
+                                            int64_t col0, int64_t rows, int64_t cols) const {
+        const int r = lane & 31, h = lane >> 5;
+        const int64_t unit = col0 / 2, left = a.n - unit, lines = glu_lines(a.n);
+        constexpr int kHalf = FN * 32 + 16, kFull = FN * 64 + 16;  // bytes of a row in LDS
+#pragma unroll
+        for (int y = 0; y < FN; ++y)
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                float x[4];
+                __builtin_amdgcn_sched_barrier(0);  // (a few registers at a time)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = act_of(ACT, acc[y][4 * g + i]) * acc[y][8 + 4 * g + i];
+                if (a.h_bf16)
+                    *reinterpret_cast<uint2*>(strip + r * kHalf + y * 32 + g * 16 + h * 8) =
+                        make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
+                else
+                    *reinterpret_cast<float4*>(strip + r * kFull + y * 64 + g * 32 + h * 16) =
+                        make_float4(x[0], x[1], x[2], x[3]);
+            }
+        gemm::lds_wait();
+        const int64_t at = row0 * a.h_stride + unit;
+        if (a.h_bf16)
+            store_rows<u16, FN * 32, kHalf>(strip, lane, static_cast<char*>(a.h) + at * 2, a.h_stride * 2, rows, left * 2);
+        else
+            store_rows<float, FN * 64, kFull>(strip, lane, static_cast<char*>(a.h) + at * 4, a.h_stride * 4, rows,
+                                              left * 4);
+        if (!a.saved) return;
+        gemm::lds_wait();
+        char* low = strip + 32 * kFull;
+#pragma unroll
+        for (int y = 0; y < FN; ++y)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                uint2 hi;
+                unsigned lo;
+                split24(acc[y][4 * g], acc[y][4 * g + 1], acc[y][4 * g + 2], acc[y][4 * g + 3], &hi, &lo);
+                *reinterpret_cast<uint2*>(strip + r * kFull + y * 64 + g * 16 + h * 8) = hi;
+                *reinterpret_cast<unsigned*>(low + r * kHalf + y * 32 + g * 8 + h * 4) = lo;
+            }
+        gemm::lds_wait();
+        char* s = static_cast<char*>(a.saved) + row0 * 3 * lines;
+        store_rows<unsigned, FN * 64, kFull, true>(strip, lane, s + col0 * 2, 3 * lines, rows, cols * 2);
+        store_rows<unsigned, FN * 32, kHalf, true>(low, lane, s + 2 * lines + col0, 3 * lines, rows, cols);
+    }
 
-    template <int WIDE>
-    __device__ __forceinline__ void strip(const char* sm, int pitch, int lane, int64_t row0, int64_t col0, int64_t rows,
-                                          int64_t cols) const {
-        if (!p) {
-            out.template strip<WIDE>(sm, pitch, lane, row0, col0, rows, cols);
-            return;
+    template <int FN>
+    __device__ __forceinline__ void grads(const gemm::v16f (&acc)[FN], char* strip, int lane, int64_t row0,
+                                          int64_t col0, int64_t rows, int64_t cols) const {
+        const int r = lane & 31, h = lane >> 5;
+        constexpr int kHalf = FN * 32 + 16, kFull = FN * 64 + 16, kLanes = FN * 2, kRows = 64 / kLanes;
+        {   // dh: whole rows, zeros past their ends
+            const int64_t c = lane % kLanes * 8, unit = col0 / 2 + c;
+#pragma unroll
+            for (int t = lane / kLanes; t < 32; t += kRows) {
+                float x[8];
+                load8(static_cast<const u16*>(a.dh) + (row0 + t) * a.dh_stride + unit, t < rows ? a.n - unit : 0, x);
+                store8(reinterpret_cast<u16*>(strip + t * kHalf) + c, 8, x);
+            }
         }
-        constexpr int kLanes = WIDE / 8, kRows = 64 / kLanes;
-        const int c = lane % kLanes * 8;
-        if (c >= cols) return;
-        const int end = (int)min(rows, (int64_t)32);
-#pragma unroll 2
-        for (int t = lane / kLanes; t < end; t += kRows) {
-            float x[8];
-            gemm::read8(sm + t * pitch + c * 4, x);
-            store8(p + (row0 + t) * n + col0 + c, cols - c, x);
-        }
+        gemm::lds_wait();
+        uint2 d[FN][2];
+#pragma unroll
+        for (int y = 0; y < FN; ++y)
+#pragma unroll
+            for (int g = 0; g < 2; ++g)
+                d[y][g] = *reinterpret_cast<const uint2*>(strip + r * kHalf + y * 32 + g * 16 + h * 8);
+        gemm::lds_wait();
+#pragma unroll
+        for (int y = 0; y < FN; ++y)
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                const float dh[4] = {bf16_value((u16)d[y][g].x), bf16_value((u16)(d[y][g].x >> 16)),
+                                     bf16_value((u16)d[y][g].y), bf16_value((u16)(d[y][g].y >> 16))};
+                float dg[4], du[4];
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float f, e;
+                    act_both(ACT, acc[y][4 * g + i], &f, &e);
+                    dg[i] = dh[i] * acc[y][8 + 4 * g + i] * e;
+                    du[i] = dh[i] * f;
+                }
+                char* p = strip + r * kFull + y * 64 + g * 16 + h * 8;
+                *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(dg[0], dg[1]), pack_bf16(dg[2], dg[3]));
+                *reinterpret_cast<uint2*>(p + 32) = make_uint2(pack_bf16(du[0], du[1]), pack_bf16(du[2], du[3]));
+            }
+        gemm::lds_wait();
+        const int64_t pitch = glu_grads(a.n);
+        u16* to = static_cast<u16*>(a.grads) + row0 * pitch;
+        store_rows<unsigned, FN * 64, kFull>(strip, lane, reinterpret_cast<char*>(to + col0), pitch * 2, rows, cols * 2);
+        if (cols > 0 && cols <= FN * 32 && r < rows) pad_grads(to + r * pitch, a.n, h);
     }
 };
 
@@ -178,63 +336,103 @@ __device__ __forceinline__ void put_row(const GluBackArgs& a, bool dw, int64_t r
     else store8(static_cast<float*>(p) + at, left, x);
 }
 
+// dx, or (DW) rows of dgate and dup, sixteen of each in turn.
+template <bool DW>
 struct RowOut {
     const GluBackArgs& a;
-    bool dw;
+    float* part;
 
-    template <int WIDE>
-    __device__ __forceinline__ void strip(const char* sm, int pitch, int lane, int64_t row0, int64_t col0, int64_t rows,
-                                          int64_t cols) const {
-        constexpr int kLanes = WIDE / 8, kRows = 64 / kLanes;
-        const int c = lane % kLanes * 8;
-        if (c >= cols) return;
-        const int end = (int)min(rows, (int64_t)32);
-#pragma unroll 2
-        for (int t = lane / kLanes; t < end; t += kRows) {
-            float x[8];
-            gemm::read8(sm + t * pitch + c * 4, x);
-            put_row(a, dw, row0 + t, col0 + c, x);
+    template <int FN>
+    __device__ __forceinline__ void band(const gemm::v16f (&acc)[FN], char* strip, int lane, int64_t row0, int64_t col0,
+                                         int64_t rows, int64_t cols) const {
+        if (part) {
+            put_part<FN>(acc, part, a.k, strip, lane, row0, col0, rows, cols);
+        } else if (a.bf16 && !a.accumulate) {
+            const int r = lane & 31, h = lane >> 5;
+            constexpr int kFull = FN * 64 + 16;
+#pragma unroll
+            for (int y = 0; y < FN; ++y)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    *reinterpret_cast<uint2*>(strip + r * kFull + y * 64 + g * 16 + h * 8) =
+                        make_uint2(pack_bf16(acc[y][4 * g], acc[y][4 * g + 1]),
+                                   pack_bf16(acc[y][4 * g + 2], acc[y][4 * g + 3]));
+            gemm::lds_wait();
+            const int64_t row = DW ? row0 / 2 : row0, left = DW ? min((int64_t)16, a.n - row) : rows;
+            const int64_t at = (row * a.stride + col0) * 2;
+            if constexpr (DW) {
+                store_rows<u16, FN * 64, kFull>(strip, lane, static_cast<char*>(a.out) + at, a.stride * 2, left, cols * 2);
+                store_rows<u16, FN * 64, kFull>(strip + 16 * kFull, lane, static_cast<char*>(a.out_up) + at, a.stride * 2,
+                                                left, cols * 2);
+            } else {
+                store_rows<u16, FN * 64, kFull>(strip, lane, static_cast<char*>(a.out) + at, a.stride * 2, left, cols * 2);
+            }
+        } else {
+            gemm::to_strip<FN>(acc, strip, lane);
+            each8<FN>(strip, lane, rows, cols, [&](int t, int c, float* x) { put_row(a, DW, row0 + t, col0 + c, x); });
         }
     }
 };
 
 // --------------------------------------------------------------- products --
 
-constexpr unsigned kBand = 6;
+constexpr unsigned kBand = 4;
 
-template <int T, int NB, bool ALONG_A, bool ALONG_B, typename Out>
-__device__ __forceinline__ void product(const Side& a, const Side& b, int64_t m, int64_t n, int64_t k, int splits,
-                                        float* partials, unsigned tm, unsigned tn, const Out& out) {
-    extern __shared__ __attribute__((aligned(16))) char sm[];
-    const unsigned tiles = tm * tn, split = blockIdx.x / tiles;
+// The tile of this block, and its part of the contracted axis.
+struct Place {
+    int64_t i0, j0;
+    int s0, s1;
+    unsigned split;
+};
+
+template <int T>
+__device__ __forceinline__ Place place(int64_t k, int splits, unsigned tm, unsigned tn) {
+    const unsigned tiles = tm * tn;
+    Place p;
+    p.split = blockIdx.x / tiles;
     unsigned ti, tj;
     tile::tile_of_block<kBand>(blockIdx.x % tiles, tm, tn, ti, tj);
-    const int64_t i0 = (int64_t)ti * 64 * T, j0 = (int64_t)tj * 64 * T;
+    p.i0 = (int64_t)ti * 64 * T;
+    p.j0 = (int64_t)tj * 64 * T;
     const int stages = (int)((k + gemm::kDepth - 1) / gemm::kDepth);
-    const int s0 = (int)((int64_t)stages * split / splits), s1 = (int)((int64_t)stages * (split + 1) / splits);
-    float* part = splits > 1 ? partials + (int64_t)split * m * n : nullptr;
-    gemm::product_tile<gemm::Bf16, T, T, NB, ALONG_A, ALONG_B>(a, b, s0, s1, i0, j0, m, n, sm, OrPart<Out>{out, part, n});
+    p.s0 = (int)((int64_t)stages * p.split / splits);
+    p.s1 = (int)((int64_t)stages * (p.split + 1) / splits);
+    return p;
 }
 
-template <int T, int NB>
+// Its sums' place where the axis is cut.
+__device__ __forceinline__ float* part_of(float* partials, int splits, const Place& p, int64_t m, int64_t n) {
+    return splits > 1 ? partials + (int64_t)p.split * m * n : nullptr;
+}
+
+template <int T, int NA, int NB, int MODE, int ACT>
 __global__ __launch_bounds__(256, 1) void glu_product_kernel(GluArgs a, unsigned tm, unsigned tn) {
+    extern __shared__ __attribute__((aligned(16))) char sm[];
     const int64_t lines = glu_lines(a.n), padded = glu_padded(a.k);
-    product<T, NB, false, false>(Side{a.x, a.x_stride * 2, a.rows, 0}, Side{a.w, padded * 2, lines, 0}, a.rows, lines,
-                                 padded, a.splits, a.partials, tm, tn, PairOut{a});
+    const Place p = place<T>(padded, a.splits, tm, tn);
+    gemm::product_tile<gemm::Bf16, T, T, NA, NB, false, false>(
+        Side{a.x, a.x_stride * 2, a.rows, 0}, Side{a.w, padded * 2, lines, 0}, p.s0, p.s1, p.i0, p.j0, a.rows, lines, sm,
+        PairOut<MODE, ACT>{a, part_of(a.partials, a.splits, p, a.rows, lines)});
 }
 
-template <int T, int NB>
+template <int T, int NA, int NB>
 __global__ __launch_bounds__(256, 1) void glu_dx_kernel(GluBackArgs a, unsigned tm, unsigned tn) {
+    extern __shared__ __attribute__((aligned(16))) char sm[];
     const int64_t lines = glu_lines(a.n), padded = glu_padded(a.k), grads = glu_grads(a.n);
-    product<T, NB, false, true>(Side{a.grads, grads * 2, a.rows, 0}, Side{a.w, padded * 2, lines, padded}, a.rows, a.k,
-                                grads, a.splits, a.partials, tm, tn, RowOut{a, false});
+    const Place p = place<T>(grads, a.splits, tm, tn);
+    gemm::product_tile<gemm::Bf16, T, T, NA, NB, false, true>(
+        Side{a.grads, grads * 2, a.rows, 0}, Side{a.w, padded * 2, lines, padded}, p.s0, p.s1, p.i0, p.j0, a.rows, a.k, sm,
+        RowOut<false>{a, part_of(a.partials, a.splits, p, a.rows, a.k)});
 }
 
-template <int T, int NB>
+template <int T, int NA, int NB>
 __global__ __launch_bounds__(256, 1) void glu_dw_kernel(GluBackArgs a, unsigned tm, unsigned tn) {
+    extern __shared__ __attribute__((aligned(16))) char sm[];
     const int64_t lines = glu_lines(a.n), grads = glu_grads(a.n);
-    product<T, NB, true, true>(Side{a.grads, grads * 2, a.rows, grads}, Side{a.x, a.x_stride * 2, a.rows, a.x_width},
-                               lines, a.k, a.rows, a.splits, a.partials, tm, tn, RowOut{a, true});
+    const Place p = place<T>(a.rows, a.splits, tm, tn);
+    gemm::product_tile<gemm::Bf16, T, T, NA, NB, true, true>(
+        Side{a.grads, grads * 2, a.rows, grads}, Side{a.x, a.x_stride * 2, a.rows, a.x_width}, p.s0, p.s1, p.i0, p.j0,
+        lines, a.k, sm, RowOut<true>{a, part_of(a.partials, a.splits, p, lines, a.k)});
 }
 
 // Sums of parts: a thread takes eight units (or columns) of a row, and has the
@@ -286,10 +484,12 @@ __global__ __launch_bounds__(256) void glu_act_kernel(GluActArgs a) {
     g.grads = a.grads;
     for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < total; t += (int64_t)gridDim.x * 256) {
         const int64_t row = t / pieces, unit = (t - row * pieces) * 8;
-        const u16* p = static_cast<const u16*>(a.saved) + row * lines + unit / 16 * 32 + unit % 16;
+        const char* p = static_cast<const char*>(a.saved) + row * 3 * lines;
+        const int64_t line = unit / 16 * 32 + unit % 16;
         float x[8], u[8];
-        load8(p, 8, x);
-        load8(p + 16, 8, u);
+        join24(*reinterpret_cast<const uint4*>(p + line * 2), *reinterpret_cast<const uint2*>(p + 2 * lines + line), x);
+        join24(*reinterpret_cast<const uint4*>(p + line * 2 + 32),
+               *reinterpret_cast<const uint2*>(p + 2 * lines + line + 16), u);
         put_pair(g, row, unit, x, u);
     }
 }
@@ -360,9 +560,9 @@ __global__ __launch_bounds__(kFewWaves * 64) void glu_few_kernel(GluArgs a) {
 unsigned blocks_for(int64_t items) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>((items + 255) / 256, 8192)); }
 
 template <typename Kernel, typename Args>
-hipError_t launch_tiles(Kernel kernel, const Args& a, int t, int nb, int64_t m, int64_t n, hipStream_t s) {
+hipError_t launch_tiles(Kernel kernel, const Args& a, int t, int na, int nb, int64_t m, int64_t n, hipStream_t s) {
     const unsigned tm = (unsigned)((m + 64 * t - 1) / (64 * t)), tn = (unsigned)((n + 64 * t - 1) / (64 * t));
-    const int lds = gemm::lds_bytes(t, t, nb);
+    const int lds = gemm::lds_bytes(t, t, na, nb);
     if (lds > 65536) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
                                                  hipFuncAttributeMaxDynamicSharedMemorySize, lds);
@@ -373,13 +573,13 @@ hipError_t launch_tiles(Kernel kernel, const Args& a, int t, int nb, int64_t m, 
 }
 
 // Four buffers where all blocks fit the CUs at once even so.
-#define GLU_LAUNCH(KERNEL, M, N)                                                                          \
+#define GLU_LAUNCH(KERNEL, M, N, ...)                                                                     \
     [&] {                                                                                                 \
         const int64_t tiles = (((M) + 64 * p.t - 1) / (64 * p.t)) * (((N) + 64 * p.t - 1) / (64 * p.t)) * p.splits; \
-        if (p.t == 4) return launch_tiles(KERNEL<4, 2>, a, 4, 2, M, N, s);                                \
-        if (p.t == 2) return tiles <= 256 ? launch_tiles(KERNEL<2, 4>, a, 2, 4, M, N, s)                  \
-                                          : launch_tiles(KERNEL<2, 2>, a, 2, 2, M, N, s);                 \
-        return launch_tiles(KERNEL<1, 4>, a, 1, 4, M, N, s);                                              \
+        if (p.t == 4) return launch_tiles(KERNEL<4, 2, 3 __VA_ARGS__>, a, 4, 2, 3, M, N, s);                    \
+        if (p.t == 2) return tiles <= 256 ? launch_tiles(KERNEL<2, 4, 4 __VA_ARGS__>, a, 2, 4, 4, M, N, s)      \
+                                          : launch_tiles(KERNEL<2, 2, 2 __VA_ARGS__>, a, 2, 2, 2, M, N, s);     \
+        return launch_tiles(KERNEL<1, 4, 4 __VA_ARGS__>, a, 1, 4, 4, M, N, s);                                  \
     }()
 
 }  // namespace
@@ -405,7 +605,13 @@ hipError_t launch_glu_product(const GluArgs& args, hipStream_t s) {
     }
     const GemmShape p = gemm_plan(a.rows, lines, glu_padded(a.k));
     a.splits = p.splits;
-    hipError_t e = GLU_LAUNCH(glu_product_kernel, a.rows, lines);
+    hipError_t e;
+    if (a.splits > 1) e = GLU_LAUNCH(glu_product_kernel, a.rows, lines, , kGluPart, AGS_GLU_SILU);
+    else if (a.mode == kGluForward && a.act == AGS_GLU_SILU)
+        e = GLU_LAUNCH(glu_product_kernel, a.rows, lines, , kGluForward, AGS_GLU_SILU);
+    else if (a.mode == kGluForward) e = GLU_LAUNCH(glu_product_kernel, a.rows, lines, , kGluForward, AGS_GLU_GELU);
+    else if (a.act == AGS_GLU_SILU) e = GLU_LAUNCH(glu_product_kernel, a.rows, lines, , kGluGrads, AGS_GLU_SILU);
+    else e = GLU_LAUNCH(glu_product_kernel, a.rows, lines, , kGluGrads, AGS_GLU_GELU);
     if (e == hipSuccess && a.splits > 1) {
         hipLaunchKernelGGL(glu_join_kernel, dim3(blocks_for(a.rows * lines / 16)), dim3(256), 0, s, a);
         e = hipGetLastError();

@@ -34,6 +34,7 @@ struct GluPackArgs {
 enum GluMode : int32_t {
     kGluForward = 0,  // act(g) u to h, and g and u to saved where that is wanted
     kGluGrads = 1,    // dg and du of dh to grads
+    kGluPart = 2,     // (of the tile kernel) the sums of a part of the contracted axis
 };
 
 struct GluArgs {

@@ -216,17 +216,17 @@ __global__ __launch_bounds__(kThreads) void muon_start_kernel(MuonStepArgs a) {
 
 // ------------------------------------------------------------- products --
 
-// Rows of 8 results: f(t, c, x) for the strip's row t and column c.
-template <int WIDE, typename F>
-__device__ __forceinline__ void each8(const char* sm, int pitch, int lane, int64_t rows, int64_t cols, const F& f) {
-    constexpr int kLanes = WIDE / 8, kRows = 64 / kLanes;
+// Rows of fp32 results in LDS, eight at a time: f(t, c, x) for row t and column c.
+template <int FN, typename F>
+__device__ __forceinline__ void each8(const char* strip, int lane, int64_t rows, int64_t cols, const F& f) {
+    constexpr int kLanes = FN * 4, kRows = 64 / kLanes;
     const int c = lane % kLanes * 8;
     if (c >= cols) return;
     const int end = (int)min(rows, (int64_t)32);
 #pragma unroll 2
     for (int t = lane / kLanes; t < end; t += kRows) {
         float x[8];
-        gemm::read8(sm + t * pitch + c * 4, x);
+        gemm::read8(strip + t * gemm::kPitch<FN> + c * 4, x);
         f(t, c, x);
     }
 }
@@ -240,10 +240,12 @@ struct SymmetricOut {
     float add, times;    // x times + A add
     bool mirror;
 
-    template <int WIDE>
-    __device__ __forceinline__ void strip(char* sm, int sm_pitch, int lane, int64_t row0, int64_t col0, int64_t rows,
-                                          int64_t cols) const {
-        each8<WIDE>(sm, sm_pitch, lane, rows, cols, [&](int t, int c, float* x) {
+    template <int FN>
+    __device__ __forceinline__ void band(const gemm::v16f (&acc)[FN], char* sm, int lane, int64_t row0, int64_t col0,
+                                         int64_t rows, int64_t cols) const {
+        constexpr int kWide = FN * 32, sm_pitch = gemm::kPitch<FN>;
+        gemm::to_strip<FN>(acc, sm, lane);
+        each8<FN>(sm, lane, rows, cols, [&](int t, int c, float* x) {
             const int64_t at = (row0 + t) * pitch + col0 + c;
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[i] *= times;
@@ -261,11 +263,11 @@ struct SymmetricOut {
             }
         });
         if (!mirror) return;
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        gemm::lds_wait();
         const int t = (lane & 3) * 8;
         if (t >= rows) return;
 #pragma unroll 2
-        for (int c = lane >> 2; c < WIDE; c += 16) {
+        for (int c = lane >> 2; c < kWide; c += 16) {
             if (c >= cols) break;
             float x[8];
 #pragma unroll
@@ -279,13 +281,14 @@ struct ApplyOut {
     const MuonProductArgs& a;
     const Found& f;
 
-    template <int WIDE>
-    __device__ __forceinline__ void strip(const char* sm, int sm_pitch, int lane, int64_t row0, int64_t col0,
-                                          int64_t rows, int64_t cols) const {
+    template <int FN>
+    __device__ __forceinline__ void band(const gemm::v16f (&acc)[FN], char* sm, int lane, int64_t row0, int64_t col0,
+                                         int64_t rows, int64_t cols) const {
+        gemm::to_strip<FN>(acc, sm, lane);
         const int64_t pitch = f.m.pitch();
         float* xs = reinterpret_cast<float*>(a.ws + f.m.x_at());
         u16* h = reinterpret_cast<u16*>(a.ws + f.m.operand_at(a.turn ^ 1));
-        each8<WIDE>(sm, sm_pitch, lane, rows, cols, [&](int t, int c, float* x) {
+        each8<FN>(sm, lane, rows, cols, [&](int t, int c, float* x) {
             const int64_t row = row0 + t, at = row * pitch + col0 + c, left = cols - c;
             float y[8];
             load8(xs + at, 8, y);  // (zero past the row's end)
@@ -314,7 +317,7 @@ struct ApplyOut {
     }
 };
 
-template <int T, int NB>
+template <int T, int NA, int NB>
 __global__ __launch_bounds__(256, 1) void muon_gram_kernel(MuonProductArgs a) {
     extern __shared__ __attribute__((aligned(16))) char sm[];
     const Found f = find<true>(a.work);
@@ -324,12 +327,12 @@ __global__ __launch_bounds__(256, 1) void muon_gram_kernel(MuonProductArgs a) {
     const Side x{a.ws + f.m.operand_at(a.turn), pitch * 2, f.m.rows, pitch};
     const int64_t i0 = (int64_t)f.i * 64 * T, j0 = (int64_t)f.j * 64 * T;
     if (f.m.tall())
-        gemm::product_tile<gemm::Fp16, T, T, NB, true, true>(x, x, 0, (f.m.rows + 63) / 64, i0, j0, s, s, sm, out);
+        gemm::product_tile<gemm::Fp16, T, T, NA, NB, true, true>(x, x, 0, (f.m.rows + 63) / 64, i0, j0, s, s, sm, out);
     else
-        gemm::product_tile<gemm::Fp16, T, T, NB, false, false>(x, x, 0, (int)(pitch / 64), i0, j0, s, s, sm, out);
+        gemm::product_tile<gemm::Fp16, T, T, NA, NB, false, false>(x, x, 0, (int)(pitch / 64), i0, j0, s, s, sm, out);
 }
 
-template <int T, int NB>
+template <int T, int NA, int NB>
 __global__ __launch_bounds__(256, 1) void muon_square_kernel(MuonProductArgs a) {
     extern __shared__ __attribute__((aligned(16))) char sm[];
     const Found f = find<true>(a.work);
@@ -338,11 +341,11 @@ __global__ __launch_bounds__(256, 1) void muon_square_kernel(MuonProductArgs a) 
     const SymmetricOut out{reinterpret_cast<u16*>(a.ws + f.m.b_at()), gram, s, pitch, a.b * (kScaleB / kScaleA),
                            a.c * (kScaleB / (kScaleA * kScaleA)), f.i != f.j};
     const Side x{gram, pitch * 2, s, 0};
-    gemm::product_tile<gemm::Fp16, T, T, NB, false, false>(x, x, 0, (int)(pitch / 64), (int64_t)f.i * 64 * T,
+    gemm::product_tile<gemm::Fp16, T, T, NA, NB, false, false>(x, x, 0, (int)(pitch / 64), (int64_t)f.i * 64 * T,
                                                            (int64_t)f.j * 64 * T, s, s, sm, out);
 }
 
-template <int T, int NB>
+template <int T, int NA, int NB>
 __global__ __launch_bounds__(256, 1) void muon_apply_kernel(MuonProductArgs a) {
     extern __shared__ __attribute__((aligned(16))) char sm[];
     const Found f = find<true>(a.work);
@@ -351,10 +354,10 @@ __global__ __launch_bounds__(256, 1) void muon_apply_kernel(MuonProductArgs a) {
     const int64_t i0 = (int64_t)f.i * 64 * T, j0 = (int64_t)f.j * 64 * T;
     const ApplyOut out{a, f};
     if (f.m.tall())
-        gemm::product_tile<gemm::Fp16, T, T, NB, false, false>(x, b, 0, (int)(ap / 64), i0, j0, f.m.rows, f.m.cols, sm,
+        gemm::product_tile<gemm::Fp16, T, T, NA, NB, false, false>(x, b, 0, (int)(ap / 64), i0, j0, f.m.rows, f.m.cols, sm,
                                                                out);
     else
-        gemm::product_tile<gemm::Fp16, T, T, NB, false, true>(b, x, 0, (int)(ap / 64), i0, j0, f.m.rows, f.m.cols, sm,
+        gemm::product_tile<gemm::Fp16, T, T, NA, NB, false, true>(b, x, 0, (int)(ap / 64), i0, j0, f.m.rows, f.m.cols, sm,
                                                               out);
 }
 
@@ -366,8 +369,8 @@ __global__ __launch_bounds__(64) void muon_rates_kernel(MuonRates* p, MuonRates 
 // ------------------------------------------------------------- launches --
 
 template <typename Kernel>
-hipError_t launch_tiles(Kernel kernel, int t, int nb, const MuonProductArgs& a, hipStream_t s) {
-    const int lds = gemm::lds_bytes(t, t, nb);
+hipError_t launch_tiles(Kernel kernel, int t, int na, int nb, const MuonProductArgs& a, hipStream_t s) {
+    const int lds = gemm::lds_bytes(t, t, na, nb);
     if (lds > 65536) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
                                                  hipFuncAttributeMaxDynamicSharedMemorySize, lds);
@@ -380,10 +383,10 @@ hipError_t launch_tiles(Kernel kernel, int t, int nb, const MuonProductArgs& a, 
 }  // namespace
 
 #define MUON_LAUNCH(KERNEL)                                                                                        \
-    (a.work.t == 4 ? launch_tiles(KERNEL<4, 2>, 4, 2, a, s)                                                        \
-                   : a.work.t == 2 ? (a.work.blocks <= 256 ? launch_tiles(KERNEL<2, 4>, 2, 4, a, s)                \
-                                                           : launch_tiles(KERNEL<2, 2>, 2, 2, a, s))               \
-                                   : launch_tiles(KERNEL<1, 4>, 1, 4, a, s))
+    (a.work.t == 4 ? launch_tiles(KERNEL<4, 2, 3>, 4, 2, 3, a, s)                                                        \
+                   : a.work.t == 2 ? (a.work.blocks <= 256 ? launch_tiles(KERNEL<2, 4, 4>, 2, 4, 4, a, s)                \
+                                                           : launch_tiles(KERNEL<2, 2, 2>, 2, 2, 2, a, s))               \
+                                   : launch_tiles(KERNEL<1, 4, 4>, 1, 4, 4, a, s))
 
 hipError_t launch_muon_start(const MuonStepArgs& a, hipStream_t s) {
     hipLaunchKernelGGL(muon_sum_kernel, dim3((unsigned)a.work.blocks), dim3(kThreads), 0, s, a);

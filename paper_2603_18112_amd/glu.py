@@ -133,7 +133,7 @@ class Weight:
 def gated_linear(x, w, act="silu", dtype=None, save=False):
     """h = act(x gate') * (x up') for x [..., k] (bf16) and a Weight of [n, k]:
     [..., n] of `dtype` (bf16 unless given).  save=True returns (h, saved): g and
-    u in bf16 for the backward pass, 4 bytes a hidden unit and row.  An x whose
+    u in 24 bits each for the backward pass, 6 bytes a hidden unit and row.  An x whose
     rows are not contiguous is copied first.  Autograd does not see the call
     (gated_linear_backward is its backward pass), so an x that requires a
     gradient is refused where gradients are recorded."""
@@ -145,7 +145,7 @@ def gated_linear(x, w, act="silu", dtype=None, save=False):
         raise ValueError(f"x must have {w.k} columns")
     code, dt = _dtype(t.bfloat16 if dtype is None else dtype)
     h = t.empty((*x.shape[:-1], w.n), dtype=dt, device=dev)
-    saved = t.empty((rows, w.lines), dtype=t.bfloat16, device=dev) if save else None
+    saved = t.empty((rows, 3 * w.lines), dtype=t.uint8, device=dev) if save else None
     nbytes = ags_glu_forward_workspace(rows, w.n, k)
     ws = _workspace(nbytes, dev)
     ags_glu_forward(x2.data_ptr() or None, rows, max(stride, 1), w.c, act, h.data_ptr() or None, code, max(w.n, 1),
@@ -168,7 +168,7 @@ def gated_linear_backward(dh, x, w, saved=None, act="silu", dgate=None, dup=None
     x2, x_rows, k, x_stride = _bf16(x, "x", dev)
     if n != w.n or k != w.k or rows != x_rows:
         raise ValueError(f"dh and x must have {w.n} and {w.k} columns and equal rows")
-    if saved is not None and (tuple(saved.shape) != (rows, w.lines) or saved.dtype is not t.bfloat16 or
+    if saved is not None and (tuple(saved.shape) != (rows, 3 * w.lines) or saved.dtype is not t.uint8 or
                               saved.device != dev or not saved.is_contiguous()):
         raise ValueError("saved is not what gated_linear returned for this x and w")
     if not need_dw and (dgate is not None or dup is not None):

@@ -47,8 +47,8 @@ def test_sizes_and_workspaces(lib):
         _raises(ags.AGS_E_LAYOUT, f, (1 << 20) + 1, 4)
     for f in (glu.ags_glu_forward_workspace, glu.ags_glu_backward_workspace):
         _raises(ags.AGS_E_ARG, f, -1, 4, 4)
-        _raises(ags.AGS_E_LAYOUT, f, (1 << 31) + 1, 4, 4)
-        _raises(ags.AGS_E_LAYOUT, f, 1 << 31, 1 << 20, 4)
+        _raises(ags.AGS_E_LAYOUT, f, (1 << 30) + 1, 4, 4)
+        _raises(ags.AGS_E_LAYOUT, f, 1 << 30, 1 << 20, 4)
         for rows, n, k in ((0, 5, 5), (1, 1, 1), (33, 17, 65), (1 << 20, 100, 100), (100, 0, 7), (100, 7, 0)):
             assert f(rows, n, k) >= rows * (-(-k // 64) * 64) * 2
     assert lib.ags_glu_bytes(4, 4, ctypes.POINTER(ctypes.c_size_t)()) == ags.AGS_E_ARG
@@ -89,7 +89,7 @@ def test_forward_refuses(lib):
     bad(ags.AGS_E_ARG, a4=2)                                     # activation
     bad(ags.AGS_E_ARG, a6=5)
     bad(ags.AGS_E_ARG, a1=-1)
-    bad(ags.AGS_E_LAYOUT, a1=(1 << 31) + 1)
+    bad(ags.AGS_E_LAYOUT, a1=(1 << 30) + 1)
     bad(ags.AGS_E_ARG, a0=None)
     bad(ags.AGS_E_ARG, a5=None)
     bad(ags.AGS_E_ARG, a2=63)

@@ -76,7 +76,9 @@ def test_whole_numbers_are_exact(rows, n, k, act):
     got, saved = glu.gated_linear(xc, w, act=act, save=True)
     assert torch.equal(got.cpu(), _rounded(h, B))
     assert torch.equal(glu.gated_linear(xc, w, act=act, dtype="f32").cpu(), h.float())
-    z = saved.cpu().view(rows, -1, 2, 16)
+    lines = w.lines
+    assert (saved[:, 2 * lines:] == 0).all()         # whole numbers up to 256 need 16 of the 24 bits
+    z = saved.cpu()[:, :2 * lines].contiguous().view(B).view(rows, -1, 2, 16)
     assert torch.equal(z[:, :, 0].reshape(rows, -1)[:, :n].double(), g)
     assert torch.equal(z[:, :, 1].reshape(rows, -1)[:, :n].double(), u)
     assert (z[:, :, 0].reshape(rows, -1)[:, n:] == 0).all() and (z[:, :, 1].reshape(rows, -1)[:, n:] == 0).all()
@@ -101,7 +103,7 @@ def _random(rows, n, k, seed=0):
 
 def _results(x, gate, up, dh, act, saved):
     """(h, dx, dgate, dup) in 64 bits and how far each may be off; saved: g and u
-    went through bf16 on the way to the gradients."""
+    went through 24 bits, 17 of them significant, on the way to the gradients."""
     x, gate, up, dh = (t.double() for t in (x, gate, up, dh))
     k, n, rows = x.shape[1], gate.shape[0], x.shape[0]
     g, u = x @ gate.t(), x @ up.t()
@@ -112,7 +114,7 @@ def _results(x, gate, up, dh, act, saved):
     h = a * u
     e_h = ea * u.abs() + a.abs() * eu + ea * eu + 2 * U * h.abs()
     if saved:
-        eg, eu = eg + H * g.abs() * 1.01, eu + H * u.abs() * 1.01
+        eg, eu = eg + 2.0 ** -17 * g.abs() * 1.01, eu + 2.0 ** -17 * u.abs() * 1.01
         ea = 1.13 * eg + 8 * U * g.abs()
     eda = 0.8 * eg + 8 * U * (1 + g.abs())
     dg, du = dh * u * da, dh * a
@@ -146,9 +148,9 @@ def test_random_numbers(rows, n, k, act):
     h32 = glu.gated_linear(x.cuda(), w, act=act, dtype="f32")
     _within(h32, *want[0], "h in fp32")
     # in the norm the results are as near as their roundings: bf16's half step is at most
-    # 2^-8 of a value, uniform roundings 2^-8 / sqrt 3, four of them one after the other
+    # 2^-8 of a value, uniform roundings 2^-8 / sqrt 3, two of them one after the other
     for a, b in zip((h32, *got), want):
-        assert float((a.double().cpu() - b[0]).norm() / b[0].norm()) < 2 * H
+        assert float((a.double().cpu() - b[0]).norm() / b[0].norm()) < H
 
 
 def test_gradient_against_differences():
