@@ -44,7 +44,9 @@ typedef enum { AGS_GLU_SILU = 0, AGS_GLU_GELU = 1 } ags_glu_act;
 
 /* Both weights, laid out for the products: rows of `padded` = k rounded up to
  * 64 bf16 elements; 16 rows of gate, the same 16 of up, and so on, `lines` = 2
- * (n rounded up to 16) rows in all, padding zero.  data: device memory of
+ * (n rounded up to 16) rows in all, padding zero.  They lie in panels of 32 rows
+ * and 64 elements, each in one piece, row after row; panel (i, j) is the
+ * (i padded / 64 + j)-th.  data: device memory of
  * ags_glu_bytes bytes, 16-byte aligned (NULL where that is 0). */
 typedef struct {
     void *data;

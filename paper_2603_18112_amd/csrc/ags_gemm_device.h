@@ -53,6 +53,13 @@ struct Fp16 {
 // the contracted axis to the next multiple of 64 are zeros (or meet zeros).
 // Along: `rows` is the contracted axis, of any length, and a row holds `width`
 // elements of its side (a multiple of 8).
+//
+// Or in panels: `rows` a multiple of 32 (along: zeros, or meet zeros, where it
+// was rounded up to one), `pitch` of 128 (64 elements); panel (i, j), rows from 32 i and
+// elements from 64 j on, is 4096 bytes in one piece, row after row, and the
+// panels of the same rows follow one another.  What a tile loads in a stage then lies
+// in pieces of 4 KiB, not in lines a pitch apart, which fall on few of the memory's
+// channels where the pitch is a power of two.
 struct Side {
     const void* p;
     int64_t pitch, rows, width;
@@ -73,11 +80,15 @@ constexpr int lds_bytes(int tm, int tn, int na, int nb) { return 64 * (tm * na +
 // each lane gets one column of them.  The pieces are permuted by 64 bytes a row,
 // so that the four rows (and the neighbouring 16 columns of the next 16 lanes)
 // lie on different banks.
-template <int W, bool ALONG>
+enum Form : int { kAcross = 0, kAlong = 1, kAcrossPanels = 2, kAlongPanels = 3 };
+
+template <int W, int FORM>
 struct Loader {
+    static constexpr bool ALONG = FORM & 1, PANELS = FORM & 2;
     static constexpr int kLoads = W / 32;       // of a wave, 1024 bytes each, a stage
     static constexpr int kFragments = W / 64;   // 32 of the side each, of a wave
     static constexpr int kRow = ALONG ? 2 * W : 128, kRows = 1024 / kRow;  // bytes of a row, rows of a load
+    static constexpr unsigned kStage = PANELS ? 4096 : 128;  // across: bytes to the next stage
 
     const char* base;     // along: of the stage that is loaded next; across: of the tile
     unsigned pitch, records, offset;
@@ -91,12 +102,13 @@ struct Loader {
         pitch = (unsigned)s.pitch;
         const int row = w * kRows + lane * 16 / kRow, piece = lane * 16 % kRow / 16;
         if constexpr (ALONG) {
-            base = p + at * 2 + (int64_t)stage * kDepth * s.pitch;
+            base = p + (PANELS ? at / 64 * 4096 : at * 2) + (int64_t)stage * kDepth * s.pitch;
             left = (int)(s.rows - (int64_t)stage * kDepth);
-            width = (unsigned)min((int64_t)W, s.width - at) * 2;
+            // (in panels: the bytes of 32 rows from this column on)
+            width = PANELS ? 32 * pitch - (unsigned)(at / 64 * 4096) : (unsigned)min((int64_t)W, s.width - at) * 2;
             last = offset = 0;
-            const int swizzle = W == 64 ? (row >> 1) & 1 : row & 3;
-            first = row * pitch + (piece ^ (4 * swizzle)) * 16;
+            const int swizzle = W == 64 ? (row >> 1) & 1 : row & 3, from = piece ^ (4 * swizzle);
+            first = PANELS ? row * 128 + from / 8 * 4096 + from % 8 * 16 : row * pitch + from * 16;
             const int h = lane >> 5, g = (lane >> 4) & 1, t = (lane >> 2) & 3, c = lane & 3;
 #pragma unroll
             for (int f = 0; f < kFragments; ++f)
@@ -105,13 +117,13 @@ struct Loader {
         } else {
             base = p + at * s.pitch;
             const int rows = (int)min((int64_t)W, s.rows - at);
-            offset = stage * 128;
+            offset = stage * kStage;
             records = live ? rows * pitch : 0u;
             left = 0;
             width = 0;
             const unsigned to = (unsigned)(piece ^ ((row >> 1) & 7)) * 16;  // row + 32 i: the same
-            first = row * pitch + to;
-            last = (rows - 1) * pitch + to;
+            first = (PANELS ? row * 128 : row * pitch) + to;
+            last = PANELS ? (rows / 32 - 1) * 32 * pitch + first : (rows - 1) * pitch + to;
             const int r = lane & 31, h = lane >> 5;
 #pragma unroll
             for (int j = 0; j < 4; ++j)
@@ -120,6 +132,7 @@ struct Loader {
     }
 
     __device__ __forceinline__ unsigned along_records() const {
+        if constexpr (PANELS) return left > 0 ? (min(left, kDepth) - 32) * pitch + width : 0u;
         return left > 0 ? (min(left, kDepth) - 1) * pitch + width : 0u;
     }
 
@@ -130,7 +143,7 @@ struct Loader {
             left -= kDepth;
             records = live ? along_records() : 0u;
         } else {
-            offset = live ? offset + 128 : 0u;  // (it may be taken off the buffer's size)
+            offset = live ? offset + kStage : 0u;  // (it may be taken off the buffer's size)
             records = live ? records : 0u;
         }
     }
@@ -140,7 +153,9 @@ struct Loader {
         const __amdgpu_buffer_rsrc_t r =
             __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, records, 0x00027000);
         const unsigned at = to + (i * 4 + w) * 1024;
-        if constexpr (ALONG) load_lds16(r, at, first + i * (4 * kRows) * pitch, 0u);
+        constexpr int kMore = 4 * kRows;  // rows to the next load
+        if constexpr (ALONG && PANELS) load_lds16(r, at, first + i * kMore / 32 * 32 * pitch + i * kMore % 32 * 128, 0u);
+        else if constexpr (ALONG) load_lds16(r, at, first + i * kMore * pitch, 0u);
         else load_lds16(r, at, min(first + i * 32 * pitch, last), offset);
     }
 
@@ -198,15 +213,15 @@ __device__ __forceinline__ void to_strip(const v16f (&acc)[FN], char* strip, int
 // a start in the last step of stage s for s + NA, whose buffer the barrier before it
 // has freed; those of b in the first step for s + NB - 1.  What a stage loads has
 // at least three steps (NA = 2) to arrive.
-template <typename E, int TM, int TN, int NA, int NB, bool ALONG_A, bool ALONG_B, typename Out>
+template <typename E, int TM, int TN, int NA, int NB, int FORM_A, int FORM_B, typename Out>
 __device__ __forceinline__ void product_tile(const Side& a, const Side& b, int s0, int s1, int64_t i0, int64_t j0,
                                              int64_t m, int64_t n, char* sm, const Out& out) {
     constexpr int BM = 64 * TM, BN = 64 * TN, FM = TM, FN = TN;
     static_assert(NB == NA || NB == NA + 1, "the count of loads under way below");
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = w >> 1, wn = w & 1;
-    Loader<BM, ALONG_A> la(a, i0, s0, s0 < s1, w, lane, wm);
-    Loader<BN, ALONG_B> lb(b, j0, s0, s0 < s1, w, lane, wn);
+    Loader<BM, FORM_A> la(a, i0, s0, s0 < s1, w, lane, wm);
+    Loader<BN, FORM_B> lb(b, j0, s0, s0 < s1, w, lane, wn);
     const unsigned lds0 = (unsigned)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)sm);
     constexpr int kA = BM / 32, kB = BN / 32;          // a wave's loads of a stage
     constexpr int kBufA = BM * 128, kBufB = BN * 128, kAtB = NA * kBufA;

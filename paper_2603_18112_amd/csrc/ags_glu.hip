@@ -38,7 +38,7 @@ __global__ __launch_bounds__(256) void glu_store_kernel(GluStoreArgs a) {
             if (a.bf16) load8(static_cast<const u16*>(p) + at, a.k - c, x);
             else load8(static_cast<const float*>(p) + at, a.k - c, x);
         }
-        store8(static_cast<u16*>(a.data) + line * padded + c, 8, x);
+        store8(static_cast<u16*>(a.data) + line / 32 * 32 * padded + c / 64 * 2048 + line % 32 * 64 + c % 64, 8, x);
     }
 }
 
@@ -61,9 +61,23 @@ __global__ __launch_bounds__(256) void glu_pack_kernel(GluPackArgs a) {
 __device__ __forceinline__ float sigmoid(float g) {
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.44269504f));
 }
+// (1 + erf(g / sqrt 2)) / 2, and e^(-g g / 2): erfc(x) = p(t) e^(-x x), t = 1 / (1 + 0.3275911 x),
+// for x >= 0, p of degree 5: formula 7.1.26 of Abramowitz and Stegun, Handbook of
+// Mathematical Functions, within 1.5e-7.
+__device__ __forceinline__ float normal_below(float g, float* e) {
+    const float x = fabsf(g) * 0.70710678f, t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.0f));
+    *e = __builtin_amdgcn_exp2f(g * g * -0.72134752f);
+    float p = fmaf(1.061405429f, t, -1.453152027f);
+    p = fmaf(p, t, 1.421413741f);
+    p = fmaf(p, t, -0.284496736f);
+    p = fmaf(p, t, 0.254829592f);
+    const float q = 0.5f * p * t * *e;
+    return g < 0.0f ? q : 1.0f - q;
+}
 __device__ __forceinline__ float act_of(int act, float g) {
     if (act == AGS_GLU_SILU) return g * sigmoid(g);
-    return 0.5f * g * (1.0f + erff(g * 0.70710678f));
+    float e;
+    return g * normal_below(g, &e);
 }
 __device__ __forceinline__ void act_both(int act, float g, float* f, float* d) {
     if (act == AGS_GLU_SILU) {
@@ -71,9 +85,10 @@ __device__ __forceinline__ void act_both(int act, float g, float* f, float* d) {
         *f = g * s;
         *d = s * fmaf(g, 1.0f - s, 1.0f);
     } else {
-        const float c = 0.5f * (1.0f + erff(g * 0.70710678f));
+        float e;
+        const float c = normal_below(g, &e);
         *f = g * c;
-        *d = fmaf(g * 0.39894228f, __builtin_amdgcn_exp2f(g * g * -0.72134752f), c);
+        *d = fmaf(g * 0.39894228f, e, c);
     }
 }
 
@@ -410,7 +425,7 @@ __global__ __launch_bounds__(256, 1) void glu_product_kernel(GluArgs a, unsigned
     extern __shared__ __attribute__((aligned(16))) char sm[];
     const int64_t lines = glu_lines(a.n), padded = glu_padded(a.k);
     const Place p = place<T>(padded, a.splits, tm, tn);
-    gemm::product_tile<gemm::Bf16, T, T, NA, NB, false, false>(
+    gemm::product_tile<gemm::Bf16, T, T, NA, NB, gemm::kAcross, gemm::kAcrossPanels>(
         Side{a.x, a.x_stride * 2, a.rows, 0}, Side{a.w, padded * 2, lines, 0}, p.s0, p.s1, p.i0, p.j0, a.rows, lines, sm,
         PairOut<MODE, ACT>{a, part_of(a.partials, a.splits, p, a.rows, lines)});
 }
@@ -420,7 +435,7 @@ __global__ __launch_bounds__(256, 1) void glu_dx_kernel(GluBackArgs a, unsigned 
     extern __shared__ __attribute__((aligned(16))) char sm[];
     const int64_t lines = glu_lines(a.n), padded = glu_padded(a.k), grads = glu_grads(a.n);
     const Place p = place<T>(grads, a.splits, tm, tn);
-    gemm::product_tile<gemm::Bf16, T, T, NA, NB, false, true>(
+    gemm::product_tile<gemm::Bf16, T, T, NA, NB, gemm::kAcross, gemm::kAlongPanels>(
         Side{a.grads, grads * 2, a.rows, 0}, Side{a.w, padded * 2, lines, padded}, p.s0, p.s1, p.i0, p.j0, a.rows, a.k, sm,
         RowOut<false>{a, part_of(a.partials, a.splits, p, a.rows, a.k)});
 }
@@ -430,7 +445,7 @@ __global__ __launch_bounds__(256, 1) void glu_dw_kernel(GluBackArgs a, unsigned 
     extern __shared__ __attribute__((aligned(16))) char sm[];
     const int64_t lines = glu_lines(a.n), grads = glu_grads(a.n);
     const Place p = place<T>(a.rows, a.splits, tm, tn);
-    gemm::product_tile<gemm::Bf16, T, T, NA, NB, true, true>(
+    gemm::product_tile<gemm::Bf16, T, T, NA, NB, gemm::kAlong, gemm::kAlong>(
         Side{a.grads, grads * 2, a.rows, grads}, Side{a.x, a.x_stride * 2, a.rows, a.x_width}, p.s0, p.s1, p.i0, p.j0,
         lines, a.k, sm, RowOut<true>{a, part_of(a.partials, a.splits, p, lines, a.k)});
 }
@@ -498,60 +513,102 @@ __global__ __launch_bounds__(256) void glu_act_kernel(GluActArgs a) {
 
 // Up to 16 MT rows of x against all of w: every weight is read once, straight
 // into registers, so the kernel is bound by the weights' bytes.  A block takes 32
-// lines of w, 16 units of gate and of up; its waves share the contracted axis,
-// 32 elements (64 bytes of a line) at a time, and their sums meet in LDS, in a
-// fixed order.
+// lines of w, 16 units of gate and of up; its waves share the contracted axis and
+// their sums meet in LDS, in a fixed order.  A wave's loads are of whole cache lines, 8
+// lines of w and 128 bytes each, one after the other in memory: as an operand the 16 lanes r then hold line r / 2, the even
+// ones the first 32 of 64 elements, the odd ones the second.  Products with both
+// halves of x are taken, and of their results those that met their own half: twice
+// the matrix instructions, which wait for memory anyway.
 constexpr int kFewWaves = 8;
 
 template <int MT>
+struct FewOperands {
+    static constexpr int kBatch = MT == 1 ? 2 : 1;  // chunks of 64 elements; two such sets are under way
+    uint4 w[kBatch][4], x[kBatch][MT][2];
+};
+
+template <int MT>
 __global__ __launch_bounds__(kFewWaves * 64) void glu_few_kernel(GluArgs a) {
-    __shared__ float red[kFewWaves][2][MT][4][64];
+    __shared__ float red[kFewWaves][2][2][2][MT][64];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, r = lane & 15, q = lane >> 4;
     const int64_t padded = glu_padded(a.k), line = (int64_t)blockIdx.x * 32;
-    const u16* pw = static_cast<const u16*>(a.w) + (line + r) * padded + q * 8;
+    const int chunks = (int)(padded / 64);
+    // a chunk is a panel of w: gate's lines 0 .. 7 and 8 .. 15, up's
+    const u16* pw = static_cast<const u16*>(a.w) + line * padded + (r >> 1) * 64 + (r & 1) * 32 + q * 8;
     const u16* px[MT];
 #pragma unroll
     for (int t = 0; t < MT; ++t)
         px[t] = static_cast<const u16*>(a.x) + min((int64_t)(t * 16 + r), a.rows - 1) * a.x_stride + q * 8;
-    gemm::v4f acc[2][MT];
+    gemm::v4f acc[4][MT][2];
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int t = 0; t < MT; ++t) acc[s][t] = gemm::v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    const int64_t chunks = padded / 32;
-    for (int64_t c = w; c < chunks; c += kFewWaves) {
-        const uint4 g = *reinterpret_cast<const uint4*>(pw + c * 32);
-        const uint4 u = *reinterpret_cast<const uint4*>(pw + 16 * padded + c * 32);
-#pragma unroll
-        for (int t = 0; t < MT; ++t) {
-            const uint4 x = *reinterpret_cast<const uint4*>(px[t] + c * 32);
-            acc[0][t] = gemm::Bf16::mfma16(g, x, acc[0][t]);
-            acc[1][t] = gemm::Bf16::mfma16(u, x, acc[1][t]);
-        }
-    }
-    // Lane l holds row l % 16 of x, and of the 16 units the four from 4 (l / 16).
-#pragma unroll
-    for (int s = 0; s < 2; ++s)
+    for (int s = 0; s < 4; ++s)
 #pragma unroll
         for (int t = 0; t < MT; ++t)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) red[w][s][t][i][lane] = acc[s][t][i];
+            for (int j = 0; j < 2; ++j) acc[s][t][j] = gemm::v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    // Chunks past the end read the last one again, and multiply zeros.
+    auto load = [&](FewOperands<MT>& o, int c) {
+#pragma unroll
+        for (int b = 0; b < FewOperands<MT>::kBatch; ++b) {
+            const int at = c + b * kFewWaves, from = min(at, chunks - 1);
+#pragma unroll
+            for (int s = 0; s < 4; ++s) o.w[b][s] = *reinterpret_cast<const uint4*>(pw + from * 2048 + s * 512);
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    o.x[b][t][j] = *reinterpret_cast<const uint4*>(px[t] + from * 64 + j * 32);
+                    if (at >= chunks) o.x[b][t][j] = make_uint4(0, 0, 0, 0);
+                }
+            if (at >= chunks) o.w[b][0] = o.w[b][1] = o.w[b][2] = o.w[b][3] = make_uint4(0, 0, 0, 0);
+        }
+    };
+    auto multiply = [&](const FewOperands<MT>& o) {
+#pragma unroll
+        for (int b = 0; b < FewOperands<MT>::kBatch; ++b)
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int s = 0; s < 4; ++s)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) acc[s][t][j] = gemm::Bf16::mfma16(o.w[b][s], o.x[b][t][j], acc[s][t][j]);
+    };
+    constexpr int kRound = kFewWaves * FewOperands<MT>::kBatch;
+    if (w < chunks) {
+        FewOperands<MT> one, two;
+        load(one, w);
+        for (int c = w; c < chunks; c += 2 * kRound) {
+            if (c + kRound < chunks) load(two, c + kRound);
+            multiply(one);
+            if (c + kRound >= chunks) break;
+            if (c + 2 * kRound < chunks) load(one, c + 2 * kRound);
+            multiply(two);
+        }
+    }
+    // A lane's four results are of operand lines 4 q .. 4 q + 3: lines 2 q and 2 q + 1 of w,
+    // by halves.
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            red[w][s >> 1][s & 1][0][t][lane] = acc[s][t][0][0] + acc[s][t][1][1];
+            red[w][s >> 1][s & 1][1][t][lane] = acc[s][t][0][2] + acc[s][t][1][3];
+        }
     __syncthreads();
+    // Eight units of a row to a thread.
     for (int e = threadIdx.x; e < MT * 32; e += kFewWaves * 64) {
         const int t = e >> 5, row = e >> 1 & 15, half = e & 1;
         if (t * 16 + row >= a.rows) continue;
-        float g[8], u[8];
+        float x[2][8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int l = (half * 2 + i / 4) * 16 + row;
-            g[i] = u[i] = 0.0f;
+        for (int i = 0; i < 8; ++i)
 #pragma unroll
-            for (int v = 0; v < kFewWaves; ++v) {
-                g[i] += red[v][0][t][i % 4][l];
-                u[i] += red[v][1][t][i % 4][l];
+            for (int up = 0; up < 2; ++up) {
+                x[up][i] = 0.0f;
+#pragma unroll
+                for (int v = 0; v < kFewWaves; ++v) x[up][i] += red[v][up][half][i & 1][t][(i >> 1) * 16 + row];
             }
-        }
-        put_pair(a, t * 16 + row, line / 2 + half * 8, g, u);
+        put_pair(a, t * 16 + row, line / 2 + half * 8, x[0], x[1]);
     }
 }
 
@@ -597,7 +654,7 @@ hipError_t launch_glu_pack(const GluPackArgs& a, hipStream_t s) {
 hipError_t launch_glu_product(const GluArgs& args, hipStream_t s) {
     GluArgs a = args;
     const int64_t lines = glu_lines(a.n);
-    if (glu_few(a.rows)) {
+    if (glu_few(a.rows, a.n, a.k)) {
         const dim3 grid((unsigned)(lines / 32)), block(kFewWaves * 64);
         if (a.rows <= 16) hipLaunchKernelGGL((glu_few_kernel<1>), grid, block, 0, s, a);
         else hipLaunchKernelGGL((glu_few_kernel<2>), grid, block, 0, s, a);

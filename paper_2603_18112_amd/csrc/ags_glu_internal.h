@@ -72,7 +72,7 @@ struct GluBackArgs {
 };
 
 // The kernel for few rows of x: reads every weight once.
-inline bool glu_few(int64_t rows) { return rows <= 32; }
+inline bool glu_few(int64_t rows, int64_t n, int64_t k) { return rows <= 16 || (rows <= 32 && n * k <= (int64_t)1 << 25); }
 
 // Weak for the same reason as the clipping launchers.
 __attribute__((weak)) hipError_t launch_glu_store(const GluStoreArgs&, hipStream_t);

@@ -42,12 +42,6 @@ __device__ __forceinline__ void store_half8(u16* p, int64_t left, const float* x
     *reinterpret_cast<uint4*>(p) =
         make_uint4(pack_half(y[0], y[1]), pack_half(y[2], y[3]), pack_half(y[4], y[5]), pack_half(y[6], y[7]));
 }
-__device__ __forceinline__ void load_half8(const u16* p, float* x) {
-    const gemm::v8h v = *reinterpret_cast<const gemm::v8h*>(p);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = (float)v[i];
-}
-
 // The matrix of this block and its number in it (i, j: its tile; i: its chunk).
 // Blocks of one matrix go to one XCD as far as that balances: blocks b, b + 8,
 // ... share one.
@@ -216,62 +210,72 @@ __global__ __launch_bounds__(kThreads) void muon_start_kernel(MuonStepArgs a) {
 
 // ------------------------------------------------------------- products --
 
-// Rows of fp32 results in LDS, eight at a time: f(t, c, x) for row t and column c.
-template <int FN, typename F>
-__device__ __forceinline__ void each8(const char* strip, int lane, int64_t rows, int64_t cols, const F& f) {
-    constexpr int kLanes = FN * 4, kRows = 64 / kLanes;
-    const int c = lane % kLanes * 8;
-    if (c >= cols) return;
-    const int end = (int)min(rows, (int64_t)32);
-#pragma unroll 2
-    for (int t = lane / kLanes; t < end; t += kRows) {
-        float x[8];
-        gemm::read8(strip + t * gemm::kPitch<FN> + c * 4, x);
-        f(t, c, x);
-    }
-}
+// How a wave goes through 32 rows of fp32 results in LDS: eight of a row to a lane, from
+// column `c` on, of the rows row(i).
+template <int FN>
+struct Walk {
+    static constexpr int kLanes = FN * 4, kRows = 64 / kLanes, kSteps = 32 / kRows;
+    int c, first, end;  // no rows where the lane's columns lie outside
+
+    __device__ __forceinline__ Walk(int lane, int64_t rows, int64_t cols)
+        : c(lane % kLanes * 8), first(lane / kLanes), end(c < cols ? (int)min(rows, (int64_t)32) : 0) {}
+    __device__ __forceinline__ int row(int i) const { return first + i * kRows; }
+    __device__ __forceinline__ bool has(int i) const { return row(i) < end; }
+    __device__ __forceinline__ char* at(char* strip, int i) const { return strip + row(i) * gemm::kPitch<FN> + c * 4; }
+};
 
 // Tiles below the diagonal are stored above it too: four lanes take the strip's
-// 32 rows of a column, 64 bytes of a row.
+// 32 rows of a column, 64 bytes of a row.  What a tile reads besides is asked for before its
+// sums go to LDS: one wait for memory, not one every other row.
 struct SymmetricOut {
     u16* to;             // A, or b A + c A A
     const u16* from;     // A, where the latter is made
-    int64_t s, pitch;
+    int64_t pitch;
     float add, times;    // x times + A add
     bool mirror;
 
     template <int FN>
     __device__ __forceinline__ void band(const gemm::v16f (&acc)[FN], char* sm, int lane, int64_t row0, int64_t col0,
                                          int64_t rows, int64_t cols) const {
-        constexpr int kWide = FN * 32, sm_pitch = gemm::kPitch<FN>;
+        const Walk<FN> walk(lane, rows, cols);
+        uint4 old[Walk<FN>::kSteps];
+        if (from) {
+#pragma unroll
+            for (int i = 0; i < walk.kSteps; ++i)
+                if (walk.has(i))
+                    old[i] = *reinterpret_cast<const uint4*>(from + (row0 + walk.row(i)) * pitch + col0 + walk.c);
+        }
         gemm::to_strip<FN>(acc, sm, lane);
-        each8<FN>(sm, lane, rows, cols, [&](int t, int c, float* x) {
-            const int64_t at = (row0 + t) * pitch + col0 + c;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] *= times;
+        for (int i = 0; i < walk.kSteps; ++i) {
+            if (!walk.has(i)) continue;
+            float x[8];
+            gemm::read8(walk.at(sm, i), x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] *= times;
             if (from) {
-                float y[8];
-                load_half8(from + at, y);
+                const gemm::v8h y = __builtin_bit_cast(gemm::v8h, old[i]);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = fmaf(y[i], add, x[i]);
+                for (int e = 0; e < 8; ++e) x[e] = fmaf((float)y[e], add, x[e]);
             }
-            store_half8(to + at, cols - c, x);
+            store_half8(to + (row0 + walk.row(i)) * pitch + col0 + walk.c, cols - walk.c, x);
             if (mirror) {
-                float* p = reinterpret_cast<float*>(sm + t * sm_pitch + c * 4);
+                float* p = reinterpret_cast<float*>(walk.at(sm, i));
                 *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
                 *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
             }
-        });
+        }
         if (!mirror) return;
         gemm::lds_wait();
         const int t = (lane & 3) * 8;
         if (t >= rows) return;
 #pragma unroll 2
-        for (int c = lane >> 2; c < kWide; c += 16) {
+        for (int c = lane >> 2; c < FN * 32; c += 16) {
             if (c >= cols) break;
             float x[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const float*>(sm + (t + i) * sm_pitch + c * 4);
+            for (int i = 0; i < 8; ++i)
+                x[i] = *reinterpret_cast<const float*>(sm + (t + i) * gemm::kPitch<FN> + c * 4);
             store_half8(to + (col0 + c) * pitch + row0 + t, rows - t, x);
         }
     }
@@ -284,36 +288,51 @@ struct ApplyOut {
     template <int FN>
     __device__ __forceinline__ void band(const gemm::v16f (&acc)[FN], char* sm, int lane, int64_t row0, int64_t col0,
                                          int64_t rows, int64_t cols) const {
-        gemm::to_strip<FN>(acc, sm, lane);
-        const int64_t pitch = f.m.pitch();
-        float* xs = reinterpret_cast<float*>(a.ws + f.m.x_at());
-        u16* h = reinterpret_cast<u16*>(a.ws + f.m.operand_at(a.turn ^ 1));
-        each8<FN>(sm, lane, rows, cols, [&](int t, int c, float* x) {
-            const int64_t row = row0 + t, at = row * pitch + col0 + c, left = cols - c;
-            float y[8];
-            load8(xs + at, 8, y);  // (zero past the row's end)
+        const Walk<FN> walk(lane, rows, cols);
+        const int64_t pitch = f.m.pitch(), left = cols - walk.c, col = col0 + walk.c;
+        float* xs = reinterpret_cast<float*>(a.ws + f.m.x_at()) + row0 * pitch + col;
+        u16* h = reinterpret_cast<u16*>(a.ws + f.m.operand_at(a.turn ^ 1)) + row0 * pitch + col;
+        float* w = a.w + f.m.offset + row0 * f.m.cols + col;
+        const bool weights = a.result == kMuonWeights;
+        float4 y[Walk<FN>::kSteps][2];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = fmaf(a.a, y[i], x[i] * (1.0f / (kScaleB * kScaleX)));
+        for (int i = 0; i < walk.kSteps; ++i)
+            if (walk.has(i)) {  // (zero past the row's end)
+                y[i][0] = *reinterpret_cast<const float4*>(xs + walk.row(i) * pitch);
+                y[i][1] = *reinterpret_cast<const float4*>(xs + walk.row(i) * pitch + 4);
+            }
+        gemm::to_strip<FN>(acc, sm, lane);
+        const float rate = weights ? -a.rates->lr * f.m.scale : 0.0f, decay = weights ? a.rates->decay : 0.0f;
+#pragma unroll
+        for (int i = 0; i < walk.kSteps; ++i) {
+            if (!walk.has(i)) continue;
+            const int t = walk.row(i);
+            const float old[8] = {y[i][0].x, y[i][0].y, y[i][0].z, y[i][0].w, y[i][1].x, y[i][1].y, y[i][1].z, y[i][1].w};
+            float x[8];
+            gemm::read8(walk.at(sm, i), x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = fmaf(a.a, old[e], x[e] * (1.0f / (kScaleB * kScaleX)));
             if (a.result == kMuonMiddle) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] = i < left ? x[i] : 0.0f;
-                store8(xs + at, 8, y);
+                for (int e = 0; e < 8; ++e) x[e] = e < left ? x[e] : 0.0f;
+                float4* p = reinterpret_cast<float4*>(xs + t * pitch);
+                p[0] = make_float4(x[0], x[1], x[2], x[3]);
+                p[1] = make_float4(x[4], x[5], x[6], x[7]);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] *= kScaleX;
-                store_half8(h + at, 8, y);
-            } else if (a.result == kMuonWeights) {
-                float* w = a.w + f.m.offset + row * f.m.cols + col0 + c;
-                const float rate = -a.rates->lr * f.m.scale, decay = a.rates->decay;
-                load8(w, left, y);
+                for (int e = 0; e < 8; ++e) x[e] *= kScaleX;
+                store_half8(h + t * pitch, 8, x);
+            } else if (weights) {
+                float v[8];
+                load8(w + (int64_t)t * f.m.cols, left, v);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] = fmaf(rate, x[i], y[i] * decay);
-                store8(w, left, y);
+                for (int e = 0; e < 8; ++e) v[e] = fmaf(rate, x[e], v[e] * decay);
+                store8(w + (int64_t)t * f.m.cols, left, v);
             } else {
-                const int64_t o = f.index * a.out_batch_stride + row * a.out_stride + col0 + c;
+                const int64_t o = f.index * a.out_batch_stride + (row0 + t) * a.out_stride + col;
                 if (a.out_bf16) store8(static_cast<u16*>(a.out) + o, left, x);
                 else store8(static_cast<float*>(a.out) + o, left, x);
             }
-        });
+        }
     }
 };
 
@@ -322,14 +341,14 @@ __global__ __launch_bounds__(256, 1) void muon_gram_kernel(MuonProductArgs a) {
     extern __shared__ __attribute__((aligned(16))) char sm[];
     const Found f = find<true>(a.work);
     const int64_t s = f.m.side(), pitch = f.m.pitch();
-    const SymmetricOut out{reinterpret_cast<u16*>(a.ws + f.m.a_at()), nullptr, s, f.m.a_pitch(), 0.0f,
+    const SymmetricOut out{reinterpret_cast<u16*>(a.ws + f.m.a_at()), nullptr, f.m.a_pitch(), 0.0f,
                            kScaleA / (kScaleX * kScaleX), f.i != f.j};
     const Side x{a.ws + f.m.operand_at(a.turn), pitch * 2, f.m.rows, pitch};
     const int64_t i0 = (int64_t)f.i * 64 * T, j0 = (int64_t)f.j * 64 * T;
     if (f.m.tall())
-        gemm::product_tile<gemm::Fp16, T, T, NA, NB, true, true>(x, x, 0, (f.m.rows + 63) / 64, i0, j0, s, s, sm, out);
+        gemm::product_tile<gemm::Fp16, T, T, NA, NB, gemm::kAlong, gemm::kAlong>(x, x, 0, (f.m.rows + 63) / 64, i0, j0, s, s, sm, out);
     else
-        gemm::product_tile<gemm::Fp16, T, T, NA, NB, false, false>(x, x, 0, (int)(pitch / 64), i0, j0, s, s, sm, out);
+        gemm::product_tile<gemm::Fp16, T, T, NA, NB, gemm::kAcross, gemm::kAcross>(x, x, 0, (int)(pitch / 64), i0, j0, s, s, sm, out);
 }
 
 template <int T, int NA, int NB>
@@ -338,10 +357,10 @@ __global__ __launch_bounds__(256, 1) void muon_square_kernel(MuonProductArgs a) 
     const Found f = find<true>(a.work);
     const int64_t s = f.m.side(), pitch = f.m.a_pitch();
     const u16* gram = reinterpret_cast<const u16*>(a.ws + f.m.a_at());
-    const SymmetricOut out{reinterpret_cast<u16*>(a.ws + f.m.b_at()), gram, s, pitch, a.b * (kScaleB / kScaleA),
+    const SymmetricOut out{reinterpret_cast<u16*>(a.ws + f.m.b_at()), gram, pitch, a.b * (kScaleB / kScaleA),
                            a.c * (kScaleB / (kScaleA * kScaleA)), f.i != f.j};
     const Side x{gram, pitch * 2, s, 0};
-    gemm::product_tile<gemm::Fp16, T, T, NA, NB, false, false>(x, x, 0, (int)(pitch / 64), (int64_t)f.i * 64 * T,
+    gemm::product_tile<gemm::Fp16, T, T, NA, NB, gemm::kAcross, gemm::kAcross>(x, x, 0, (int)(pitch / 64), (int64_t)f.i * 64 * T,
                                                            (int64_t)f.j * 64 * T, s, s, sm, out);
 }
 
@@ -354,10 +373,10 @@ __global__ __launch_bounds__(256, 1) void muon_apply_kernel(MuonProductArgs a) {
     const int64_t i0 = (int64_t)f.i * 64 * T, j0 = (int64_t)f.j * 64 * T;
     const ApplyOut out{a, f};
     if (f.m.tall())
-        gemm::product_tile<gemm::Fp16, T, T, NA, NB, false, false>(x, b, 0, (int)(ap / 64), i0, j0, f.m.rows, f.m.cols, sm,
+        gemm::product_tile<gemm::Fp16, T, T, NA, NB, gemm::kAcross, gemm::kAcross>(x, b, 0, (int)(ap / 64), i0, j0, f.m.rows, f.m.cols, sm,
                                                                out);
     else
-        gemm::product_tile<gemm::Fp16, T, T, NA, NB, false, true>(b, x, 0, (int)(ap / 64), i0, j0, f.m.rows, f.m.cols, sm,
+        gemm::product_tile<gemm::Fp16, T, T, NA, NB, gemm::kAcross, gemm::kAlong>(b, x, 0, (int)(ap / 64), i0, j0, f.m.rows, f.m.cols, sm,
                                                               out);
 }
 

@@ -113,15 +113,17 @@ inline int muon_tile_side(const std::vector<MuonProduct>& v) {
     int best = 1;
     double least = 1e30;
     for (int t : {1, 2, 4}) {
-        const double stage = t == 1 ? 0.09 : t == 2 ? 0.26 : 1.15;   // us on a CU that is full of such tiles
-        const double alone = t == 1 ? 0.26 : t == 2 ? 0.34 : 1.15, ends = t == 1 ? 1.4 : t == 2 ? 3 : 6;
         double sum = 0, longest = 0;
         for (const MuonProduct& p : v) {
             const double stages = (double)((p.k + 63) / 64);
-            sum += (double)muon_tiles(p, t) * (double)p.count * (stages * stage + ends * stage / alone);
-            longest = std::max(longest, stages * alone + ends);
+            sum += (double)muon_tiles(p, t) * (double)p.count * gemm_among(t, stages);
+            longest = std::max(longest, gemm_alone(t, stages));
         }
-        const double us = std::max(sum / 256, longest);
+        // Long launches run at the clock that the power limit leaves: 0.70 PFLOP/s with
+        // tiles of 128 squared, 1.2 with 256.
+        if (sum > 256 * 100) sum *= t == 4 ? 1.25 : t == 2 ? 1.7 : 1.5;
+        // a last round that is not full takes as long as a full one
+        const double us = std::max(sum / 256 + (t == 4 ? 0.5 : t == 2 ? 0.25 : 0.1) * longest, longest);
         if (us < least) {
             least = us;
             best = t;

@@ -231,7 +231,7 @@ def test_weight_updates_in_place():
     assert torch.equal(glu.gated_linear(x.bfloat16().cuda(), w).cpu(), _rounded(_whole_results(x, gate, up, dh)[2], B))
     m = torch.randn(30, 50).cuda()
     w.update(m, m)
-    z = w.data.view(-1, 2, 16, 64)
+    z = w.data.view(-1, 2, 16, 64)              # one panel to 32 lines: k is below 64
     assert torch.equal(z[:, 0].reshape(-1, 64)[:30, :50], m.bfloat16()) and torch.equal(z[:, 0], z[:, 1])
     assert (z[:, 0].reshape(-1, 64)[30:] == 0).all() and (z[:, 0].reshape(-1, 64)[:, 50:] == 0).all()
 
