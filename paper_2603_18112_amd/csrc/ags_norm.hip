@@ -64,10 +64,23 @@ __device__ __forceinline__ void store8_any(void* p, bool bf16, int64_t at, int64
     else store8(static_cast<float*>(p) + at, left, x);
 }
 
+// v plus what the lane that CTRL names holds, zero where there is none.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float plus(float v) {
+    return v + __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(v), CTRL, ROWS, 0xf, false));
+}
+
+// The sum over a wave, in every lane: within rows of 16 lanes by shifts of 1, 2, 4, 8,
+// then the rows' last lanes to the next row and the next half.  (Six shuffles through
+// LDS took a third of a row's time.)
 __device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-    return v;
+    v = plus<0x111, 0xf>(v);
+    v = plus<0x112, 0xf>(v);
+    v = plus<0x114, 0xf>(v);
+    v = plus<0x118, 0xf>(v);
+    v = plus<0x142, 0xa>(v);
+    v = plus<0x143, 0xc>(v);
+    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 63));
 }
 
 // Sums of N values over the G lanes of a row, in every lane.  Over a block they
@@ -94,46 +107,132 @@ __device__ __forceinline__ void row_sum(float (&v)[N], float (*red)[N][16], int 
     }
 }
 
+// 16 bytes of a row: 8 or 4 elements, as they lie in memory, and as fp32.
+template <typename T>
+struct Piece {
+    static constexpr int kN = 16 / sizeof(T);
+
+    // What lies before the row's end (`left` elements); the rest zeros.
+    static __device__ __forceinline__ uint4 load(const T* p, int64_t left) {
+        if (left >= kN) {
+            const auto w = *reinterpret_cast<const Unaligned<unsigned, 4, sizeof(T)>*>(p);
+            return make_uint4(w.v[0], w.v[1], w.v[2], w.v[3]);
+        }
+        unsigned v[4] = {};
+#pragma unroll
+        for (int i = 0; i < kN; ++i)
+            if (i < left) {
+                if constexpr (kN == 8) v[i >> 1] |= (unsigned)p[i] << (16 * (i & 1));
+                else v[i] = __float_as_uint(p[i]);
+            }
+        return make_uint4(v[0], v[1], v[2], v[3]);
+    }
+    static __device__ __forceinline__ void unpack(uint4 w, float* x) {
+        const unsigned v[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int i = 0; i < kN; ++i)
+            x[i] = __uint_as_float(kN == 4 ? v[i] : i & 1 ? v[i >> 1] & 0xffff0000u : v[i >> 1] << 16);
+    }
+};
+
+// N elements of a tensor of either type from element `at` on, as many as lie in it.
+template <int N>
+__device__ __forceinline__ void load_any(const void* p, bool bf16, int64_t at, int64_t left, float* x) {
+    if constexpr (N == 8) {
+        load8_any(p, bf16, at, left, x);
+    } else if (bf16) {
+        const unsigned short* q = static_cast<const unsigned short*>(p) + at;
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = i < left ? __uint_as_float((unsigned)q[i] << 16) : 0.0f;
+    } else {
+        Piece<float>::unpack(Piece<float>::load(static_cast<const float*>(p) + at, left), x);
+    }
+}
+template <int N>
+__device__ __forceinline__ void store_any(void* p, bool bf16, int64_t at, int64_t left, const float* x) {
+    if constexpr (N == 8) {
+        store8_any(p, bf16, at, left, x);
+    } else if (bf16) {
+        unsigned short* q = static_cast<unsigned short*>(p) + at;
+        const unsigned v[2] = {pack2(x[0], x[1]), pack2(x[2], x[3])};
+        if (left >= 4) {
+            Unaligned<unsigned, 2, 2> w;
+            w.v[0] = v[0], w.v[1] = v[1];
+            *reinterpret_cast<Unaligned<unsigned, 2, 2>*>(q) = w;
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < left) q[i] = (unsigned short)(v[i >> 1] >> (16 * (i & 1)));
+    } else {
+        float* q = static_cast<float*>(p) + at;
+        if (left >= 4) {
+            Unaligned<float, 4, 4> w;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w.v[i] = x[i];
+            *reinterpret_cast<Unaligned<float, 4, 4>*>(q) = w;
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < left) q[i] = x[i];
+    }
+}
+
 // ---------------------------------------------------------------- forward --
 
-// G lanes to a row, NV pieces of 8 elements each; a block of B threads has B / G
-// rows at a time.  T: x's type.
+// G lanes to a row, NV pieces of 16 bytes each; a block of B threads has B / G
+// rows at a time, and asks for the next ones while it reduces these.  T: x's type.
 template <typename T, int G, int NV, int B>
 __global__ __launch_bounds__(B) void norm_kernel(NormArgs a) {
+    constexpr int N = Piece<T>::kN;
+    // weight and bias stay in registers where these suffice
+    constexpr bool kKeep = B < 1024 || NV * N <= 16;
     __shared__ float red[2][1][16];
     const int lane = threadIdx.x % G;
     const int64_t cols = a.cols, step = (int64_t)gridDim.x * (B / G);
-    float w[NV][8], b[NV][8];
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const int64_t c = ((int64_t)j * G + lane) * 8;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) w[j][i] = 1.0f, b[j][i] = 0.0f;
-        if (c < cols) {
-            if (a.weight) load8_any(a.weight, a.w_bf16, c, cols - c, w[j]);
-            if (a.bias) load8_any(a.bias, a.w_bf16, c, cols - c, b[j]);
-        }
-    }
-    for (int64_t row = (int64_t)blockIdx.x * (B / G) + threadIdx.x / G; row < a.rows; row += step) {
-        const T* p = static_cast<const T*>(a.x) + row * a.x_stride;
-        float x[NV][8], s[1] = {0.0f};
+    int64_t row = (int64_t)blockIdx.x * (B / G) + threadIdx.x / G;
+    uint4 raw[NV];
+    auto fetch = [&](int64_t r) {
+        const T* p = static_cast<const T*>(a.x) + r * a.x_stride;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const int64_t c = ((int64_t)j * G + lane) * 8;
-            load8(p + c, cols - c, x[j]);
+            const int64_t c = ((int64_t)j * G + lane) * N;
+            raw[j] = Piece<T>::load(p + c, r < a.rows ? cols - c : 0);
         }
+    };
+    fetch(row);
+    auto affine = [&](int j, float (&w)[N], float (&b)[N]) {
+        const int64_t c = ((int64_t)j * G + lane) * N;
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i] = 1.0f, b[i] = 0.0f;
+        if (c < cols) {
+            if (a.weight) load_any<N>(a.weight, a.w_bf16, c, cols - c, w);
+            if (a.bias) load_any<N>(a.bias, a.w_bf16, c, cols - c, b);
+        }
+    };
+    float w[kKeep ? NV : 1][N], b[kKeep ? NV : 1][N];
+    if constexpr (kKeep) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) affine(j, w[j], b[j]);
+    }
+    for (; row < a.rows; row += step) {
+        float x[NV][N], s[1] = {0.0f};
+#pragma unroll
+        for (int j = 0; j < NV; ++j) Piece<T>::unpack(raw[j], x[j]);
+        if (row + step < a.rows) fetch(row + step);
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s[0] += x[j][i];
+            for (int i = 0; i < N; ++i) s[0] += x[j][i];
         row_sum<G, 1>(s, red, 0);
         const float mean = s[0] / (float)cols;
         s[0] = 0.0f;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const int64_t c = ((int64_t)j * G + lane) * 8;
+            const int64_t c = ((int64_t)j * G + lane) * N;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < N; ++i) {
                 x[j][i] -= mean;
                 if (c + i < cols) s[0] = fmaf(x[j][i], x[j][i], s[0]);
             }
@@ -142,11 +241,13 @@ __global__ __launch_bounds__(B) void norm_kernel(NormArgs a) {
         const float rstd = 1.0f / sqrtf(s[0] / (float)cols + a.eps);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const int64_t c = ((int64_t)j * G + lane) * 8;
+            const int64_t c = ((int64_t)j * G + lane) * N;
             if (c >= cols) continue;
+            const int k = kKeep ? j : 0;
+            if constexpr (!kKeep) affine(j, w[0], b[0]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[j][i] = fmaf(x[j][i] * rstd, w[j][i], b[j][i]);
-            store8_any(a.y, a.y_bf16, row * a.y_stride + c, cols - c, x[j]);
+            for (int i = 0; i < N; ++i) x[j][i] = fmaf(x[j][i] * rstd, w[k][i], b[k][i]);
+            store_any<N>(a.y, a.y_bf16, row * a.y_stride + c, cols - c, x[j]);
         }
         if (a.saved && lane == 0) {
             a.saved[row] = mean;
@@ -204,51 +305,77 @@ __global__ __launch_bounds__(kLong) void norm_long_kernel(NormArgs a) {
 // a block's rows.
 template <typename T, int G, int NV, int B, bool DW>
 __global__ __launch_bounds__(B) void norm_backward_kernel(NormBackwardArgs a) {
+    constexpr int N = Piece<T>::kN;
+    // 1024 threads have 128 registers each: no row ahead, the weight read anew
+    constexpr bool kRoom = B < 1024 || !DW;
     __shared__ float red[2][2][16];
     const int lane = threadIdx.x % G;
     const int64_t cols = a.cols, step = (int64_t)gridDim.x * (B / G);
-    float w[NV][8], dw[NV][8], db[NV][8];
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const int64_t c = ((int64_t)j * G + lane) * 8;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) w[j][i] = 1.0f, dw[j][i] = 0.0f, db[j][i] = 0.0f;
-        if (c < cols && a.weight) load8_any(a.weight, a.w_bf16, c, cols - c, w[j]);
-    }
-    int slot = 0;
-    for (int64_t row = (int64_t)blockIdx.x * (B / G) + threadIdx.x / G; row < a.rows; row += step, slot ^= 1) {
-        const T *px = static_cast<const T*>(a.x) + row * a.x_stride, *pd = static_cast<const T*>(a.dy) + row * a.dy_stride;
-        const float mean = a.saved[row], rstd = a.saved[a.rows + row];
-        float z[NV][8], g[NV][8], s[2] = {0.0f, 0.0f};
+    int64_t row = (int64_t)blockIdx.x * (B / G) + threadIdx.x / G;
+    uint4 raw_x[NV], raw_d[NV];
+    float mean = 0.0f, rstd = 0.0f;
+    auto fetch = [&](int64_t r) {
+        const T *px = static_cast<const T*>(a.x) + r * a.x_stride, *pd = static_cast<const T*>(a.dy) + r * a.dy_stride;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const int64_t c = ((int64_t)j * G + lane) * 8;
-            load8(px + c, cols - c, z[j]);
-            load8(pd + c, cols - c, g[j]);
+            const int64_t c = ((int64_t)j * G + lane) * N;
+            raw_x[j] = Piece<T>::load(px + c, cols - c);
+            raw_d[j] = Piece<T>::load(pd + c, cols - c);
         }
+        mean = a.saved[r];
+        rstd = a.saved[a.rows + r];
+    };
+    if (kRoom && row < a.rows) fetch(row);
+    auto weight = [&](int j, float (&w)[N]) {
+        const int64_t c = ((int64_t)j * G + lane) * N;
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
+        for (int i = 0; i < N; ++i) w[i] = 1.0f;
+        if (c < cols && a.weight) load_any<N>(a.weight, a.w_bf16, c, cols - c, w);
+    };
+    float w[kRoom ? NV : 1][N], dw[NV][N], db[NV][N];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                z[j][i] = (z[j][i] - mean) * rstd;
+    for (int j = 0; j < NV; ++j) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) dw[j][i] = 0.0f, db[j][i] = 0.0f;
+        if constexpr (kRoom) weight(j, w[j]);
+    }
+    int slot = 0;
+    for (; row < a.rows; row += step, slot ^= 1) {
+        if constexpr (!kRoom) fetch(row);
+        float z[NV][N], g[NV][N], s[2] = {0.0f, 0.0f};
+        const float mu = mean, rs = rstd;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            Piece<T>::unpack(raw_x[j], z[j]);
+            Piece<T>::unpack(raw_d[j], g[j]);
+        }
+        if (kRoom && row + step < a.rows) fetch(row + step);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int k = kRoom ? j : 0;
+            if constexpr (!kRoom) weight(j, w[0]);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                z[j][i] = (z[j][i] - mu) * rs;
                 if constexpr (DW) {
                     dw[j][i] = fmaf(g[j][i], z[j][i], dw[j][i]);
                     db[j][i] += g[j][i];
                 }
-                g[j][i] *= w[j][i];
+                g[j][i] *= w[k][i];
                 s[0] += g[j][i];
                 s[1] = fmaf(g[j][i], z[j][i], s[1]);  // (past the row's end g is zero)
             }
+        }
         if (!a.dx) continue;
         row_sum<G, 2>(s, red, slot);
         const float m0 = s[0] / (float)cols, m1 = s[1] / (float)cols;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const int64_t c = ((int64_t)j * G + lane) * 8;
+            const int64_t c = ((int64_t)j * G + lane) * N;
             if (c >= cols) continue;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) z[j][i] = rstd * (g[j][i] - m0 - z[j][i] * m1);
-            store8(static_cast<T*>(a.dx) + row * a.dx_stride + c, cols - c, z[j]);
+            for (int i = 0; i < N; ++i) z[j][i] = rs * (g[j][i] - m0 - z[j][i] * m1);
+            store_any<N>(a.dx, a.bf16, row * a.dx_stride + c, cols - c, z[j]);
         }
     }
     if constexpr (DW) {
@@ -256,21 +383,21 @@ __global__ __launch_bounds__(B) void norm_backward_kernel(NormBackwardArgs a) {
         if constexpr (G == B) {
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
-                const int64_t c = ((int64_t)j * G + lane) * 8;
+                const int64_t c = ((int64_t)j * G + lane) * N;
                 if (c >= cols) continue;
-                store8(out + c, cols - c, dw[j]);
-                store8(out + cols + c, cols - c, db[j]);
+                store_any<N>(out, false, c, cols - c, dw[j]);
+                store_any<N>(out, false, cols + c, cols - c, db[j]);
             }
         } else {
             // the block's waves, each with rows of its own, one after the other
-            __shared__ float sum[2][G * NV * 8];
+            __shared__ float sum[2][G * NV * N];
             for (int k = 0; k < B / G; ++k) {
                 if ((int)threadIdx.x / G == k) {
 #pragma unroll
                     for (int j = 0; j < NV; ++j)
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const int at = (j * 8 + i) * G + lane;
+                        for (int i = 0; i < N; ++i) {
+                            const int at = (j * N + i) * G + lane;
                             sum[0][at] = k ? sum[0][at] + dw[j][i] : dw[j][i];
                             sum[1][at] = k ? sum[1][at] + db[j][i] : db[j][i];
                         }
@@ -279,12 +406,12 @@ __global__ __launch_bounds__(B) void norm_backward_kernel(NormBackwardArgs a) {
             }
             for (int t = threadIdx.x; t < 2 * G * NV; t += B) {
                 const int which = t / (G * NV), j = t / G % NV, l = t % G;
-                const int64_t c = ((int64_t)j * G + l) * 8;
+                const int64_t c = ((int64_t)j * G + l) * N;
                 if (c >= cols) continue;
-                float v[8];
+                float v[N];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = sum[which][(j * 8 + i) * G + l];
-                store8(out + which * cols + c, cols - c, v);
+                for (int i = 0; i < N; ++i) v[i] = sum[which][(j * N + i) * G + l];
+                store_any<N>(out, false, which * cols + c, cols - c, v);
             }
         }
     }
@@ -362,7 +489,7 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(NormBackwardArgs a) {
 }
 
 // 64 columns of one of the two gradients to a block; its waves share the parts.
-constexpr int kJoinWaves = 8;
+constexpr int kJoinWaves = 16;
 
 __global__ __launch_bounds__(kJoinWaves * 64) void norm_join_kernel(NormBackwardArgs a) {
     __shared__ float sum[kJoinWaves][64];
@@ -375,7 +502,7 @@ __global__ __launch_bounds__(kJoinWaves * 64) void norm_join_kernel(NormBackward
     float v = 0.0f;
     if (c < cols) {
         const float* p = a.partials + which * cols + c;
-#pragma unroll 8
+#pragma unroll 16
         for (int k = wave; k < a.parts; k += kJoinWaves) v += p[(int64_t)k * 2 * cols];
     }
     sum[wave][lane] = v;
@@ -399,18 +526,23 @@ unsigned norm_blocks(int64_t rows, int64_t at_once, int64_t most) {
     return (unsigned)std::max<int64_t>(1, std::min<int64_t>((rows + at_once - 1) / at_once, most));
 }
 
+// NV below is in pieces of bf16; rows of fp32 have twice as many.  More lanes to a row
+// have fewer registers each and more rows in all under way: 8192 x 4096 bf16 with 512, 256
+// and 128 lanes 27.4, 32 and 39 us (4.9 TB/s; a copy 4.7); for 16384 x 8192 with 1024,
+// 512 and 256 lanes 117, 112 and 112.
 template <typename T>
 hipError_t forward(const NormArgs& a, hipStream_t s) {
     const int64_t n = a.cols;
-#define NORM_FORWARD(G, NV, B, MOST)                                                                       \
-    hipLaunchKernelGGL((norm_kernel<T, G, NV, B>), dim3(norm_blocks(a.rows, B / G, MOST)), dim3(B), 0, s, a)
+    constexpr int F = sizeof(T) / 2;
+#define NORM_FORWARD(G, NV, B, MOST)                                                                           \
+    hipLaunchKernelGGL((norm_kernel<T, G, NV * F, B>), dim3(norm_blocks(a.rows, B / G, MOST)), dim3(B), 0, s, a)
     if (n <= 512) NORM_FORWARD(64, 1, 256, 2048);
     else if (n <= 1024) NORM_FORWARD(64, 2, 256, 1536);
     else if (n <= 2048) NORM_FORWARD(256, 1, 256, 2048);
-    else if (n <= 4096) NORM_FORWARD(256, 2, 256, 1536);
+    else if (n <= 4096) NORM_FORWARD(512, 1, 512, 1024);
     else if (n <= 8192) NORM_FORWARD(512, 2, 512, 768);
     else if (n <= 16384) NORM_FORWARD(1024, 2, 1024, 512);
-    else if (n <= kNormForwardCols) NORM_FORWARD(1024, 4, 1024, 256);
+    else if (F == 1 && n <= kNormForwardCols) NORM_FORWARD(1024, 4 / F, 1024, 256);
     else
         hipLaunchKernelGGL((norm_long_kernel<T>), dim3(norm_blocks(a.rows, 1, 512)), dim3(kLong), 0, s, a);
 #undef NORM_FORWARD
@@ -421,11 +553,12 @@ template <typename T>
 hipError_t backward(const NormBackwardArgs& a, hipStream_t s) {
     const int64_t n = a.cols;
     const bool dw = a.dweight || a.dbias;
-#define NORM_BACKWARD(G, NV, B)                                                                                   \
-    do {                                                                                                          \
-        if (dw) hipLaunchKernelGGL((norm_backward_kernel<T, G, NV, B, true>), dim3(a.parts), dim3(B), 0, s, a);   \
-        else hipLaunchKernelGGL((norm_backward_kernel<T, G, NV, B, false>),                                       \
-                                dim3(norm_blocks(a.rows, B / G, 1024)), dim3(B), 0, s, a);                        \
+    constexpr int F = sizeof(T) / 2;
+#define NORM_BACKWARD(G, NV, B)                                                                                       \
+    do {                                                                                                              \
+        if (dw) hipLaunchKernelGGL((norm_backward_kernel<T, G, NV * F, B, true>), dim3(a.parts), dim3(B), 0, s, a);   \
+        else hipLaunchKernelGGL((norm_backward_kernel<T, G, NV * F, B, false>),                                       \
+                                dim3(norm_blocks(a.rows, B / G, 1024)), dim3(B), 0, s, a);                            \
     } while (0)
     if (a.rows == 0) {}  // empty sums
     else if (n <= 512) NORM_BACKWARD(64, 1, 512);

@@ -75,10 +75,11 @@ def _vector(v, cols, what, device):
     """(contiguous [cols] or None, its type's code, address)."""
     if v is None:
         return None, ags.AGS_F32, None
-    if tuple(v.shape) != (cols,) or v.device != device:
+    if v.dim() != 1 or v.shape[0] != cols or v.device != device:
         raise ValueError(f"{what} must be [{cols}], on x's device")
     code = _dtype(v.dtype)[0]
-    v = v.contiguous()
+    if not v.is_contiguous():
+        v = v.contiguous()
     return v, code, v.data_ptr() or None
 
 
@@ -115,8 +116,8 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, dtype=None, save=False):
     bias, b_code, b_ptr = _vector(bias, cols, "bias", dev)
     if weight is not None and bias is not None and w_code != b_code:
         raise ValueError("weight and bias differ in type")
-    y = t.empty(x.shape, dtype=out_dt, device=dev)
-    saved = t.empty((2, rows), dtype=t.float32, device=dev) if save else None
+    y = x.new_empty(x.shape, dtype=out_dt)
+    saved = x.new_empty((2, rows), dtype=t.float32) if save else None
     ags_layer_norm(x2.data_ptr() or None, code, rows, cols, max(stride, 1), w_ptr, b_ptr,
                    w_code if weight is not None else b_code, eps, y.data_ptr() or None, out_code, max(cols, 1),
                    (saved.data_ptr() or None) if save else None, _stream(dev))
@@ -144,7 +145,7 @@ def layer_norm_backward(dy, x, saved, weight=None, dweight=None, dbias=None, dw_
     dbias, db_code = _grad_vector(dbias, need_db, cols, dw_dtype, accumulate, "dbias", dev)
     if None not in (dw_code, db_code) and dw_code != db_code:
         raise ValueError("dweight and dbias differ in type")
-    dx = t.empty(x.shape, dtype=x.dtype, device=dev) if need_dx else None
+    dx = x.new_empty(x.shape) if need_dx else None
     if not (need_dx or need_dw or need_db):
         return None, None, None
     nbytes = ags_layer_norm_backward_workspace(rows, cols) if need_dw or need_db else 0
