@@ -189,6 +189,9 @@ constexpr int kPitch = FN * 128 + 16;
 template <int FN>
 constexpr int kStrip = 32 * kPitch<FN>;
 
+// For outputs that read nothing.
+struct Nothing {};
+
 template <int FN>
 __device__ __forceinline__ void to_strip(const v16f (&acc)[FN], char* strip, int lane) {
     char* p = strip + (lane & 31) * kPitch<FN> + (lane >> 5) * 16;
@@ -205,9 +208,12 @@ __device__ __forceinline__ void to_strip(const v16f (&acc)[FN], char* strip, int
 // contracted axis.  A wave has TM x TN fragments of 32 x 32 results; `out` gets 32 rows of
 // them at a time, and the wave's part of LDS:
 //
-//   out.band<TN>(fragments, strip, lane, row0, col0, rows, cols)
+//   out.band<TN>(fragments, strip, lane, row0, col0, rows, cols, ahead)
 //
-// from (row0, col0) on rows x cols lie in the output (more than the 32 x 32 TN, or none).
+// from (row0, col0) on rows x cols lie in the output (more than the 32 x 32 TN, or
+// none).  `ahead` is what out.begin<TN>(lane, row0, col0, rows, cols) returned: tiles of
+// up to 128 squared have the registers to ask, before their first stage, for what their bands
+// will read; larger ones ask when a band begins.
 //
 // LDS holds NA stages of a and NB of b (NB = NA or NA + 1).  A stage is four steps.  Loads of
 // a start in the last step of stage s for s + NA, whose buffer the barrier before it
@@ -282,6 +288,14 @@ __device__ __forceinline__ void product_tile(const Side& a, const Side& b, int s
         step(3, next_a, next_b, [&](int i) { la.load(i, lds0 + ca * kBufA, w); }, kA);
         la.advance(s + NA + 1 < s1);
     };
+    const int64_t row0 = i0 + wm * (BM / 2), col0 = j0 + wn * (BN / 2);
+    constexpr bool kAhead = FM <= 2;
+    decltype(out.template begin<FN>(lane, row0, col0, m, n)) ahead[kAhead ? FM : 1];
+    if constexpr (kAhead) {
+#pragma unroll
+        for (int x = 0; x < FM; ++x)
+            ahead[x] = out.template begin<FN>(lane, row0 + x * 32, col0, m - row0 - x * 32, n - col0);
+    }
     if (s0 < s1) {
 #pragma unroll
         for (int t = 0; t < NB; ++t) {
@@ -311,19 +325,20 @@ __device__ __forceinline__ void product_tile(const Side& a, const Side& b, int s
     // 32 rows at a time, through the wave's own part of LDS.
     block_barrier();
     char* strip = sm + w * kStrip<FN>;
-    const int64_t row0 = i0 + wm * (BM / 2), col0 = j0 + wn * (BN / 2);
     // (written out: the compiler gives up unrolling the loop where `out` is long, and
     // the sums would go to memory)
-    auto band = [&](const v16f (&c)[FN], int64_t row) {
-        out.template band<FN>(c, strip, lane, row, col0, m - row, n - col0);
+    auto band = [&](const v16f (&c)[FN], int x) {
+        const int64_t row = row0 + x * 32;
+        if constexpr (!kAhead) ahead[0] = out.template begin<FN>(lane, row, col0, m - row, n - col0);
+        out.template band<FN>(c, strip, lane, row, col0, m - row, n - col0, ahead[kAhead ? x : 0]);
         lds_wait();
         __builtin_amdgcn_sched_barrier(0);
     };
-    band(acc[0], row0);
-    if constexpr (FM > 1) band(acc[1], row0 + 32);
+    band(acc[0], 0);
+    if constexpr (FM > 1) band(acc[1], 1);
     if constexpr (FM > 2) {
-        band(acc[2], row0 + 64);
-        band(acc[3], row0 + 96);
+        band(acc[2], 2);
+        band(acc[3], 3);
     }
     static_assert(FM == 1 || FM == 2 || FM == 4, "bands of a tile");
 }

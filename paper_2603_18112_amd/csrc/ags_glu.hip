@@ -228,8 +228,13 @@ struct PairOut {
     float* part;
 
     template <int FN>
+    __device__ __forceinline__ gemm::Nothing begin(int, int64_t, int64_t, int64_t, int64_t) const {
+        return {};
+    }
+
+    template <int FN>
     __device__ __forceinline__ void band(const gemm::v16f (&acc)[FN], char* strip, int lane, int64_t row0, int64_t col0,
-                                         int64_t rows, int64_t cols) const {
+                                         int64_t rows, int64_t cols, gemm::Nothing) const {
         if constexpr (MODE == kGluPart) put_part<FN>(acc, part, glu_lines(a.n), strip, lane, row0, col0, rows, cols);
         else if constexpr (MODE == kGluForward) forward<FN>(acc, strip, lane, row0, col0, rows, cols);
         else grads<FN>(acc, strip, lane, row0, col0, rows, cols);
@@ -358,8 +363,13 @@ struct RowOut {
     float* part;
 
     template <int FN>
+    __device__ __forceinline__ gemm::Nothing begin(int, int64_t, int64_t, int64_t, int64_t) const {
+        return {};
+    }
+
+    template <int FN>
     __device__ __forceinline__ void band(const gemm::v16f (&acc)[FN], char* strip, int lane, int64_t row0, int64_t col0,
-                                         int64_t rows, int64_t cols) const {
+                                         int64_t rows, int64_t cols, gemm::Nothing) const {
         if (part) {
             put_part<FN>(acc, part, a.k, strip, lane, row0, col0, rows, cols);
         } else if (a.bf16 && !a.accumulate) {

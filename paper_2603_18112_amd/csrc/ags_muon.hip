@@ -225,8 +225,7 @@ struct Walk {
 };
 
 // Tiles below the diagonal are stored above it too: four lanes take the strip's
-// 32 rows of a column, 64 bytes of a row.  What a tile reads besides is asked for before its
-// sums go to LDS: one wait for memory, not one every other row.
+// 32 rows of a column, 64 bytes of a row.
 struct SymmetricOut {
     u16* to;             // A, or b A + c A A
     const u16* from;     // A, where the latter is made
@@ -235,16 +234,26 @@ struct SymmetricOut {
     bool mirror;
 
     template <int FN>
-    __device__ __forceinline__ void band(const gemm::v16f (&acc)[FN], char* sm, int lane, int64_t row0, int64_t col0,
-                                         int64_t rows, int64_t cols) const {
+    struct Old {
+        uint4 v[Walk<FN>::kSteps];
+    };
+    template <int FN>
+    __device__ __forceinline__ Old<FN> begin(int lane, int64_t row0, int64_t col0, int64_t rows, int64_t cols) const {
         const Walk<FN> walk(lane, rows, cols);
-        uint4 old[Walk<FN>::kSteps];
-        if (from) {
+        Old<FN> old;
 #pragma unroll
-            for (int i = 0; i < walk.kSteps; ++i)
-                if (walk.has(i))
-                    old[i] = *reinterpret_cast<const uint4*>(from + (row0 + walk.row(i)) * pitch + col0 + walk.c);
+        for (int i = 0; i < walk.kSteps; ++i) {
+            old.v[i] = make_uint4(0, 0, 0, 0);
+            if (from && walk.has(i))
+                old.v[i] = *reinterpret_cast<const uint4*>(from + (row0 + walk.row(i)) * pitch + col0 + walk.c);
         }
+        return old;
+    }
+
+    template <int FN>
+    __device__ __forceinline__ void band(const gemm::v16f (&acc)[FN], char* sm, int lane, int64_t row0, int64_t col0,
+                                         int64_t rows, int64_t cols, const Old<FN>& old) const {
+        const Walk<FN> walk(lane, rows, cols);
         gemm::to_strip<FN>(acc, sm, lane);
 #pragma unroll
         for (int i = 0; i < walk.kSteps; ++i) {
@@ -254,7 +263,7 @@ struct SymmetricOut {
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] *= times;
             if (from) {
-                const gemm::v8h y = __builtin_bit_cast(gemm::v8h, old[i]);
+                const gemm::v8h y = __builtin_bit_cast(gemm::v8h, old.v[i]);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[e] = fmaf((float)y[e], add, x[e]);
             }
@@ -286,28 +295,42 @@ struct ApplyOut {
     const Found& f;
 
     template <int FN>
+    struct Old {
+        float4 v[Walk<FN>::kSteps][2];
+    };
+    // (zero past the row's end)
+    template <int FN>
+    __device__ __forceinline__ Old<FN> begin(int lane, int64_t row0, int64_t col0, int64_t rows, int64_t cols) const {
+        const Walk<FN> walk(lane, rows, cols);
+        const int64_t pitch = f.m.pitch();
+        const float* xs = reinterpret_cast<const float*>(a.ws + f.m.x_at()) + row0 * pitch + col0 + walk.c;
+        Old<FN> old;
+#pragma unroll
+        for (int i = 0; i < walk.kSteps; ++i)
+            if (walk.has(i)) {
+                old.v[i][0] = *reinterpret_cast<const float4*>(xs + walk.row(i) * pitch);
+                old.v[i][1] = *reinterpret_cast<const float4*>(xs + walk.row(i) * pitch + 4);
+            }
+        return old;
+    }
+
+    template <int FN>
     __device__ __forceinline__ void band(const gemm::v16f (&acc)[FN], char* sm, int lane, int64_t row0, int64_t col0,
-                                         int64_t rows, int64_t cols) const {
+                                         int64_t rows, int64_t cols, const Old<FN>& ahead) const {
         const Walk<FN> walk(lane, rows, cols);
         const int64_t pitch = f.m.pitch(), left = cols - walk.c, col = col0 + walk.c;
         float* xs = reinterpret_cast<float*>(a.ws + f.m.x_at()) + row0 * pitch + col;
         u16* h = reinterpret_cast<u16*>(a.ws + f.m.operand_at(a.turn ^ 1)) + row0 * pitch + col;
         float* w = a.w + f.m.offset + row0 * f.m.cols + col;
         const bool weights = a.result == kMuonWeights;
-        float4 y[Walk<FN>::kSteps][2];
-#pragma unroll
-        for (int i = 0; i < walk.kSteps; ++i)
-            if (walk.has(i)) {  // (zero past the row's end)
-                y[i][0] = *reinterpret_cast<const float4*>(xs + walk.row(i) * pitch);
-                y[i][1] = *reinterpret_cast<const float4*>(xs + walk.row(i) * pitch + 4);
-            }
         gemm::to_strip<FN>(acc, sm, lane);
         const float rate = weights ? -a.rates->lr * f.m.scale : 0.0f, decay = weights ? a.rates->decay : 0.0f;
 #pragma unroll
         for (int i = 0; i < walk.kSteps; ++i) {
             if (!walk.has(i)) continue;
             const int t = walk.row(i);
-            const float old[8] = {y[i][0].x, y[i][0].y, y[i][0].z, y[i][0].w, y[i][1].x, y[i][1].y, y[i][1].z, y[i][1].w};
+            const float old[8] = {ahead.v[i][0].x, ahead.v[i][0].y, ahead.v[i][0].z, ahead.v[i][0].w,
+                                  ahead.v[i][1].x, ahead.v[i][1].y, ahead.v[i][1].z, ahead.v[i][1].w};
             float x[8];
             gemm::read8(walk.at(sm, i), x);
 #pragma unroll

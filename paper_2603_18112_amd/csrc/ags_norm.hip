@@ -182,12 +182,11 @@ __device__ __forceinline__ void store_any(void* p, bool bf16, int64_t at, int64_
 // ---------------------------------------------------------------- forward --
 
 // G lanes to a row, NV pieces of 16 bytes each; a block of B threads has B / G
-// rows at a time, and asks for the next ones while it reduces these.  T: x's type.
-template <typename T, int G, int NV, int B>
+// rows at a time, and asks for the next ones while it reduces these.  KEEP: weight and
+// bias stay in registers, for all the block's rows.  T: x's type.
+template <typename T, int G, int NV, int B, bool KEEP>
 __global__ __launch_bounds__(B) void norm_kernel(NormArgs a) {
     constexpr int N = Piece<T>::kN;
-    // weight and bias stay in registers where these suffice
-    constexpr bool kKeep = B < 1024 || NV * N <= 16;
     __shared__ float red[2][1][16];
     const int lane = threadIdx.x % G;
     const int64_t cols = a.cols, step = (int64_t)gridDim.x * (B / G);
@@ -211,8 +210,8 @@ __global__ __launch_bounds__(B) void norm_kernel(NormArgs a) {
             if (a.bias) load_any<N>(a.bias, a.w_bf16, c, cols - c, b);
         }
     };
-    float w[kKeep ? NV : 1][N], b[kKeep ? NV : 1][N];
-    if constexpr (kKeep) {
+    float w[KEEP ? NV : 1][N], b[KEEP ? NV : 1][N];
+    if constexpr (KEEP) {
 #pragma unroll
         for (int j = 0; j < NV; ++j) affine(j, w[j], b[j]);
     }
@@ -243,8 +242,8 @@ __global__ __launch_bounds__(B) void norm_kernel(NormArgs a) {
         for (int j = 0; j < NV; ++j) {
             const int64_t c = ((int64_t)j * G + lane) * N;
             if (c >= cols) continue;
-            const int k = kKeep ? j : 0;
-            if constexpr (!kKeep) affine(j, w[0], b[0]);
+            const int k = KEEP ? j : 0;
+            if constexpr (!KEEP) affine(j, w[0], b[0]);
 #pragma unroll
             for (int i = 0; i < N; ++i) x[j][i] = fmaf(x[j][i] * rstd, w[k][i], b[k][i]);
             store_any<N>(a.y, a.y_bf16, row * a.y_stride + c, cols - c, x[j]);
@@ -534,15 +533,18 @@ template <typename T>
 hipError_t forward(const NormArgs& a, hipStream_t s) {
     const int64_t n = a.cols;
     constexpr int F = sizeof(T) / 2;
-#define NORM_FORWARD(G, NV, B, MOST)                                                                           \
-    hipLaunchKernelGGL((norm_kernel<T, G, NV * F, B>), dim3(norm_blocks(a.rows, B / G, MOST)), dim3(B), 0, s, a)
-    if (n <= 512) NORM_FORWARD(64, 1, 256, 2048);
-    else if (n <= 1024) NORM_FORWARD(64, 2, 256, 1536);
-    else if (n <= 2048) NORM_FORWARD(256, 1, 256, 2048);
-    else if (n <= 4096) NORM_FORWARD(512, 1, 512, 1024);
-    else if (n <= 8192) NORM_FORWARD(512, 2, 512, 768);
-    else if (n <= 16384) NORM_FORWARD(1024, 2, 1024, 512);
-    else if (F == 1 && n <= kNormForwardCols) NORM_FORWARD(1024, 4 / F, 1024, 256);
+#define NORM_FORWARD(G, NV, B, MOST, KEEP)                                                                 \
+    hipLaunchKernelGGL((norm_kernel<T, G, NV * F, B, KEEP>), dim3(norm_blocks(a.rows, B / G, MOST)), dim3(B), 0, s, a)
+    // one row to a wave: more waves are worth more than weights in registers (5001 x
+    // 1000 fp32 11.5 us against 15.2; 16384 x 1024 bf16 19.5 and 16.2)
+    if (n <= 512) NORM_FORWARD(64, 1, 256, 2048, true);
+    else if (n <= 1024 && a.rows <= 6144) NORM_FORWARD(64, 2, 256, 1536, false);
+    else if (n <= 1024) NORM_FORWARD(64, 2, 256, 1536, true);
+    else if (n <= 2048) NORM_FORWARD(256, 1, 256, 2048, true);
+    else if (n <= 4096) NORM_FORWARD(512, 1, 512, 1024, true);
+    else if (n <= 8192) NORM_FORWARD(512, 2, 512, 768, true);
+    else if (n <= 16384) NORM_FORWARD(1024, 2, 1024, 512, true);
+    else if (F == 1 && n <= kNormForwardCols) NORM_FORWARD(1024, 4 / F, 1024, 256, false);
     else
         hipLaunchKernelGGL((norm_long_kernel<T>), dim3(norm_blocks(a.rows, 1, 512)), dim3(kLong), 0, s, a);
 #undef NORM_FORWARD
