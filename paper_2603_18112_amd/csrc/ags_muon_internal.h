@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <functional>
 #include <vector>
 
 #include "ags_gemm_internal.h"
@@ -97,8 +98,6 @@ struct MuonProductArgs {
     int32_t out_bf16;
 };
 
-// The tile side for a launch of products: the least estimated time, of all the
-// tiles over all CUs, and of the longest.
 struct MuonProduct {
     int64_t m, n, k, count;
     bool symmetric;
@@ -109,21 +108,43 @@ inline int64_t muon_tiles(const MuonProduct& p, int t) {
     return p.symmetric ? tm * (tm + 1) / 2 : tm * tn;
 }
 
+// The tile side for a launch of products: the least estimated time, the tiles going to
+// the CUs the longest first.  Cold operands and the longer ends of these kernels
+// cost 2.5, 6 and 12 us a launch more than gemm_alone says, and long launches with
+// tiles of 128 squared half as much again: the power limit leaves them less of the clock.
+// Within 2 % of the fastest of the choices for each launch of ResNet-50's matrices,
+// VGG-16's classifier, eight 512 x 2048 and 1000 x 512; the launches by themselves, tiles of
+// 64 / 128 / 256 squared (us): VGG-16's A - / 718 / 524, its A A - / 183 / 208, its X - /
+// 1115 / 1007, eight A of 512 x 2048 16.7 / 20.7 / -.
 inline int muon_tile_side(const std::vector<MuonProduct>& v) {
     int best = 1;
     double least = 1e30;
     for (int t : {1, 2, 4}) {
         double sum = 0, longest = 0;
+        int64_t tiles = 0;
         for (const MuonProduct& p : v) {
             const double stages = (double)((p.k + 63) / 64);
-            sum += (double)muon_tiles(p, t) * (double)p.count * gemm_among(t, stages);
+            const int64_t n = muon_tiles(p, t) * p.count;
+            tiles += n;
+            sum += (double)n * gemm_among(t, stages);
             longest = std::max(longest, gemm_alone(t, stages));
         }
-        // Long launches run at the clock that the power limit leaves: 0.70 PFLOP/s with
-        // tiles of 128 squared, 1.2 with 256.
-        if (sum > 256 * 100) sum *= t == 4 ? 1.25 : t == 2 ? 1.7 : 1.5;
-        // a last round that is not full takes as long as a full one
-        const double us = std::max(sum / 256 + (t == 4 ? 0.5 : t == 2 ? 0.25 : 0.1) * longest, longest);
+        double us = sum / 256 + longest;
+        if (tiles <= 16384) {
+            std::vector<double> each, cu(256, 0.0);
+            for (const MuonProduct& p : v)
+                each.insert(each.end(), (size_t)(muon_tiles(p, t) * p.count), gemm_among(t, (double)((p.k + 63) / 64)));
+            std::sort(each.begin(), each.end(), std::greater<double>());
+            us = longest;
+            for (double d : each) {
+                std::pop_heap(cu.begin(), cu.end(), std::greater<double>());
+                cu.back() += d;
+                if (cu.back() > d) us = std::max(us, cu.back());
+                std::push_heap(cu.begin(), cu.end(), std::greater<double>());
+            }
+        }
+        if (sum > 256 * 150 && t < 4) us *= 1.5;
+        us += t == 4 ? 12 : t == 2 ? 6 : 2.5;
         if (us < least) {
             least = us;
             best = t;
