@@ -33,7 +33,9 @@
  * ags_last_error(NULL); work goes on hip_stream and the call returns without
  * waiting.  A handle's calls share its workspace and are ordered as ags.h
  * describes (a call on another stream than the last one waits for it by an
- * event, except while a stream captures a graph); one thread at a time.
+ * event, except while a stream captures a graph); one thread at a time.  Graphs
+ * that captured a handle's steps use its workspace too: their replays must not
+ * overlap one another, nor the handle's other calls.
  */
 #ifndef AGS_MUON_H
 #define AGS_MUON_H

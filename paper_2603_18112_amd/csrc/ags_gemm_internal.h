@@ -13,6 +13,9 @@ struct GemmShape {
     int32_t t, splits;
 };
 
+// A launch of blocks of 256 threads holds fewer than 2^32 threads.
+constexpr int64_t kGemmMaxBlocks = ((int64_t)1 << 24) - 1;
+
 constexpr int64_t gemm_up(int64_t x, int64_t unit) { return (x + unit - 1) / unit * unit; }
 
 // The time of a tile of 64 t squared in us, its axis `stages` stages of 64 long: by itself
@@ -38,7 +41,9 @@ inline GemmShape gemm_plan(int64_t m, int64_t n, int64_t k) {
         if (s > 1 && (all < 2 * s || m * n >= (int64_t)1 << 31)) break;
         const double stages = std::ceil(all / s);
         for (int t = 1; t <= 4; t *= 2) {
-            const double tiles = (double)((m + 64 * t - 1) / (64 * t)) * (double)((n + 64 * t - 1) / (64 * t));
+            const int64_t blocks = ((m + 64 * t - 1) / (64 * t)) * ((n + 64 * t - 1) / (64 * t));
+            if (t < 4 && blocks > kGemmMaxBlocks / s) continue;
+            const double tiles = (double)blocks;
             const double load = tiles * s / 256;  // blocks of a CU
             double us;
             if (t == 1) us = load <= 1.2 ? gemm_alone(t, stages) : gemm_among(t, stages) * std::ceil(load * 4) / 4;

@@ -628,7 +628,9 @@ unsigned blocks_for(int64_t items) { return (unsigned)std::max<int64_t>(1, std::
 
 template <typename Kernel, typename Args>
 hipError_t launch_tiles(Kernel kernel, const Args& a, int t, int na, int nb, int64_t m, int64_t n, hipStream_t s) {
-    const unsigned tm = (unsigned)((m + 64 * t - 1) / (64 * t)), tn = (unsigned)((n + 64 * t - 1) / (64 * t));
+    const int64_t tiles_m = (m + 64 * t - 1) / (64 * t), tiles_n = (n + 64 * t - 1) / (64 * t);
+    if (tiles_m * tiles_n > kGemmMaxBlocks / a.splits) return hipErrorInvalidConfiguration;
+    const unsigned tm = (unsigned)tiles_m, tn = (unsigned)tiles_n;
     const int lds = gemm::lds_bytes(t, t, na, nb);
     if (lds > 65536) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),

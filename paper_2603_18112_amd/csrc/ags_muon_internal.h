@@ -130,7 +130,10 @@ inline int muon_tile_side(const std::vector<MuonProduct>& v) {
             longest = std::max(longest, gemm_alone(t, stages));
         }
         double us = sum / 256 + longest;
-        if (tiles <= 16384) {
+        if (v.size() == 1) {
+            us = tiles <= 256 ? longest
+                              : std::max(longest, (double)((tiles + 255) / 256) * gemm_among(t, (double)((v[0].k + 63) / 64)));
+        } else if (tiles <= 16384) {
             std::vector<double> each, cu(256, 0.0);
             for (const MuonProduct& p : v)
                 each.insert(each.end(), (size_t)(muon_tiles(p, t) * p.count), gemm_among(t, (double)((p.k + 63) / 64)));

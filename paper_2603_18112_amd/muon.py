@@ -4,6 +4,7 @@ argument marshalling only; everything runs in the HIP kernels of the library.
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 
 from . import ags
@@ -129,18 +130,14 @@ def ags_muon_destroy(handle):
 # Device memory and streams come from torch; work goes on the current stream
 # (choose another with torch.cuda.stream).
 
-_schedules = {}
+_usual = functools.lru_cache(maxsize=64)(make_schedule)
 
 
 def _schedule(steps, coefficients, eps):
-    """make_schedule, made once for each set of numbers."""
-    try:
-        key = steps, coefficients, eps
-        if key not in _schedules:
-            _schedules[key] = make_schedule(steps, coefficients, eps)
-        return _schedules[key]
-    except TypeError:       # coefficients in a list
-        return make_schedule(steps, coefficients, eps)
+    """make_schedule, made once for each number of steps of the usual coefficients."""
+    if coefficients is COEFFICIENTS and type(steps) is int and type(eps) is float:
+        return _usual(steps, COEFFICIENTS, eps)
+    return make_schedule(steps, coefficients, eps)
 
 
 def _rows(x, what):
@@ -206,7 +203,8 @@ class Muon:
     a scale that is not given is :func:`spectral_scale`.  ``w`` and ``m`` are
     contiguous fp32 CUDA tensors of equal size, updated in place by
     :meth:`step`; its gradients are a contiguous [K, stride] tensor of
-    ``grad_dtype``, as for ``ags.AGS``.
+    ``grad_dtype``, as for ``ags.AGS``.  Graphs that captured a handle's steps
+    share its workspace: their replays must not overlap.
     """
 
     def __init__(self, layers, w, m, K, *, grad_dtype="f32", lr=0.02, momentum=0.95, weight_decay=0.0, nesterov=True,

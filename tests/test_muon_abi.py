@@ -80,6 +80,11 @@ def test_orthogonalize_refuses(lib):
     bad(ags.AGS_E_ARG, a8=X + 64)                                # out over x
     bad(ags.AGS_E_ARG, a12=Y)                                    # workspace over out
     bad(ags.AGS_E_ARG, a3=-1)
+    # 2^20 matrices of 20 tiles each: more threads than a launch holds
+    ws = muon.ags_muon_orthogonalize_workspace(1 << 20, 64, 1280)
+    far = 1 << 46
+    _raises(ags.AGS_E_LAYOUT, muon.ags_muon_orthogonalize, far, B, 1 << 20, 64, 1280, 81920, 1280,
+            muon.make_schedule(), 2 * far, B, 81920, 1280, 4 * far, ws)
     muon.ags_muon_orthogonalize(None, F, 0, 8, 40, 320, 40, muon.make_schedule(), None, F, 320, 40)   # nothing to do
 
 
