@@ -410,15 +410,15 @@ struct Place {
     unsigned split;
 };
 
-template <int T>
+template <int TM, int TN>
 __device__ __forceinline__ Place place(int64_t k, int splits, unsigned tm, unsigned tn) {
     const unsigned tiles = tm * tn;
     Place p;
     p.split = blockIdx.x / tiles;
     unsigned ti, tj;
     tile::tile_of_block<kBand>(blockIdx.x % tiles, tm, tn, ti, tj);
-    p.i0 = (int64_t)ti * 64 * T;
-    p.j0 = (int64_t)tj * 64 * T;
+    p.i0 = (int64_t)ti * 64 * TM;
+    p.j0 = (int64_t)tj * 64 * TN;
     const int stages = (int)((k + gemm::kDepth - 1) / gemm::kDepth);
     p.s0 = (int)((int64_t)stages * p.split / splits);
     p.s1 = (int)((int64_t)stages * (p.split + 1) / splits);
@@ -430,32 +430,32 @@ __device__ __forceinline__ float* part_of(float* partials, int splits, const Pla
     return splits > 1 ? partials + (int64_t)p.split * m * n : nullptr;
 }
 
-template <int T, int NA, int NB, int MODE, int ACT>
+template <int TM, int TN, int NA, int NB, int MODE, int ACT>
 __global__ __launch_bounds__(256, 1) void glu_product_kernel(GluArgs a, unsigned tm, unsigned tn) {
     extern __shared__ __attribute__((aligned(16))) char sm[];
     const int64_t lines = glu_lines(a.n), padded = glu_padded(a.k);
-    const Place p = place<T>(padded, a.splits, tm, tn);
-    gemm::product_tile<gemm::Bf16, T, T, NA, NB, gemm::kAcross, gemm::kAcrossPanels>(
+    const Place p = place<TM, TN>(padded, a.splits, tm, tn);
+    gemm::product_tile<gemm::Bf16, TM, TN, NA, NB, gemm::kAcross, gemm::kAcrossPanels>(
         Side{a.x, a.x_stride * 2, a.rows, 0}, Side{a.w, padded * 2, lines, 0}, p.s0, p.s1, p.i0, p.j0, a.rows, lines, sm,
         PairOut<MODE, ACT>{a, part_of(a.partials, a.splits, p, a.rows, lines)});
 }
 
-template <int T, int NA, int NB>
+template <int TM, int TN, int NA, int NB>
 __global__ __launch_bounds__(256, 1) void glu_dx_kernel(GluBackArgs a, unsigned tm, unsigned tn) {
     extern __shared__ __attribute__((aligned(16))) char sm[];
     const int64_t lines = glu_lines(a.n), padded = glu_padded(a.k), grads = glu_grads(a.n);
-    const Place p = place<T>(grads, a.splits, tm, tn);
-    gemm::product_tile<gemm::Bf16, T, T, NA, NB, gemm::kAcross, gemm::kAlongPanels>(
+    const Place p = place<TM, TN>(grads, a.splits, tm, tn);
+    gemm::product_tile<gemm::Bf16, TM, TN, NA, NB, gemm::kAcross, gemm::kAlongPanels>(
         Side{a.grads, grads * 2, a.rows, 0}, Side{a.w, padded * 2, lines, padded}, p.s0, p.s1, p.i0, p.j0, a.rows, a.k, sm,
         RowOut<false>{a, part_of(a.partials, a.splits, p, a.rows, a.k)});
 }
 
-template <int T, int NA, int NB>
+template <int TM, int TN, int NA, int NB>
 __global__ __launch_bounds__(256, 1) void glu_dw_kernel(GluBackArgs a, unsigned tm, unsigned tn) {
     extern __shared__ __attribute__((aligned(16))) char sm[];
     const int64_t lines = glu_lines(a.n), grads = glu_grads(a.n);
-    const Place p = place<T>(a.rows, a.splits, tm, tn);
-    gemm::product_tile<gemm::Bf16, T, T, NA, NB, gemm::kAlong, gemm::kAlong>(
+    const Place p = place<TM, TN>(a.rows, a.splits, tm, tn);
+    gemm::product_tile<gemm::Bf16, TM, TN, NA, NB, gemm::kAlong, gemm::kAlong>(
         Side{a.grads, grads * 2, a.rows, grads}, Side{a.x, a.x_stride * 2, a.rows, a.x_width}, p.s0, p.s1, p.i0, p.j0,
         lines, a.k, sm, RowOut<true>{a, part_of(a.partials, a.splits, p, lines, a.k)});
 }
@@ -627,11 +627,11 @@ __global__ __launch_bounds__(kFewWaves * 64) void glu_few_kernel(GluArgs a) {
 unsigned blocks_for(int64_t items) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>((items + 255) / 256, 8192)); }
 
 template <typename Kernel, typename Args>
-hipError_t launch_tiles(Kernel kernel, const Args& a, int t, int na, int nb, int64_t m, int64_t n, hipStream_t s) {
-    const int64_t tiles_m = (m + 64 * t - 1) / (64 * t), tiles_n = (n + 64 * t - 1) / (64 * t);
+hipError_t launch_tiles(Kernel kernel, const Args& a, const GemmShape& p, int na, int nb, int64_t m, int64_t n, hipStream_t s) {
+    const int64_t tiles_m = gemm_tiles(m, p.tm), tiles_n = gemm_tiles(n, p.tn);
     if (tiles_m * tiles_n > kGemmMaxBlocks / a.splits) return hipErrorInvalidConfiguration;
     const unsigned tm = (unsigned)tiles_m, tn = (unsigned)tiles_n;
-    const int lds = gemm::lds_bytes(t, t, na, nb);
+    const int lds = gemm::lds_bytes(p.tm, p.tn, na, nb);
     if (lds > 65536) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
                                                  hipFuncAttributeMaxDynamicSharedMemorySize, lds);
@@ -644,11 +644,13 @@ hipError_t launch_tiles(Kernel kernel, const Args& a, int t, int na, int nb, int
 // Four buffers where all blocks fit the CUs at once even so.
 #define GLU_LAUNCH(KERNEL, M, N, ...)                                                                     \
     [&] {                                                                                                 \
-        const int64_t tiles = (((M) + 64 * p.t - 1) / (64 * p.t)) * (((N) + 64 * p.t - 1) / (64 * p.t)) * p.splits; \
-        if (p.t == 4) return launch_tiles(KERNEL<4, 2, 3 __VA_ARGS__>, a, 4, 2, 3, M, N, s);                    \
-        if (p.t == 2) return tiles <= 256 ? launch_tiles(KERNEL<2, 4, 4 __VA_ARGS__>, a, 2, 4, 4, M, N, s)      \
-                                          : launch_tiles(KERNEL<2, 2, 2 __VA_ARGS__>, a, 2, 2, 2, M, N, s);     \
-        return launch_tiles(KERNEL<1, 4, 4 __VA_ARGS__>, a, 1, 4, 4, M, N, s);                                  \
+        const bool one = gemm_tiles(M, p.tm) * gemm_tiles(N, p.tn) * p.splits <= 256;                     \
+        if (p.tm == 4) return launch_tiles(KERNEL<4, 4, 2, 3 __VA_ARGS__>, a, p, 2, 3, M, N, s);          \
+        if (p.tn == 2) return one ? launch_tiles(KERNEL<2, 2, 4, 4 __VA_ARGS__>, a, p, 4, 4, M, N, s)     \
+                                  : launch_tiles(KERNEL<2, 2, 2, 2 __VA_ARGS__>, a, p, 2, 2, M, N, s);    \
+        if (p.tm == 2) return one ? launch_tiles(KERNEL<2, 1, 4, 4 __VA_ARGS__>, a, p, 4, 4, M, N, s)     \
+                                  : launch_tiles(KERNEL<2, 1, 3, 3 __VA_ARGS__>, a, p, 3, 3, M, N, s);    \
+        return launch_tiles(KERNEL<1, 1, 4, 4 __VA_ARGS__>, a, p, 4, 4, M, N, s);                         \
     }()
 
 }  // namespace
