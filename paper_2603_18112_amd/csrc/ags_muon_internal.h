@@ -65,6 +65,7 @@ struct MuonWork {
     int32_t each;        // without a table: of a matrix
     int32_t tiles_n;     // without a table: tiles to a row; 0: those not above the diagonal
     int32_t t;           // a tile's side is 64 t
+    int32_t stages;      // the shortest contracted axis, in stages of 64
 };
 
 struct MuonRates {
