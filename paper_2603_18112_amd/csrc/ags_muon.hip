@@ -42,6 +42,7 @@ __device__ __forceinline__ void store_half8(u16* p, int64_t left, const float* x
     *reinterpret_cast<uint4*>(p) =
         make_uint4(pack_half(y[0], y[1]), pack_half(y[2], y[3]), pack_half(y[4], y[5]), pack_half(y[6], y[7]));
 }
+
 // The matrix of this block and its number in it (i, j: its tile; i: its chunk).
 // Blocks of one matrix go to one XCD as far as that balances: blocks b, b + 8,
 // ... share one.

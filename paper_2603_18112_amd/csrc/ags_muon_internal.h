@@ -115,8 +115,9 @@ inline int64_t muon_tiles(const MuonProduct& p, int t) {
 // tiles of 128 squared half as much again: the power limit leaves them less of the clock.
 // Within 2 % of the fastest of the choices for each launch of ResNet-50's matrices,
 // VGG-16's classifier, eight 512 x 2048 and 1000 x 512; the launches by themselves, tiles of
-// 64 / 128 / 256 squared (us): VGG-16's A - / 718 / 524, its A A - / 183 / 208, its X - /
-// 1115 / 1007, eight A of 512 x 2048 16.7 / 20.7 / -.
+// 64 / 128 / 256 squared (us): VGG-16's A - / 718 / 524, its A A - / 163 / 208, its X - /
+// 1115 / 1007, eight A of 512 x 2048 16.7 / 20.7 / -.  Tiles of 128 x 64 gained nothing: those
+// eight 16.6, ResNet-50's A 43 against 39.
 inline int muon_tile_side(const std::vector<MuonProduct>& v) {
     int best = 1;
     double least = 1e30;
