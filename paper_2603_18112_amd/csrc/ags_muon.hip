@@ -5,6 +5,7 @@
 // muon_gram_kernel    A = X X' (or X' X)
 // muon_square_kernel  b A + c A A
 // muon_apply_kernel   X <- a X + (b A + c A A) X; the last one updates the weights
+// muon_thin_gram_kernel, muon_thin_apply_kernel   both for thin matrices, all steps in one
 //
 // Every launch covers all matrices: a block finds its tile in a table, or from
 // its number where all matrices are alike.
@@ -412,6 +413,139 @@ __global__ __launch_bounds__(256, 1) void muon_apply_kernel(MuonProductArgs a) {
                                                               out);
 }
 
+// ------------------------------------------------------------------ thin --
+
+// A thin matrix as `n` columns of its shorter side, from c0 of the longer on, in LDS.
+constexpr int kThin = kMuonThin, kThinCols = kMuonThinCols;
+struct ThinTile {
+    float v[kThin][kThinCols + 1];
+};
+
+// Calls f(i, c) for every element i of the shorter side and c of n of the longer,
+// neighbours in memory by neighbouring threads.
+template <typename F>
+__device__ __forceinline__ void thin_each(bool tall, int s, int n, F&& f) {
+    for (int t = threadIdx.x; t < s * n; t += kThreads) {
+        if (tall) f(t % s, t / s);
+        else f(t / n, t % n);
+    }
+}
+
+__device__ __forceinline__ void thin_load(const MuonStepArgs& a, const Found& f, int64_t c0, int n, ThinTile& x) {
+    const bool tall = f.m.tall();
+    thin_each(tall, (int)f.m.side(), n, [&](int i, int c) {
+        const int64_t row = tall ? c0 + c : i, col = tall ? i : c0 + c;
+        float v;
+        if (!a.from_x) {
+            v = reinterpret_cast<const float*>(a.ws + f.m.x_at())[row * f.m.pitch() + col];
+        } else {
+            const int64_t at = f.index * a.batch_stride + row * a.row_stride + col;
+            v = a.bf16 ? gemm::bf16_value(static_cast<const u16*>(a.grads)[at]) : static_cast<const float*>(a.grads)[at];
+        }
+        x.v[i][c] = v;
+    });
+}
+
+// U U' (U' U) over a part of the longer side: a thread has one sum, whose products are
+// exact in fp64.
+__global__ __launch_bounds__(kThreads) void muon_thin_gram_kernel(MuonThinArgs a) {
+    __shared__ ThinTile x;
+    const Found f = find<false>(a.in.work);
+    const int s = (int)f.m.side(), i = threadIdx.x / kThin, j = threadIdx.x % kThin;
+    const int64_t from = (int64_t)f.i * f.m.part, end = min(f.m.length(), from + f.m.part);
+    double sum = 0.0;
+    for (int64_t c0 = from; c0 < end; c0 += kThinCols) {
+        const int n = (int)min(end - c0, (int64_t)kThinCols);
+        __syncthreads();
+        thin_load(a.in, f, c0, n, x);
+        __syncthreads();
+        if (i < s && j < s)
+#pragma unroll 4
+            for (int c = 0; c < n; ++c) sum = fma((double)x.v[i][c], (double)x.v[j][c], sum);
+    }
+    reinterpret_cast<double*>(a.in.ws + f.m.parts_at())[(int64_t)f.i * kThreads + threadIdx.x] = sum;
+}
+
+struct ThinSquare {
+    double v[kThin][kThin + 1];
+};
+
+__device__ __forceinline__ double thin_product(const ThinSquare& a, const ThinSquare& b, int i, int j) {
+    double sum = 0.0;
+#pragma unroll
+    for (int k = 0; k < kThin; ++k) sum = fma(a.v[i][k], b.v[k][j], sum);
+    return sum;
+}
+
+// The steps on A alone (p = a + b A + c A A: A <- p A p, Q <- p Q; the matrices are
+// polynomials of one symmetric one and commute), by every block anew, then its part of
+// Q U.  Both launches together, in graphs (us; as the products above): 1 x 4096 17 (123), 16 x
+// 4096 26 (124), 16 x 100 000 78 (1914), 24 of 16 x 8192 64 (286).  Bound by the waits of
+// either launch and by fp64 in order; memory takes 3 us of the longest.
+__global__ __launch_bounds__(kThreads) void muon_thin_apply_kernel(MuonThinArgs a) {
+    __shared__ ThinTile x;
+    __shared__ ThinSquare A, Q, P;
+    __shared__ float q[kThin][kThin];
+    const Found f = find<false>(a.in.work);
+    const int s = (int)f.m.side(), i = threadIdx.x / kThin, j = threadIdx.x % kThin;
+    const double* parts = reinterpret_cast<const double*>(a.in.ws + f.m.parts_at());
+    double sum = 0.0;
+#pragma unroll 8
+    for (int k = 0; k < f.m.parts; ++k) sum += parts[(int64_t)k * kThreads + threadIdx.x];
+    A.v[i][j] = sum;
+    __syncthreads();
+    double trace = 0.0;
+    for (int k = 0; k < s; ++k) trace += A.v[k][k];
+    // a zero matrix stays zero with eps = 0 too
+    const double inv = trace == 0.0 ? 0.0 : 1.0 / (sqrt(trace) + a.in.eps);
+    __syncthreads();
+    A.v[i][j] = sum * inv * inv;
+    Q.v[i][j] = i == j ? inv : 0.0;
+    __syncthreads();
+    for (int t = 0; t < a.steps; ++t) {
+        const double p = fma(a.abc[3 * t + 2], thin_product(A, A, i, j),
+                             fma(a.abc[3 * t + 1], A.v[i][j], i == j ? a.abc[3 * t] : 0.0));
+        P.v[i][j] = p;
+        __syncthreads();
+        const double pq = thin_product(P, Q, i, j), pa = thin_product(P, A, i, j);
+        __syncthreads();
+        Q.v[i][j] = pq;
+        A.v[i][j] = pa;
+        __syncthreads();
+        const double pap = thin_product(A, P, i, j);
+        __syncthreads();
+        A.v[i][j] = pap;
+        __syncthreads();
+    }
+    // Q holds the division by the norm, which may lie outside fp32's range: a power of two of it
+    // goes to U's elements.
+    const int e = inv > 0.0 && inv < HUGE_VAL ? ilogb(inv) : 0;
+    q[i][j] = (float)ldexp(Q.v[i][j], -e);
+    const MuonProductArgs& o = a.out;
+    const bool tall = f.m.tall(), weights = o.result == kMuonWeights;
+    const float rate = weights ? -o.rates->lr * f.m.scale : 0.0f, decay = weights ? o.rates->decay : 0.0f;
+    const int64_t from = (int64_t)f.i * f.m.part, end = min(f.m.length(), from + f.m.part);
+    for (int64_t c0 = from; c0 < end; c0 += kThinCols) {
+        const int n = (int)min(end - c0, (int64_t)kThinCols);
+        __syncthreads();
+        thin_load(a.in, f, c0, n, x);
+        __syncthreads();
+        thin_each(tall, s, n, [&](int r, int c) {
+            float y = 0.0f;
+            for (int k = 0; k < s; ++k) y = fmaf(q[r][k], ldexpf(x.v[k][c], e), y);
+            const int64_t row = tall ? c0 + c : r, col = tall ? r : c0 + c;
+            if (weights) {
+                float* w = o.w + f.m.offset + row * f.m.cols + col;
+                *w = fmaf(rate, y, *w * decay);
+            } else {
+                const int64_t at = f.index * o.out_batch_stride + row * o.out_stride + col;
+                if (o.out_bf16) static_cast<u16*>(o.out)[at] = (u16)gemm::pack_bf16(y, 0.0f);
+                else static_cast<float*>(o.out)[at] = y;
+            }
+        });
+    }
+}
+
 // The learning rate in force, written by one lane, as that of the AGS step.
 __global__ __launch_bounds__(64) void muon_rates_kernel(MuonRates* p, MuonRates r) {
     if (threadIdx.x == 0) *p = r;
@@ -444,11 +578,19 @@ hipError_t launch_tiles(Kernel kernel, int t, int na, int nb, const MuonProductA
      : a.work.stages >= 8   ? launch_tiles(KERNEL<2, 2, 3>, 2, 2, 3, a, s)                        \
                             : launch_tiles(KERNEL<2, 2, 2>, 2, 2, 2, a, s))
 
-hipError_t launch_muon_start(const MuonStepArgs& a, hipStream_t s) {
+hipError_t launch_muon_sum(const MuonStepArgs& a, hipStream_t s) {
     hipLaunchKernelGGL(muon_sum_kernel, dim3((unsigned)a.work.blocks), dim3(kThreads), 0, s, a);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+    return hipGetLastError();
+}
+hipError_t launch_muon_start(const MuonStepArgs& a, hipStream_t s) {
     hipLaunchKernelGGL(muon_start_kernel, dim3((unsigned)a.work.blocks), dim3(kThreads), 0, s, a);
+    return hipGetLastError();
+}
+hipError_t launch_muon_thin(const MuonThinArgs& a, hipStream_t s) {
+    hipLaunchKernelGGL(muon_thin_gram_kernel, dim3((unsigned)a.in.work.blocks), dim3(kThreads), 0, s, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(muon_thin_apply_kernel, dim3((unsigned)a.in.work.blocks), dim3(kThreads), 0, s, a);
     return hipGetLastError();
 }
 hipError_t launch_muon_gram(const MuonProductArgs& a, hipStream_t s) { return MUON_LAUNCH(muon_gram_kernel); }

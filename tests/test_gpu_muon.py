@@ -71,6 +71,36 @@ def test_random_matrices(rows, cols, kind):
     _near(muon.orthogonalize(ub.cuda()), want, off)
 
 
+@pytest.mark.parametrize("side", [1, 2, 3, 7, 16])
+@pytest.mark.parametrize("length", [1, 16, 100, 513, 3000, 140000])
+@pytest.mark.parametrize("tall", [False, True])
+def test_thin_matrices(side, length, tall):
+    """One side of up to 16: X = Q U / |U| with Q rounded to fp32 and sums of `side`
+    products, (side + 2) 2^-24 of the sum of magnitudes."""
+    u = _random(min(side, length), max(side, length), "full", 4)
+    if side == 3:                    # one singular value
+        u = u[:, :1] @ u[:1]
+    x = u.t().contiguous() if tall else u
+    norm = u.double().norm() + 1e-7
+    a, q = u.double() @ u.double().t() / norm ** 2, torch.eye(u.shape[0], dtype=torch.float64)
+    for _ in range(5):
+        p = ref.DEFAULT[0] * torch.eye(u.shape[0], dtype=torch.float64) + ref.DEFAULT[1] * a + ref.DEFAULT[2] * a @ a
+        a, q = p @ a @ p, p @ q
+    want, tol = q @ u.double() / norm, (u.shape[0] + 2) * 2.0 ** -24 * 1.001 * (q.abs() @ u.double().abs() / norm)
+    got = muon.orthogonalize(x.cuda(), dtype="f32").cpu()
+    assert (((got.t() if tall else got).double() - want).abs() <= tol + 1e-12 * want.abs()).all()
+    # and as the step of a matrix among others
+    o = -(-x.numel() // 8) * 8
+    other = _random(70, 90, "full", 5)
+    w, m = (torch.zeros(o + 6304).cuda() for _ in range(2))
+    grads = torch.zeros(1, o + 6304)
+    grads[0, :x.numel()], grads[0, o:o + 6300] = x.reshape(-1), other.reshape(-1)
+    opt = muon.Muon([(0, *x.shape, 1.0), (o, 70, 90, 1.0)], w, m, 1, lr=1.0, momentum=0.0, nesterov=False)
+    opt.step(grads.cuda())
+    assert torch.equal(-w[:x.numel()].cpu().view(x.shape), got)
+    assert torch.equal(-w[o:o + 6300].view(70, 90), muon.orthogonalize(other.cuda(), dtype="f32"))
+
+
 @pytest.mark.parametrize("steps,coefficients", [(1, ref.DEFAULT), (2, DYADIC), (12, (1.5, -0.5, 0.0)),
                                                 (3, ((3.4445, -4.775, 2.0315), (2.0, -1.5, 0.5), (1.5, -0.5, 0.0)))])
 def test_other_schedules(steps, coefficients):
