@@ -23,9 +23,11 @@
  * rounded to fp16, scaled by powers of two, with fp32 sums: X carries no
  * rounding from step to step, whose error the steps would multiply by up to
  * a each; the result is off by 0.03 to 0.3 % of its norm whatever the singular
- * values (in bf16 throughout: up to 40 %).  With a side of up to 16 the steps run
- * in 64 bits on U U' alone, and X = Q U in fp32.  Sums are added in an order
- * that the sizes alone fix: equal inputs give equal results bit for bit.
+ * values (in bf16 throughout: up to 40 %), up to 1 % where all but a few rows or
+ * columns are zero, as the roundings of few numbers do not average out.  With a
+ * side of up to 16 the steps run in 64 bits on U U' alone, and X = Q U in fp32.
+ * Sums are added in an order that the sizes alone fix: equal inputs give equal
+ * results bit for bit.
  * A NaN or an infinity makes its matrix NaN, no other; a zero matrix stays zero.
  *
  * Conventions as in ags.h: C linkage, ags_status results, arguments checked
