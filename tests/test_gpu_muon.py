@@ -151,6 +151,20 @@ def test_scales_zeros_and_nonfinite_values():
     assert torch.equal(muon.orthogonalize(x, eps=0.0, dtype="f32")[0], base)
 
 
+@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 300), (300, 3), (16, 20)])
+def test_scales_zeros_and_nonfinite_values_of_thin_matrices(rows, cols):
+    u = _random(rows, cols, "full", 6)
+    base = muon.orthogonalize(u.cuda(), eps=0.0, dtype="f32")
+    for p in (-100, 90):
+        assert torch.equal(muon.orthogonalize((u.double() * 2.0 ** p).float().cuda(), eps=0.0, dtype="f32"), base)
+    x = torch.stack([u, torch.zeros_like(u), u, u]).cuda()
+    x[2, 0, 0], x[3, -1, -1] = float("nan"), float("inf")
+    for eps in (0.0, 1e-7):
+        got = muon.orthogonalize(x, eps=eps, dtype="f32")
+        assert torch.isfinite(got[0]).all() and (got[1] == 0).all() and torch.isnan(got[2]).all() and torch.isnan(got[3]).all()
+    assert torch.equal(muon.orthogonalize(x, eps=0.0, dtype="f32")[0], base)
+
+
 def test_empty():
     for shape in ((0, 4), (4, 0), (0, 3, 3), (2, 0, 3)):
         assert muon.orthogonalize(torch.empty(shape).cuda()).shape == shape
