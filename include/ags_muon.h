@@ -22,10 +22,17 @@
  * X is held in fp32, norms are summed in fp64.  The products' operands are
  * rounded to fp16, scaled by powers of two, with fp32 sums: X carries no
  * rounding from step to step, whose error the steps would multiply by up to
- * a each; the result is off by 0.03 to 0.3 % of its norm whatever the singular
- * values (in bf16 throughout: up to 40 %), up to 1 % where all but a few rows or
- * columns are zero, as the roundings of few numbers do not average out.  With a
- * side of up to 16 the steps run in 64 bits on U U' alone, and X = Q U in fp32.
+ * a each; after five of the usual steps the result is off by 0.03 to 0.3 % of its
+ * norm whatever the singular values (in bf16 throughout: up to 40 %), up to 1 %
+ * where all but a few rows or columns are zero, as the roundings of few numbers do
+ * not average out; after more, by up to 2 %.  Singular values that are zero take part
+ * as those roundings: they stay below 1 % through eight of the usual steps, and from
+ * about twelve on come out like any others.
+ *
+ * With a side of up to 16 the steps run in 64 bits on U U' alone, X = Q U is rounded to
+ * fp32 once, and singular values that are zero stay zero.  Where the steps multiply
+ * small ones by more than 2^18 in all (eleven usual steps), those below 2^-23 of |U|
+ * count as zero.
  * Sums are added in an order that the sizes alone fix: equal inputs give equal
  * results bit for bit.
  * A NaN or an infinity makes its matrix NaN, no other; a zero matrix stays zero.

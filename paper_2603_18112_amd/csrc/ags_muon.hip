@@ -5,7 +5,8 @@
 // muon_gram_kernel    A = X X' (or X' X)
 // muon_square_kernel  b A + c A A
 // muon_apply_kernel   X <- a X + (b A + c A A) X; the last one updates the weights
-// muon_thin_gram_kernel, muon_thin_apply_kernel   both for thin matrices, all steps in one
+// muon_thin_gram_kernel, muon_thin_apply_kernel   both for thin matrices, all steps in one;
+//                     muon_thin_eigen_kernel   between them for long schedules
 //
 // Every launch covers all matrices: a block finds its tile in a table, or from
 // its number where all matrices are alike.
@@ -477,50 +478,153 @@ __device__ __forceinline__ double thin_product(const ThinSquare& a, const ThinSq
     return sum;
 }
 
-// The steps on A alone (p = a + b A + c A A: A <- p A p, Q <- p Q; the matrices are
-// polynomials of one symmetric one and commute), by every block anew, then its part of
-// Q U.  Both launches together, in graphs (us; as the products above): 1 x 4096 17 (123), 16 x
-// 4096 26 (124), 16 x 100 000 78 (1914), 24 of 16 x 8192 64 (286).  Bound by the waits of
-// either launch and by fp64 in order; memory takes 3 us of the longest.
-__global__ __launch_bounds__(kThreads) void muon_thin_apply_kernel(MuonThinArgs a) {
-    __shared__ ThinTile x;
-    __shared__ ThinSquare A, Q, P;
-    __shared__ float q[kThin][kThin];
-    const Found f = find<false>(a.in.work);
-    const int s = (int)f.m.side(), i = threadIdx.x / kThin, j = threadIdx.x % kThin;
-    const double* parts = reinterpret_cast<const double*>(a.in.ws + f.m.parts_at());
+// Index i's partner in a round among m (even): every pair meets once in m - 1 rounds; an
+// index past m is by itself.
+__device__ __forceinline__ int thin_partner(int i, int round, int m) {
+    const int n = m - 1;
+    int p = 2 * round - i;
+    p = p < 0 ? p + n : p >= n ? p - n : p;
+    p = i == round ? n : p;
+    p = i == n ? round : p;
+    return i >= m ? i : p;
+}
+// Row i of the rotation that takes A's element (i, p) away: *self for i, the result for p.
+// The angle is within 2^-22, the rotation's rows of length 1 in fp64.
+__device__ __forceinline__ double thin_rotation(const ThinSquare& A, int i, int p, double* self) {
+    const int lo = min(i, p), hi = max(i, p);
+    const float off = (float)A.v[lo][hi];
+    const bool none = i == p || fabsf(off) < 0x1p-100f;  // (no branch: two of these go on at once)
+    const float d = (float)(A.v[hi][hi] - A.v[lo][lo]) * 0.5f * __builtin_amdgcn_rcpf(off), l = fabsf(d);
+    const float root = l > 1e9f ? l : __builtin_amdgcn_sqrtf(fmaf(d, d, 1.0f));
+    const double t = (double)copysignf(__builtin_amdgcn_rcpf(l + root), d);
+    const double r = fma(t, t, 1.0);
+    double c = (double)__builtin_amdgcn_rsqf((float)r);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) c *= fma(-0.5 * r, c * c, 1.5);
+    *self = none ? 1.0 : c;
+    return none ? 0.0 : i == lo ? -t * c : t * c;
+}
+
+// Eigenvalues (the diagonal of A) and eigenvectors (columns of V) of A[0], of trace 1, by
+// Jacobi's rotations, eight pairs at a time; returns which of the two buffers holds them.
+// Off-diagonal elements vanish quadratically, in 4 to 8 sweeps in simulations of
+// full, graded and repeated spectra; those below 2^-30 are cleared outright, what is left of them
+// would be below 2^-52.  Elements between indices of no weight (below) do not matter.
+__device__ __forceinline__ int thin_eigen(ThinSquare (&A)[2], ThinSquare (&V)[2], int s, int i, int j) {
+    constexpr int kSweeps = 16;
+    const int m = (s + 1) & ~1;
+    int at = 0;
+    V[0].v[i][j] = i == j ? 1.0 : 0.0;
+    __syncthreads();
+    for (int sweep = 0; sweep < kSweeps; ++sweep) {
+        const bool left = i != j && fabs(A[at].v[i][j]) > 0x1p-80 && fmax(A[at].v[i][i], A[at].v[j][j]) > 0x1p-50;
+        if (!__syncthreads_or(left)) break;
+        for (int round = 0; round < m - 1; ++round, at ^= 1) {
+            const ThinSquare &X = A[at], &W = V[at];
+            const int p = thin_partner(i, round, m), q = thin_partner(j, round, m);
+            double ci, cj;
+            const double si = thin_rotation(X, i, p, &ci), sj = thin_rotation(X, j, q, &cj);
+            const double u = fma(sj, X.v[i][q], cj * X.v[i][j]), v = fma(sj, X.v[p][q], cj * X.v[p][j]);
+            const bool clear = i != j && p == j && fabs(X.v[min(i, j)][max(i, j)]) < 0x1p-30;
+            const double a = fma(si, v, ci * u), w = fma(sj, W.v[i][q], cj * W.v[i][j]);
+            A[at ^ 1].v[i][j] = clear ? 0.0 : a;
+            V[at ^ 1].v[i][j] = w;
+            __syncthreads();
+        }
+    }
+    return at;
+}
+
+// A of a matrix, summed over its parts, its trace, and one over the norm.
+__device__ __forceinline__ double thin_gram(const MuonStepArgs& a, const Found& f, ThinSquare& A, double* trace,
+                                            double* inv) {
+    const double* parts = reinterpret_cast<const double*>(a.ws + f.m.parts_at());
     double sum = 0.0;
 #pragma unroll 8
     for (int k = 0; k < f.m.parts; ++k) sum += parts[(int64_t)k * kThreads + threadIdx.x];
-    A.v[i][j] = sum;
+    A.v[threadIdx.x / kThin][threadIdx.x % kThin] = sum;
     __syncthreads();
-    double trace = 0.0;
-    for (int k = 0; k < s; ++k) trace += A.v[k][k];
+    *trace = 0.0;
+    for (int k = 0; k < (int)f.m.side(); ++k) *trace += A.v[k][k];
     // a zero matrix stays zero with eps = 0 too
-    const double inv = trace == 0.0 ? 0.0 : 1.0 / (sqrt(trace) + a.in.eps);
+    *inv = *trace == 0.0 ? 0.0 : 1.0 / (sqrt(*trace) + a.eps);
     __syncthreads();
-    A.v[i][j] = sum * inv * inv;
-    Q.v[i][j] = i == j ? inv : 0.0;
-    __syncthreads();
-    for (int t = 0; t < a.steps; ++t) {
-        const double p = fma(a.abc[3 * t + 2], thin_product(A, A, i, j),
-                             fma(a.abc[3 * t + 1], A.v[i][j], i == j ? a.abc[3 * t] : 0.0));
-        P.v[i][j] = p;
-        __syncthreads();
-        const double pq = thin_product(P, Q, i, j), pa = thin_product(P, A, i, j);
-        __syncthreads();
-        Q.v[i][j] = pq;
-        A.v[i][j] = pa;
-        __syncthreads();
-        const double pap = thin_product(A, P, i, j);
-        __syncthreads();
-        A.v[i][j] = pap;
-        __syncthreads();
+    return sum;
+}
+
+// X = Q U, Q U in fp64, in one of two ways, by how much the steps multiply a singular value near zero
+// in all (kThinStepsGain): that is what they do to roundings in directions that U does not have.
+//
+// kThinSteps: by steps on A alone (p = a + b A + c A A: A <- p A p, Q <- p Q; the matrices are
+// polynomials of one symmetric one and commute).  A's own roundings, 2^-53 of its trace, grow by p^2
+// a step, and where they reach 1 the steps break off: by up to 2^36 here (ten usual steps).
+// kThinEigen: by eigenvalues of A (muon_thin_eigen_kernel, a block to a matrix), each put through the
+// steps by itself: Q has f(s) / s for the singular value s.  Those below 2^-46 of their sum,
+// which A's own roundings reach (sums of up to 2^20 products), count as none: singular values
+// under 2^-23 of |U|.
+//
+// In graphs (us), 5 / 10 / 11 / 32 usual steps, the last two by eigenvalues: 1 x 4096 17 / 23 / 14 /
+// 15, 16 x 4096 26 / 32 / 93 / 95, 16 x 100 000 77 / 83 / 143 / 144, 24 of 16 x 8192 65 / 86 / 139 / 141
+// (as the products above, five steps take 123, 124, 1914 and 286).  Bound by the waits of each
+// launch and by fp64 in order; memory takes 3 us of the longest.  A round of rotations takes
+// 0.65 us, a chain of LDS reads and some forty operations.
+__global__ __launch_bounds__(kThreads) void muon_thin_eigen_kernel(MuonThinArgs a) {
+    __shared__ ThinSquare A[2], V[2];
+    const Found f = find<false>(a.in.work);
+    if (f.i != 0) return;
+    const int i = threadIdx.x / kThin, j = threadIdx.x % kThin;
+    double trace, inv;
+    const double sum = thin_gram(a.in, f, A[0], &trace, &inv);
+    A[0].v[i][j] = trace > 0.0 ? sum / trace : 0.0;
+    const int at = thin_eigen(A, V, (int)f.m.side(), i, j);
+    // (a NaN or an infinity of U makes the trace one, and is not compared away)
+    double q = trace < HUGE_VAL ? 0.0 : __builtin_nan("");
+    if (A[at].v[j][j] > 0x1p-46) {
+        double y = A[at].v[j][j] * trace * inv * inv;
+        q = inv;
+        for (int t = 0; t < a.steps; ++t) {
+            const double p = fma(fma(a.abc[3 * t + 2], y, a.abc[3 * t + 1]), y, a.abc[3 * t]);
+            q *= p;
+            y *= p * p;
+        }
     }
-    // Q holds the division by the norm, which may lie outside fp32's range: a power of two of it
-    // goes to U's elements.
-    const int e = inv > 0.0 && inv < HUGE_VAL ? ilogb(inv) : 0;
-    q[i][j] = (float)ldexp(Q.v[i][j], -e);
+    A[at ^ 1].v[j][i] = V[at].v[i][j] * q;
+    __syncthreads();
+    // (in place of the first part, which no block reads any more)
+    reinterpret_cast<double*>(a.in.ws + f.m.parts_at())[threadIdx.x] = thin_product(V[at], A[at ^ 1], i, j);
+}
+
+// The steps by every block anew, or what the eigenvalues' kernel left, then its part of Q U.
+template <int WAY>
+__global__ __launch_bounds__(kThreads) void muon_thin_apply_kernel(MuonThinArgs a) {
+    __shared__ ThinTile x;
+    __shared__ ThinSquare A, Q, P;
+    const Found f = find<false>(a.in.work);
+    const int s = (int)f.m.side(), i = threadIdx.x / kThin, j = threadIdx.x % kThin;
+    if constexpr (WAY == kThinSteps) {
+        double trace, inv;
+        const double sum = thin_gram(a.in, f, A, &trace, &inv);
+        A.v[i][j] = sum * inv * inv;
+        Q.v[i][j] = i == j ? inv : 0.0;
+        __syncthreads();
+        for (int t = 0; t < a.steps; ++t) {
+            const double p = fma(a.abc[3 * t + 2], thin_product(A, A, i, j),
+                                 fma(a.abc[3 * t + 1], A.v[i][j], i == j ? a.abc[3 * t] : 0.0));
+            P.v[i][j] = p;
+            __syncthreads();
+            const double pq = thin_product(P, Q, i, j), pa = thin_product(P, A, i, j);
+            __syncthreads();
+            Q.v[i][j] = pq;
+            A.v[i][j] = pa;
+            __syncthreads();
+            const double pap = thin_product(A, P, i, j);
+            __syncthreads();
+            A.v[i][j] = pap;
+            __syncthreads();
+        }
+    } else {
+        Q.v[i][j] = reinterpret_cast<const double*>(a.in.ws + f.m.parts_at())[threadIdx.x];
+    }
     const MuonProductArgs& o = a.out;
     const bool tall = f.m.tall(), weights = o.result == kMuonWeights;
     const float rate = weights ? -o.rates->lr * f.m.scale : 0.0f, decay = weights ? o.rates->decay : 0.0f;
@@ -531,8 +635,9 @@ __global__ __launch_bounds__(kThreads) void muon_thin_apply_kernel(MuonThinArgs 
         thin_load(a.in, f, c0, n, x);
         __syncthreads();
         thin_each(tall, s, n, [&](int r, int c) {
-            float y = 0.0f;
-            for (int k = 0; k < s; ++k) y = fmaf(q[r][k], ldexpf(x.v[k][c], e), y);
+            double v = 0.0;
+            for (int k = 0; k < s; ++k) v = fma(Q.v[r][k], (double)x.v[k][c], v);
+            const float y = (float)v;
             const int64_t row = tall ? c0 + c : r, col = tall ? r : c0 + c;
             if (weights) {
                 float* w = o.w + f.m.offset + row * f.m.cols + col;
@@ -587,10 +692,16 @@ hipError_t launch_muon_start(const MuonStepArgs& a, hipStream_t s) {
     return hipGetLastError();
 }
 hipError_t launch_muon_thin(const MuonThinArgs& a, hipStream_t s) {
-    hipLaunchKernelGGL(muon_thin_gram_kernel, dim3((unsigned)a.in.work.blocks), dim3(kThreads), 0, s, a);
-    const hipError_t e = hipGetLastError();
+    const dim3 grid((unsigned)a.in.work.blocks), block(kThreads);
+    hipLaunchKernelGGL(muon_thin_gram_kernel, grid, block, 0, s, a);
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess && a.way == kThinEigen) {
+        hipLaunchKernelGGL(muon_thin_eigen_kernel, grid, block, 0, s, a);
+        e = hipGetLastError();
+    }
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(muon_thin_apply_kernel, dim3((unsigned)a.in.work.blocks), dim3(kThreads), 0, s, a);
+    if (a.way == kThinSteps) hipLaunchKernelGGL(muon_thin_apply_kernel<kThinSteps>, grid, block, 0, s, a);
+    else hipLaunchKernelGGL(muon_thin_apply_kernel<kThinEigen>, grid, block, 0, s, a);
     return hipGetLastError();
 }
 hipError_t launch_muon_gram(const MuonProductArgs& a, hipStream_t s) { return MUON_LAUNCH(muon_gram_kernel); }

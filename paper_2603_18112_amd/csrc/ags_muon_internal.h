@@ -21,6 +21,13 @@ namespace ags {
 constexpr int32_t kMuonThin = 16;
 // Elements of the longer side that a block takes at once, of at most 256 blocks.
 constexpr int32_t kMuonThinCols = 128;
+// How their Q is made: by steps on U U' or by its eigenvalues; by how much the steps may multiply a
+// singular value in all for the first (ags_muon.hip).
+enum MuonThinWay : int32_t { kThinSteps = 0, kThinEigen = 1 };
+constexpr double kThinStepsGain = 262144.0;
+inline MuonThinWay muon_thin_way(double gain) {
+    return gain <= kThinStepsGain ? kThinSteps : kThinEigen;
+}
 
 // What stands in a matrix's part of the workspace: X in fp32 (before the first
 // step: what is to be orthogonalised), X as operands (two, read and written in
@@ -120,6 +127,7 @@ struct MuonThinArgs {
     MuonStepArgs in;     // (its work: a block for each part)
     MuonProductArgs out;
     int32_t steps;
+    int32_t way;         // a MuonThinWay
     double abc[3 * AGS_MUON_MAX_STEPS];
 };
 
