@@ -15,9 +15,12 @@
  *   dweight = sum over the rows of dy z,  dbias = sum over the rows of dy
  *
  * Everything is computed in fp32 (the variance from the differences, not
- * from the squares) and rounded once, where it is stored.  Sums are added in
- * an order that the sizes alone fix: equal inputs give equal results bit for
- * bit.  A row that holds a NaN or an infinity has NaN in its whole y and dx, and
+ * from the squares) and rounded once, where it is stored; but the mean is held in
+ * 48 bits, so that a row far from zero loses nothing of its differences.  It is
+ * saved in fp32, and the backward pass takes it as saved: its z is off by up to
+ * 2^-24 |mean| rstd.  Where squared differences leave fp32's range they are scaled.
+ * Sums are added in an order that the sizes alone fix: equal inputs give equal
+ * results bit for bit.  A row that holds a NaN or an infinity has NaN in its whole y and dx, and
  * in what dweight sums; other rows' y and dx are untouched.  Constant rows
  * have z = 0 as long as eps > 0 (with eps = 0 they divide by zero).
  *

@@ -89,11 +89,29 @@ __device__ __forceinline__ float wave_sum(float v) {
     return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 63));
 }
 
+// The same in fp64, by halves.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double plus(double v) {
+    const int2 u = __builtin_bit_cast(int2, v);
+    return v + __builtin_bit_cast(double, make_int2(__builtin_amdgcn_update_dpp(0, u.x, CTRL, ROWS, 0xf, false),
+                                                    __builtin_amdgcn_update_dpp(0, u.y, CTRL, ROWS, 0xf, false)));
+}
+__device__ __forceinline__ double wave_sum(double v) {
+    v = plus<0x111, 0xf>(v);
+    v = plus<0x112, 0xf>(v);
+    v = plus<0x114, 0xf>(v);
+    v = plus<0x118, 0xf>(v);
+    v = plus<0x142, 0xa>(v);
+    v = plus<0x143, 0xc>(v);
+    const int2 u = __builtin_bit_cast(int2, v);
+    return __builtin_bit_cast(double, make_int2(__builtin_amdgcn_readlane(u.x, 63), __builtin_amdgcn_readlane(u.y, 63)));
+}
+
 // Sums of N values over the G lanes of a row, in every lane.  Over a block they
-// meet in LDS, in slot 0 or 1 in turn: one barrier a sum, since the next sum's
-// barrier lies between two uses of a slot.
-template <int G, int N>
-__device__ __forceinline__ void row_sum(float (&v)[N], float (*red)[N][16], int slot) {
+// meet in LDS, in two slots (or arrays) in turn: one barrier a sum, since the next
+// sum's barrier lies between two uses of a slot.
+template <int G, typename S, int N>
+__device__ __forceinline__ void row_sum(S (&v)[N], S (*red)[N][16], int slot) {
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
     if constexpr (G > 64) {
@@ -105,7 +123,7 @@ __device__ __forceinline__ void row_sum(float (&v)[N], float (*red)[N][16], int 
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            float s = 0.0f;
+            S s = 0;
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) s += red[slot][i][w];
             v[i] = s;
@@ -187,12 +205,64 @@ __device__ __forceinline__ void store_any(void* p, bool bf16, int64_t at, int64_
 
 // ---------------------------------------------------------------- forward --
 
+// The mean as two fp32 numbers (hi alone would put its rounding into every difference and,
+// squared, into the variance: a constant fp32 row of 10000.1 had z = -0.3).  The sum
+// of a row is exact where its elements are near one another, and its rounding small beside
+// the spread where they are not: fp32 is added in fp64; bf16, of 8 bits, in fp32, times
+// 2^-16, which keeps the largest of 2^16 columns in range and denormals whole.  A
+// constant row's hi is its value, and all differences are zeros.
+//
+// Differences from fp32 take hi away first, exact for an element near the mean, then lo.
+// Those from bf16 leave lo out: it is no more than 2^-25 of the mean, elements of one row are
+// equal or 2^-8 apart, so z takes it in one operation and the variance as its square
+// (8192 x 4096 bf16 in a graph 24.9 us; with lo in each difference 25.3, with sums in fp64 too 26.0).
+constexpr float kSumScale = 0x1p-16f;
+
+struct Mean {
+    float hi, lo;
+
+    __device__ __forceinline__ Mean(double sum, int64_t cols, double inv)
+        : hi((float)(sum * inv)), lo((float)(fma(-(double)hi, (double)cols, sum) * inv)) {}
+    __device__ __forceinline__ Mean(float sum, int64_t cols, double inv) {
+        const float m = sum / (float)cols;
+        hi = m * (1.0f / kSumScale);
+        lo = fmaf(-m, (float)cols, sum) * (float)inv * (1.0f / kSumScale);
+    }
+    __device__ __forceinline__ float off(float x) const { return (x - hi) - lo; }
+};
+// Squares whose sum is not between 2^-90 and fp32's largest number (one comparison of the bits of a
+// sum that is not negative).  The power of two that brings such a row's differences into
+// fp32's range; NaN stays.
+__device__ __forceinline__ bool row_unusual(float squares) {
+    return __float_as_uint(squares) - 0x12800000u > 0x7f7fffffu - 0x12800000u;
+}
+__device__ __forceinline__ float row_scale(float squares, float eps) {
+    if (!(squares < 0x1p-90f)) return 0x1p-96f;
+    return eps < 0x1p-90f ? 0x1p90f : 1.0f;
+}
+
+template <typename T>
+using RowSum = typename std::conditional<sizeof(T) == 2, float, double>::type;
+
+template <int N>
+__device__ __forceinline__ void add_to(double& sum, const float (&x)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum += (double)x[i];
+}
+template <int N>
+__device__ __forceinline__ void add_to(float& sum, const float (&x)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum = fmaf(x[i], kSumScale, sum);
+}
+
 // G lanes to a row, NV pieces of 16 bytes each; a block of B threads has B / G
 // rows at a time, and asks for the next ones while it reduces these.  KEEP: weight and
 // bias stay in registers, for all the block's rows.  T: x's type.
 template <typename T, int G, int NV, int B, bool KEEP>
 __global__ __launch_bounds__(B) void norm_kernel(NormArgs a) {
     constexpr int N = Piece<T>::kN;
+    constexpr bool kLater = sizeof(T) == 2;  // what the mean's lo is taken into
+    __shared__ RowSum<T> red_sum[1][1][16];
     __shared__ float red[2][1][16];
     const int lane = threadIdx.x % G;
     const int64_t cols = a.cols, step = (int64_t)gridDim.x * (B / G);
@@ -223,27 +293,50 @@ __global__ __launch_bounds__(B) void norm_kernel(NormArgs a) {
     }
     for (; row < a.rows; row += step) {
         float x[NV][N], s[1] = {0.0f};
+        RowSum<T> sum[1] = {0};
 #pragma unroll
         for (int j = 0; j < NV; ++j) Piece<T>::unpack(raw[j], x[j]);
         if (row + step < a.rows) fetch(row + step);
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
-#pragma unroll
-            for (int i = 0; i < N; ++i) s[0] += x[j][i];
-        row_sum<G, 1>(s, red, 0);
-        const float mean = s[0] / (float)cols;
-        s[0] = 0.0f;
+        for (int j = 0; j < NV; ++j) add_to(sum[0], x[j]);
+        row_sum<G>(sum, red_sum, 0);
+        const Mean mean(sum[0], cols, a.inv_cols);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int64_t c = ((int64_t)j * G + lane) * N;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                x[j][i] -= mean;
+                x[j][i] = kLater ? x[j][i] - mean.hi : mean.off(x[j][i]);
                 if (c + i < cols) s[0] = fmaf(x[j][i], x[j][i], s[0]);
             }
         }
-        row_sum<G, 1>(s, red, 1);
-        const float rstd = 1.0f / sqrtf(s[0] / (float)cols + a.eps);
+        row_sum<G>(s, red, 0);
+        auto reciprocal = [&](float squares, float scale) {
+            float var = squares / (float)cols;
+            if constexpr (kLater) {
+                const float lo = mean.lo * scale;
+                var = fmaf(-lo, lo, var);
+                var = var < 0.0f ? 0.0f : var;  // (NaN stays)
+            }
+            return scale / sqrtf(var + a.eps * scale * scale);
+        };
+        float rstd = reciprocal(s[0], 1.0f);
+        const float scale = row_unusual(s[0]) ? row_scale(s[0], a.eps) : 1.0f;
+        if (scale != 1.0f) {  // (all the row's lanes, or none)
+            s[0] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                const int64_t c = ((int64_t)j * G + lane) * N;
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const float d = x[j][i] * scale;
+                    if (c + i < cols) s[0] = fmaf(d, d, s[0]);
+                }
+            }
+            row_sum<G>(s, red, 1);
+            rstd = reciprocal(s[0], scale);
+        }
+        const float shift = -mean.lo * rstd;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int64_t c = ((int64_t)j * G + lane) * N;
@@ -251,11 +344,12 @@ __global__ __launch_bounds__(B) void norm_kernel(NormArgs a) {
             const int k = KEEP ? j : 0;
             if constexpr (!KEEP) affine(j, w[0], b[0]);
 #pragma unroll
-            for (int i = 0; i < N; ++i) x[j][i] = fmaf(x[j][i] * rstd, w[k][i], b[k][i]);
+            for (int i = 0; i < N; ++i)
+                x[j][i] = fmaf(kLater ? fmaf(x[j][i], rstd, shift) : x[j][i] * rstd, w[k][i], b[k][i]);
             store_any<N>(a.y, a.y_bf16, row * a.y_stride + c, cols - c, x[j]);
         }
         if (a.saved && lane == 0) {
-            a.saved[row] = mean;
+            a.saved[row] = mean.hi;
             a.saved[a.rows + row] = rstd;
         }
     }
@@ -265,40 +359,53 @@ constexpr int kLong = 1024;  // threads to a long row
 
 template <typename T>
 __global__ __launch_bounds__(kLong) void norm_long_kernel(NormArgs a) {
+    __shared__ double red_sum[1][1][16];
     __shared__ float red[2][1][16];
     const int64_t cols = a.cols;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const T* p = static_cast<const T*>(a.x) + row * a.x_stride;
         float s[1] = {0.0f}, x[8];
+        double sum[1] = {0.0};
         for (int64_t c = threadIdx.x * 8; c < cols; c += kLong * 8) {
             load8(p + c, cols - c, x);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) s[0] += x[i];
-        }
-        row_sum<kLong, 1>(s, red, 0);
-        const float mean = s[0] / (float)cols;
-        s[0] = 0.0f;
-        for (int64_t c = threadIdx.x * 8; c < cols; c += kLong * 8) {
-            load8(p + c, cols - c, x);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float d = x[i] - mean;
-                if (c + i < cols) s[0] = fmaf(d, d, s[0]);
+            if constexpr (sizeof(T) == 2) {
+                float part = 0.0f;
+                add_to(part, x);
+                sum[0] += (double)part * (1.0 / kSumScale);
+            } else {
+                add_to(sum[0], x);
             }
         }
-        row_sum<kLong, 1>(s, red, 1);
-        const float rstd = 1.0f / sqrtf(s[0] / (float)cols + a.eps);
+        row_sum<kLong>(sum, red_sum, 0);
+        const Mean mean(sum[0], cols, a.inv_cols);
+        float scale = 1.0f;
+        for (int pass = 0; pass < 2; ++pass) {  // (a second one where row_scale asks for it)
+            s[0] = 0.0f;
+            for (int64_t c = threadIdx.x * 8; c < cols; c += kLong * 8) {
+                load8(p + c, cols - c, x);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float d = mean.off(x[i]) * scale;
+                    if (c + i < cols) s[0] = fmaf(d, d, s[0]);
+                }
+            }
+            row_sum<kLong>(s, red, pass);
+            if (pass || !row_unusual(s[0])) break;
+            scale = row_scale(s[0], a.eps);
+            if (scale == 1.0f) break;
+        }
+        const float rstd = scale / sqrtf(s[0] / (float)cols + a.eps * scale * scale);
         for (int64_t c = threadIdx.x * 8; c < cols; c += kLong * 8) {
             float w[8] = {1, 1, 1, 1, 1, 1, 1, 1}, b[8] = {};
             if (a.weight) load8_any(a.weight, a.w_bf16, c, cols - c, w);
             if (a.bias) load8_any(a.bias, a.w_bf16, c, cols - c, b);
             load8(p + c, cols - c, x);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = fmaf((x[i] - mean) * rstd, w[i], b[i]);
+            for (int i = 0; i < 8; ++i) x[i] = fmaf(mean.off(x[i]) * rstd, w[i], b[i]);
             store8_any(a.y, a.y_bf16, row * a.y_stride + c, cols - c, x);
         }
         if (a.saved && threadIdx.x == 0) {
-            a.saved[row] = mean;
+            a.saved[row] = mean.hi;
             a.saved[a.rows + row] = rstd;
         }
     }
@@ -372,7 +479,7 @@ __global__ __launch_bounds__(B) void norm_backward_kernel(NormBackwardArgs a) {
             }
         }
         if (!a.dx) continue;
-        row_sum<G, 2>(s, red, slot);
+        row_sum<G>(s, red, slot);
         const float m0 = s[0] / (float)cols, m1 = s[1] / (float)cols;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
@@ -451,7 +558,7 @@ __global__ __launch_bounds__(kLong) void norm_dx_long_kernel(NormBackwardArgs a)
                 }
                 if (pass == 1) store8(static_cast<T*>(a.dx) + row * a.dx_stride + c, cols - c, z);
             }
-            if (pass == 0) row_sum<kLong, 2>(s, red, slot);
+            if (pass == 0) row_sum<kLong>(s, red, slot);
         }
     }
 }

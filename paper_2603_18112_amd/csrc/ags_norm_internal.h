@@ -16,6 +16,7 @@ struct NormArgs {
     void* y;
     float* saved;  // [2][rows], or NULL
     int64_t rows, cols, x_stride, y_stride;
+    double inv_cols;  // 1 / cols
     float eps;
     int32_t bf16, w_bf16, y_bf16;
 };
