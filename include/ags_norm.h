@@ -46,7 +46,8 @@ extern "C" {
 
 /* y [rows][y_stride] from x [rows, cols] (row i at element i * x_stride;
  * rows need their element's alignment only).  d_weight, d_bias: [cols] of
- * w_dtype; NULL stands for ones and zeros.  eps >= 0.  d_saved: fp32
+ * w_dtype; NULL stands for ones and zeros.  0 <= eps <= 3.4e38; in fp32, where one
+ * above zero is at least 1.2e-38.  d_saved: fp32
  * [2][rows], the means, then the rstds, for the backward pass; or NULL.
  * AGS_E_LAYOUT where cols exceeds 2^24 or rows 2^40. */
 ags_status ags_layer_norm(const void *d_x, int32_t dtype, int64_t rows, int64_t cols,

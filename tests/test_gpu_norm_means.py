@@ -119,3 +119,14 @@ def test_a_single_element_beside_large_ones():
             (ry, rm, rr), (ey, em, er) = ref.forward(x, None, None, 1e-5, F)
             for got, want, tol in ((y, ry, ey), (saved[0], rm, em), (saved[1], rr, er)):
                 assert ((got.double().cpu() - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("cols", [100, 5000, 40000])
+def test_eps_below_the_smallest_fp32_number(cols):
+    """Constant rows have z = 0 with any eps above zero."""
+    x = torch.full((3, cols), 7.0).cuda()
+    for eps in (1e-38, 1e-46, 1e-300):
+        y, saved = norm.layer_norm(x, eps=eps, save=True)
+        assert (y == 0).all() and torch.isfinite(saved).all()
+        dx, dw, db = norm.layer_norm_backward(torch.zeros_like(x), x, saved)
+        assert (dx == 0).all() and (dw == 0).all()
