@@ -13,7 +13,8 @@
  *
  * act is SiLU, g / (1 + e^-g), or GELU, g (1 + erf(g / sqrt 2)) / 2.
  *
- * Activations, weights and gradients are bf16, sums fp32.  h is rounded once.
+ * Activations, weights and gradients are bf16, sums fp32; act and act' are computed in
+ * fp32, act(g) within 2^-24 (20 + 2 g g) of itself.  h is rounded once.
  * The backward pass rounds dg and du to bf16, as operands of its products;
  * where g and u were saved they have 24 bits (16 of mantissa).  Sums are added in an order that
  * the sizes alone fix: equal inputs give equal results bit for bit.  NaN and

@@ -63,16 +63,22 @@ __global__ __launch_bounds__(256) void glu_pack_kernel(GluPackArgs a) {
 __device__ __forceinline__ float sigmoid(float g) {
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.44269504f));
 }
-// (1 + erf(g / sqrt 2)) / 2, and e^(-g g / 2): erfc(x) = p(t) e^(-x x), t = 1 / (1 + 0.3275911 x),
-// for x >= 0, p of degree 5: formula 7.1.26 of Abramowitz and Stegun, Handbook of
-// Mathematical Functions, within 1.5e-7.
+// (1 + erf(g / sqrt 2)) / 2, and e^(-g g / 2): erfc(x) = p(t) e^(-x x), t = 1 / (1 + 0.43 x), for
+// x >= 0, so that results far below zero keep their bits.  p, of degree 8, has the least largest
+// relative error for 0 <= x <= 9.5 (linear programming over 3500 points): 1.5 x 2^-24; the
+// whole is within (8 + 1.3 g g) 2^-24 in emulated fp32, the second part the exponent's rounding.
+// (Formula 7.1.26 of Abramowitz and Stegun, of degree 5, is within 1.5e-7 absolutely: 1 % off
+// at g = -8.  With it 8192 x 4096 -> 16384 forward takes 1.70 ms, so 1.71.)
 __device__ __forceinline__ float normal_below(float g, float* e) {
-    const float x = fabsf(g) * 0.70710678f, t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.0f));
+    const float x = fabsf(g), t = __builtin_amdgcn_rcpf(fmaf(0.304055930f, x, 1.0f));
     *e = __builtin_amdgcn_exp2f(g * g * -0.72134752f);
-    float p = fmaf(1.061405429f, t, -1.453152027f);
-    p = fmaf(p, t, 1.421413741f);
-    p = fmaf(p, t, -0.284496736f);
-    p = fmaf(p, t, 0.254829592f);
+    float p = fmaf(0.073707901f, t, -0.310373306f);
+    p = fmaf(p, t, 0.383705586f);
+    p = fmaf(p, t, -0.085725665f);
+    p = fmaf(p, t, 0.246844411f);
+    p = fmaf(p, t, 0.204951108f);
+    p = fmaf(p, t, 0.244375437f);
+    p = fmaf(p, t, 0.242514610f);
     const float q = 0.5f * p * t * *e;
     return g < 0.0f ? q : 1.0f - q;
 }
