@@ -62,8 +62,9 @@ extern "C" {
 #define AGS_MUON_MAX_STEPS 32
 
 /* The steps' coefficients.  They must keep singular values of up to 1 below
- * 1.38, and b s^2 + c s^4 below 3.9, the ranges that fp16 operands are scaled
- * for (AGS_E_ARG). */
+ * 1.41, but for the last step's, and b s^2 + c s^4 below 3.99, the ranges that
+ * fp16 operands are scaled for, with room for the operands' roundings: 5 |b| s^2 +
+ * 8 |c| s^4 times s 2^-11 a step, s the largest (AGS_E_ARG). */
 typedef struct {
     int32_t steps;          /* 1 .. AGS_MUON_MAX_STEPS                   */
     int32_t reserved;       /* must be 0                                 */

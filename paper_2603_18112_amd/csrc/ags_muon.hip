@@ -31,10 +31,10 @@ using mx::Unaligned;
 typedef unsigned short u16;
 typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 
-// Powers of two that bring the operands into fp16's range: X and A have
-// singular values up to 1.38 and 1.9, b A + c A A up to 3.9 (the schedule is
-// checked for these), so no element exceeds 2^16 - 2^5; elements down to 2^-14
-// of the scale keep 11 bits.  (The usual coefficients: 1.20, 1.45, 2.81.)
+// Powers of two that bring the operands into fp16's range, whose largest number is 2^16 - 2^5: X and A
+// have singular values up to 1.41 and 1.988, b A + c A A up to 3.99, roundings included (the
+// schedule is checked for these); elements down to 2^-14 of the scale keep 11 bits.  (The usual
+// coefficients: 1.25, 1.56, 2.84.)
 constexpr float kScaleX = 32768.0f, kScaleA = 32768.0f, kScaleB = 16384.0f;
 
 __device__ __forceinline__ unsigned pack_half(float x, float y) {
