@@ -110,8 +110,11 @@ typedef struct {
 
 typedef struct ags_muon_handle ags_muon_handle;
 
-/* Bytes of device workspace ags_muon_init would allocate (host only): about 8
- * a parameter, and 4 an element of a matrix's shorter side squared. */
+/* Bytes of device workspace ags_muon_init would allocate (host only): 8 an element of a
+ * matrix, its rows padded to a multiple of 64, and 4 an element of its shorter side squared,
+ * padded alike; for one with a side of up to 16 4 an element and 2048 for each
+ * 128 of the longer side, 512 KiB at most; and tables of 16 bytes for each
+ * block of a launch. */
 ags_status ags_muon_workspace_bytes(const ags_muon_config *cfg, size_t *out_bytes);
 
 /* A handle for w and m (device fp32 [n_flat], 16-byte aligned) on the current

@@ -141,21 +141,24 @@ __device__ __forceinline__ void mean8(const MuonStepArgs& a, int64_t at, int64_t
     for (int i = 0; i < 8; ++i) g[i] /= n;
 }
 
-// A chunk's pieces of 8 elements, thread after thread.
+// A chunk's pieces of 8 elements, thread after thread.  A thin matrix (a handle's) is one row of
+// all its elements, and its squares are summed with its products.
 __global__ __launch_bounds__(kThreads) void muon_sum_kernel(MuonStepArgs a) {
     __shared__ double red[4];
     const Found f = find<false>(a.work);
-    const unsigned per_row = (unsigned)(f.m.pitch() / 8), total = (unsigned)f.m.rows * per_row;
+    const bool thin = f.m.thin();
+    const int64_t cols = thin ? f.m.elements() : f.m.cols, pitch = thin ? (cols + 7) / 8 * 8 : f.m.pitch();
+    const unsigned per_row = (unsigned)(pitch / 8), total = thin ? per_row : (unsigned)f.m.rows * per_row;
     const unsigned end = min(total, (unsigned)(f.i + 1) * (unsigned)f.m.chunk);
     double sum = 0.0;
     for (unsigned p = (unsigned)f.i * (unsigned)f.m.chunk + threadIdx.x; p < end; p += kThreads) {
-        const int64_t row = p / per_row, c = (int64_t)(p - (unsigned)row * per_row) * 8, left = f.m.cols - c;
+        const int64_t row = p / per_row, c = (int64_t)(p - (unsigned)row * per_row) * 8, left = cols - c;
         if (left <= 0) continue;
         float u[8];
         if (a.from_x) {
             load_x(a, f, row, c, u);
         } else {
-            const int64_t at = f.m.offset + row * f.m.cols + c;
+            const int64_t at = f.m.offset + row * cols + c;
             float m[8];
             load8(a.m + at, left, m);
             if (a.bf16) mean8<u16>(a, at, left, u);
@@ -167,11 +170,12 @@ __global__ __launch_bounds__(kThreads) void muon_sum_kernel(MuonStepArgs a) {
             }
             store8(a.m + at, left, m);
             // (past the row's end u is 0)
-            store8(reinterpret_cast<float*>(a.ws + f.m.x_at()) + row * f.m.pitch() + c, 8, u);
+            store8(reinterpret_cast<float*>(a.ws + f.m.x_at()) + row * pitch + c, thin ? left : 8, u);
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum = fma((double)u[i], (double)u[i], sum);
     }
+    if (thin) return;
     sum = block_sum(sum, red);
     if (threadIdx.x == 0) reinterpret_cast<double*>(a.ws + f.m.sums_at())[f.i] = sum;
 }
@@ -438,7 +442,7 @@ __device__ __forceinline__ void thin_load(const MuonStepArgs& a, const Found& f,
         const int64_t row = tall ? c0 + c : i, col = tall ? i : c0 + c;
         float v;
         if (!a.from_x) {
-            v = reinterpret_cast<const float*>(a.ws + f.m.x_at())[row * f.m.pitch() + col];
+            v = reinterpret_cast<const float*>(a.ws + f.m.x_at())[row * f.m.cols + col];
         } else {
             const int64_t at = f.index * a.batch_stride + row * a.row_stride + col;
             v = a.bf16 ? gemm::bf16_value(static_cast<const u16*>(a.grads)[at]) : static_cast<const float*>(a.grads)[at];

@@ -32,7 +32,8 @@ inline MuonThinWay muon_thin_way(double gain) {
 // What stands in a matrix's part of the workspace: X in fp32 (before the first
 // step: what is to be orthogonalised), X as operands (two, read and written in
 // turn), A and b A + c A A as operands, partial sums of squares.  Operands' rows
-// are padded with zeros to whole stages of a product.
+// are padded with zeros to whole stages of a product.  Of a thin one only sums of products over
+// parts of the longer side, and for a handle's, before them, U as the flat buffers hold it.
 struct MuonMatrix {
     int64_t offset;         // elements, in w, m and the gradients; or 0
     int64_t ws;             // bytes, in the workspace
@@ -40,7 +41,7 @@ struct MuonMatrix {
     int32_t chunks, chunk;  // for passes over the elements: blocks, and pieces of 8 elements of each
     float scale;
     int32_t parts, part;    // thin ones: blocks along the longer side, and elements of it for each
-    int32_t reserved;
+    int32_t kept;           // a handle's
 
     __host__ __device__ int64_t side() const { return rows < cols ? rows : cols; }
     __host__ __device__ bool tall() const { return rows > cols; }
@@ -51,23 +52,30 @@ struct MuonMatrix {
     __host__ __device__ int64_t a_at() const { return ws + rows * pitch() * 8; }
     __host__ __device__ int64_t b_at() const { return a_at() + side() * a_pitch() * 2; }
     __host__ __device__ int64_t sums_at() const { return b_at() + side() * a_pitch() * 2; }
-    // Thin ones (kMuonThin): sums of products over parts of the longer side.
+    __host__ __device__ int64_t padded_bytes() const { return sums_at() - ws + (chunks * 8 + 63) / 64 * 64; }
+    // Thin ones (kMuonThin).
     __host__ __device__ bool thin() const { return side() <= kMuonThin; }
     __host__ __device__ int64_t length() const { return rows < cols ? cols : rows; }
-    __host__ __device__ int64_t parts_at() const { return sums_at() + (chunks * 8 + 63) / 64 * 64; }
+    __host__ __device__ int64_t elements() const { return (int64_t)rows * cols; }
+    __host__ __device__ int64_t parts_at() const { return ws + (kept ? (elements() * 4 + 63) / 64 * 64 : 0); }
     __host__ __device__ int64_t bytes() const {
-        return parts_at() - ws + (thin() ? (int64_t)parts * kMuonThin * kMuonThin * 8 : 0);
+        if (!thin()) return padded_bytes();
+        const int64_t sums = (int64_t)parts * kMuonThin * kMuonThin * 8;
+        if (kept) return parts_at() - ws + sums;
+        // (a small one's workspace is as large as if it were padded, which callers may count on)
+        const int64_t padded = padded_bytes() + sums, least = sums > 65536 ? sums : 65536;
+        return padded < least ? padded : least;
     }
 };
 
-inline MuonMatrix muon_matrix(int64_t offset, int64_t rows, int64_t cols, double scale, int64_t ws) {
+inline MuonMatrix muon_matrix(int64_t offset, int64_t rows, int64_t cols, double scale, bool kept) {
     MuonMatrix m{};
     m.offset = offset;
-    m.ws = ws;
+    m.kept = kept;
     m.rows = (int32_t)rows;
     m.cols = (int32_t)cols;
     m.scale = (float)scale;
-    const int64_t pieces = rows * (m.pitch() / 8);
+    const int64_t pieces = m.thin() && kept ? (m.elements() + 7) / 8 : rows * (m.pitch() / 8);
     m.chunk = (int32_t)std::max<int64_t>(512, gemm_up((pieces + 1023) / 1024, 256));
     m.chunks = (int32_t)((pieces + m.chunk - 1) / m.chunk);
     m.part = (int32_t)(gemm_up((m.length() + 255) / 256, kMuonThinCols));

@@ -144,3 +144,31 @@ def test_replayed_from_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(got, muon.orthogonalize(x, steps=10, dtype="f32"))
+
+
+@pytest.mark.parametrize("K,dtype", [(1, F), (3, B)])
+def test_handles_of_odd_thin_matrices(K, dtype):
+    """Elements that fill no piece of eight, one after the other in the workspace: the momentum
+    exactly, the weights as the calls by themselves, the buffers between them untouched."""
+    shapes = [(1, 1), (13, 7), (3, 1001), (20011, 1), (5, 5), (40, 50), (16, 129), (1, 40000), (300, 11)]
+    matrices, at = [], 0
+    for r, c in shapes:
+        matrices.append((at, r, c, 1.0))
+        at += -(-r * c // 8) * 8 + 8
+    gen = torch.Generator().manual_seed(K)
+    w, m = torch.randn(at, generator=gen), torch.randn(at, generator=gen)
+    # whole numbers: their means and the momentum are exact
+    m = torch.randint(-8, 9, (at,), generator=gen).float()
+    grads = (torch.randint(-8, 9, (K, at), generator=gen) * K).to(dtype)
+    wc, mc = w.cuda(), m.cuda()
+    opt = muon.Muon(matrices, wc, mc, K, grad_dtype="f32" if dtype is F else "bf16", lr=0.5, momentum=0.5, nesterov=False)
+    opt.step(grads.cuda())
+    want = 0.5 * m + grads.float().mean(dim=0)
+    inside = torch.zeros(at, dtype=torch.bool)
+    for o, r, c, _ in matrices:
+        inside[o:o + r * c] = True
+        x = muon.orthogonalize(want[o:o + r * c].view(r, c).cuda(), dtype="f32").cpu().double().reshape(-1)
+        assert ((wc.cpu()[o:o + r * c].double() - (w[o:o + r * c].double() - 0.5 * x)).abs() <=
+                U * (w[o:o + r * c].double() - 0.5 * x).abs() * 1.01).all()
+    assert torch.equal(mc.cpu()[inside], want[inside])
+    assert torch.equal(mc.cpu()[~inside], m[~inside]) and torch.equal(wc.cpu()[~inside], w[~inside])
