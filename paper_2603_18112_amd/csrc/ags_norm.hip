@@ -214,8 +214,9 @@ __device__ __forceinline__ void store_any(void* p, bool bf16, int64_t at, int64_
 //
 // Differences from fp32 take hi away first, exact for an element near the mean, then lo.
 // Those from bf16 leave lo out: it is no more than 2^-25 of the mean, elements of one row are
-// equal or 2^-8 apart, so z takes it in one operation and the variance as its square
-// (8192 x 4096 bf16 in a graph 24.9 us; with lo in each difference 25.3, with sums in fp64 too 26.0).
+// equal or 2^-8 apart, so z takes it in one operation and the variance as its square (8192 x
+// 4096 bf16 in a graph 24.9 us; with lo in each difference 25.3, with sums in fp64 too 26.0;
+// since the variance is a product, not a quotient, 24.3).
 constexpr float kSumScale = 0x1p-16f;
 
 struct Mean {
@@ -312,7 +313,7 @@ __global__ __launch_bounds__(B) void norm_kernel(NormArgs a) {
         }
         row_sum<G>(s, red, 0);
         auto reciprocal = [&](float squares, float scale) {
-            float var = squares / (float)cols;
+            float var = squares * (float)a.inv_cols;
             if constexpr (kLater) {
                 const float lo = mean.lo * scale;
                 var = fmaf(-lo, lo, var);
