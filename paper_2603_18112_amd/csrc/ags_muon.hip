@@ -142,13 +142,14 @@ __device__ __forceinline__ void mean8(const MuonStepArgs& a, int64_t at, int64_t
 }
 
 // A chunk's pieces of 8 elements, thread after thread.  A thin matrix (a handle's) is one row of
-// all its elements, and its squares are summed with its products.
+// all its elements (room for the last eight included), and its squares are summed with its products.
 __global__ __launch_bounds__(kThreads) void muon_sum_kernel(MuonStepArgs a) {
     __shared__ double red[4];
     const Found f = find<false>(a.work);
     const bool thin = f.m.thin();
-    const int64_t cols = thin ? f.m.elements() : f.m.cols, pitch = thin ? (cols + 7) / 8 * 8 : f.m.pitch();
-    const unsigned per_row = (unsigned)(pitch / 8), total = thin ? per_row : (unsigned)f.m.rows * per_row;
+    const int cols = thin ? f.m.rows * f.m.cols : f.m.cols;
+    const unsigned per_row = thin ? (unsigned)(cols + 7) / 8 : (unsigned)(f.m.pitch() / 8);
+    const unsigned total = thin ? per_row : (unsigned)f.m.rows * per_row;
     const unsigned end = min(total, (unsigned)(f.i + 1) * (unsigned)f.m.chunk);
     double sum = 0.0;
     for (unsigned p = (unsigned)f.i * (unsigned)f.m.chunk + threadIdx.x; p < end; p += kThreads) {
@@ -170,7 +171,7 @@ __global__ __launch_bounds__(kThreads) void muon_sum_kernel(MuonStepArgs a) {
             }
             store8(a.m + at, left, m);
             // (past the row's end u is 0)
-            store8(reinterpret_cast<float*>(a.ws + f.m.x_at()) + row * pitch + c, thin ? left : 8, u);
+            store8(reinterpret_cast<float*>(a.ws + f.m.x_at()) + row * f.m.pitch() + c, 8, u);
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum = fma((double)u[i], (double)u[i], sum);
