@@ -11,9 +11,10 @@
 //
 // All are bound by memory: x (and dy) read once and y (dx) written once, with a few
 // operations a byte.  Measured (us, bytes that have to move over the time): forward 8192 x
-// 4096 bf16 25.4 (5.3 TB/s; a copy's rate is 4.7), 5001 x 1000 fp32 11.5 (3.5), one row of
-// 4096 3.0; backward with both gradients 16384 x 8192 bf16 151 + 5 (5.2), 5001 x 1000 fp32
-// 15.2 + 3.9 (3.1).  Small ones are bound by a launch and two or three waits for memory.
+// 4096 bf16 25.5 (5.3 TB/s; a copy's rate is 4.7), 5001 x 1000 fp32 11.6 (3.5), one row of
+// 4096 3.1; backward with both gradients 16384 x 8192 bf16 151 + 5 (5.2), 5001 x 1000 fp32
+// 15.1 + 4.1 (3.1).  Small ones are bound by a launch and two or three waits for memory, long
+// rows by their three reads: 2048 x 65536 bf16 forward 215 (2.5), backward 246 + 108 + 8 (2.2).
 #include <type_traits>
 
 #include "ags_mx_device.h"

@@ -106,7 +106,8 @@ def _bf16(x, what, device=None):
 class Weight:
     """The two weights gate, up [n, k] of a gated block, in bf16, laid out for
     its products.  :meth:`update` stores new values (after an optimizer step)
-    in the same buffer."""
+    in the same buffer.  It is a copy that autograd does not see, of parameters
+    that require a gradient too: gated_linear_backward returns theirs."""
 
     def __init__(self, gate, up):
         gate, self.n, self.k, _ = _matrix(gate, "gate")
