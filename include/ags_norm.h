@@ -18,7 +18,8 @@
  * from the squares) and rounded once, where it is stored; but the mean is held in
  * 48 bits, so that a row far from zero loses nothing of its differences.  It is
  * saved in fp32, and the backward pass takes it as saved: its z is off by up to
- * 2^-24 |mean| rstd.  Where squared differences leave fp32's range they are scaled.
+ * 2^-24 |mean| rstd.  Differences must stay in fp32's range (a row's spread below
+ * 3.4e38); where their squares leave it they are scaled.
  * Sums are added in an order that the sizes alone fix: equal inputs give equal
  * results bit for bit.  A row that holds a NaN or an infinity has NaN in its whole y and dx, and
  * in what dweight sums; other rows' y and dx are untouched.  Constant rows
